@@ -48,7 +48,8 @@ typedef enum {
   FATHOM_ERR_WORKSPACE = -5    /* workspace missing or smaller than the *_workspace_size() */
 } fathom_status;
 
-typedef enum { FATHOM_F32 = 0, FATHOM_F16 = 1 } fathom_dtype;
+/* FATHOM_BF16 is a type of the paged cache's calls; the others refuse it. */
+typedef enum { FATHOM_F32 = 0, FATHOM_F16 = 1, FATHOM_BF16 = 2 } fathom_dtype;
 
 typedef enum {
   FATHOM_WATERFILL = 0,   /* Sec. 3.3 Eq. (wf): graded depths under a bit budget B */
@@ -63,6 +64,8 @@ typedef enum {
 #define FATHOM_DEV_TOPK_FALLBACK 4u  /* the fused filter under-collected and the exact unfiltered path ran */
 #define FATHOM_DEV_TOPK_SHORT 8u     /* fewer than k eligible keys: trailing slots hold index -1, value NaN */
 #define FATHOM_DEV_BAD_N 16u         /* n[u] < 0 or > 64 * nb_cap: that unit is treated as empty */
+#define FATHOM_DEV_BAD_PAGE 32u      /* a page number outside the pool, or a ring state that cannot be: see the paged calls */
+#define FATHOM_DEV_PAGES_SHORT 64u   /* fathom_paged_map: too few free pages, some requests kept their old length */
 
 /*
  * fathom_pack -- Sec. 3.2, Eq. (2): per-channel 4-bit quantisation with one
@@ -343,6 +346,160 @@ fathom_status fathom_klt_rotate_keys(const void* K, fathom_dtype kdt, int64_t ld
  */
 fathom_status fathom_klt_rotate_q(const void* q, fathom_dtype qdt, int U, int G, int D, const float* V,
                                   float* out, void* stream);
+
+/*
+ * Paged cache.  The K and V rows of S requests lie in P pages of `page` tokens,
+ * each page holding all H KV heads of its tokens: row t of page p, head h is
+ * the D elements at K[p*ld_page + h*ld_head + t*ld_tok] (V likewise), so both
+ * head-major ([P][H][page][D]) and token-major ([P][page][H][D]) pools are
+ * served.  table [S][ld_table] int32 (device) lists the pages of each request:
+ * position i of request s is row i % page of page table[s][i / page]; entries
+ * past the request's last page are not read.  A page number outside [0, P)
+ * raises BAD_PAGE wherever it is met and its rows count as absent; it never
+ * leads to an access outside the pool.  Unit u = s*H + h is KV head h of
+ * request s, and query heads h*G .. h*G + G - 1 of a request are its G heads.
+ *
+ * All calls: page a power of two in 16 .. 1024; 1 <= H <= 1024; S <=
+ * FATHOM_MAX_SEQS; ld_table*page < 2^31; K and V 16-byte aligned with strides
+ * that are multiples of 8 elements, ld_tok in [D, 2^20]; dt FATHOM_F16 or
+ * FATHOM_BF16.  Outside these: FATHOM_ERR_UNSUPPORTED for sizes and types,
+ * FATHOM_ERR_INVALID for pointers and strides.
+ */
+#define FATHOM_MAX_SEQS 4096 /* requests per call */
+typedef struct {
+  void* K;         /* written by fathom_paged_write only */
+  void* V;         /* (fathom_paged_pack does not read it: may be NULL) */
+  fathom_dtype dt;
+  int H;
+  int page;
+  int64_t P, ld_page, ld_head, ld_tok;
+} fathom_pages;
+
+/*
+ * fathom_paged_map -- block tables and slot maps from request lengths.  Request
+ * s goes from n_old[s] to n[s] tokens (fewer: it is cut back, 0: it ends).
+ * With pages(x) = ceil(x / page):
+ *   start[s]  = sum over r < s of max(n[r] - n_old[r], 0): where the rows of its
+ *               new tokens begin in arrays of new tokens; start[S] is their number.
+ *   Requests that grow take max(pages(n) - pages(n_old), 0) pages from the front
+ *   of the ring of free pages, in the order of s, into table[s][pages(n_old) ..];
+ *   requests that shrink return table[s][pages(n) .. pages(n_old)) to its end,
+ *   in the order of s (the entries are left as they were).  Pages returned by
+ *   a call are taken by later calls only.
+ *   slots[start[s] + i] = table[s][p / page]*page + p % page, p = n_old[s] + i;
+ *               every other slot below T is -1.
+ *   n_now[s]  = n[s], and n_unit[s*H + h] = n_now[s] for the per-unit calls.
+ * A request that cannot be served keeps n_now = n_old, takes no page, and its
+ * slots are -1: with PAGES_SHORT from the first request on whose pages exceed
+ * those left (and all after it that need pages); with BAD_N where its rows end
+ * past T.  Lengths outside [0, ld_table*page]: BAD_N, no rows, n_now = n_old, or
+ * 0 where n_old is outside.
+ *
+ *   n_old, n  [S] int64 (device).      table [S][ld_table] int32 (device, updated).
+ *   ring      [P] int32 (device, updated): the free pages are ring[(head + i) % P],
+ *             i < count.
+ *   state     [2] int64 (device): head in [0, P) and count in [0, P].
+ *   slots [T], start [S + 1], n_now [S], n_unit [S*H] (or NULL), state_out [2]:
+ *             int64 (device, written); n_now may be n_old or n, state_out may be
+ *             state, and no others may overlap.
+ * Device status: BAD_N, PAGES_SHORT, BAD_PAGE (a page number outside [0, P), a
+ * state outside its range: nothing is taken or returned; or more pages returned
+ * than the ring can hold: none is returned).
+ */
+fathom_status fathom_paged_map(const int64_t* n_old, const int64_t* n, int S, int H, int page,
+                               int32_t* table, int64_t ld_table, int32_t* ring, int64_t P,
+                               const int64_t* state, int64_t* slots, int64_t T, int64_t* start,
+                               int64_t* n_now, int64_t* n_unit, int64_t* state_out,
+                               uint32_t* dev_status, void* stream);
+
+/*
+ * fathom_paged_write -- the K and V rows of T new tokens to their slots: row
+ * (i, h) goes to row slots[i] % page of page slots[i] / page, head h, rounded
+ * to the pages' type (to nearest, ties to even).  Rows with a negative slot are
+ * skipped; a slot of P*page or more raises BAD_PAGE and is skipped.  Where two
+ * rows have one slot, either may stay.
+ *   Krows, Vrows  [T][H][D], row (i, h) at Krows[i*ldk_tok + h*ldk_head] (V: ldv_*);
+ *            sdt FATHOM_F32 or the pages' type; 16-byte aligned, strides >= 0 and
+ *            multiples of 16 bytes; T*H <= 2^30.
+ *   slots    [T] int64 (device).
+ * Device status: BAD_PAGE.
+ */
+fathom_status fathom_paged_write(const void* Krows, const void* Vrows, fathom_dtype sdt,
+                                 int64_t ldk_tok, int64_t ldk_head, int64_t ldv_tok,
+                                 int64_t ldv_head, const int64_t* slots, int64_t T, int D,
+                                 const fathom_pages* pages, uint32_t* dev_status, void* stream);
+
+/*
+ * fathom_paged_pack -- fathom_pack (n_old NULL) and fathom_pack_append over
+ * keys in pages: the bit-plane store of U = S*H units, unit s*H + h from KV
+ * head h of request s, the same bits as from contiguous rows (bf16 keys convert
+ * to fp32 exactly).  Rows of absent pages count as zeros.
+ *   n, n_old [S] int64 (device), per request; nb_cap, planes, scales, max_new as
+ *            fathom_pack_append, with U = S*H <= 65535.
+ * Device status: as fathom_pack_append (n above ld_table*page is BAD_N too), BAD_PAGE.
+ */
+fathom_status fathom_paged_pack(const fathom_pages* pages, const int32_t* table, int64_t ld_table,
+                                const int64_t* n_old, const int64_t* n, int64_t max_new, int S, int D,
+                                int64_t nb_cap, uint64_t* planes, uint16_t* scales,
+                                uint32_t* dev_status, void* stream);
+
+/*
+ * fathom_paged_sparse_attn -- fathom_sparse_attn over rows in pages (rows of
+ * absent pages are skipped): the same set, order and fp32 arithmetic, bit for
+ * bit that of contiguous rows.
+ *   q        [S*H][G][D] (qdt FATHOM_F32, FATHOM_F16 or FATHOM_BF16), contiguous.
+ *   n        [S] int64 (device), per request.
+ *   idx, k, n_sink, n_local, sm_scale, out, ws: as fathom_sparse_attn with
+ *            U = S*H, the workspace of fathom_sparse_attn_workspace_size; S*H*G <= 65535.
+ * Device status: BAD_N (n outside [0, ld_table*page]: the request is empty), BAD_PAGE.
+ */
+fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fathom_pages* pages,
+                                       const int32_t* table, int64_t ld_table, const int64_t* n, int S,
+                                       int G, int D, const int32_t* idx, int k, int n_sink, int n_local,
+                                       float sm_scale, float* out, void* ws, size_t ws_bytes,
+                                       uint32_t* dev_status, void* stream);
+
+/*
+ * fathom_paged_attn -- dense attention of new tokens over a paged cache that
+ * holds them already (fathom_paged_write): chunks of prompts, single tokens and
+ * mixtures, each request with start[s + 1] - start[s] new tokens, the last ones of
+ * its n[s].  New token i of request s is at position p = n[s] - new + i; its
+ * query head hg sees the positions j in [max(first, 0), max(p + 1, min(prefix[s], n[s]))):
+ *   z_j = sm_scale * q . K_j;  softcap > 0: z_j = softcap * tanh(z_j / softcap);
+ *   slopes: z_j -= slopes[hg] * |p - j|;
+ *   out = sum_j softmax_j(z) V_j, and 0 where it sees no position.
+ * Rows outside what a token sees do not enter its result, whatever they hold.
+ *
+ *   q        [T][H*G][D] of the pages' type, row (i, hg) at q[i*ldq_tok + hg*ldq_head];
+ *            16-byte aligned, strides >= 0 and multiples of 8 elements.
+ *   start    [S + 1] int64 (device), non-decreasing, 0 <= start[0], start[S] <= T:
+ *            rows of T outside every request are left as they were in out.
+ *   n        [S] int64 (device): tokens of each request, the new ones among them.
+ *   max_new  host bound on start[s + 1] - start[s]; selects work and sizes the launch.
+ *   sm_scale, softcap  finite; softcap 0: none.      slopes [H*G] fp32 or NULL.
+ *   prefix   [S] int64 or NULL: leading positions that every token of the request
+ *            sees, later ones among them.
+ *   first    [T] int64 or NULL: the first position that a token sees (the start of
+ *            its document).
+ *   out      [T][H*G][D] of the pages' type, contiguous, 16-byte aligned.
+ *   ws       device workspace of at least fathom_paged_attn_workspace_size(T, S,
+ *            H, G, max_new) bytes, 256-byte aligned (any contents).
+ * Scores, softmax statistics and sums are fp32; the probabilities of chunks (more
+ * than 32 query rows, new*G, of a request) are rounded to the pages' type once, those of
+ * fewer rows enter as a sum of two such values.  Sums are in an order that
+ * depends on the lengths and sizes only.  1 <= G <= 8; T*H*G <= 2^30.
+ * Device status: BAD_N (n outside [0, ld_table*page], more new tokens than n or than
+ * max_new, a start out of order or outside [0, T]: that request's rows are left as
+ * they were), BAD_PAGE.
+ */
+fathom_status fathom_paged_attn(const void* q, int64_t ldq_tok, int64_t ldq_head,
+                                const fathom_pages* pages, const int32_t* table, int64_t ld_table,
+                                const int64_t* start, const int64_t* n, int S, int64_t T,
+                                int64_t max_new, int G, int D, float sm_scale, float softcap,
+                                const float* slopes, const int64_t* prefix, const int64_t* first,
+                                void* out, void* ws, size_t ws_bytes, uint32_t* dev_status,
+                                void* stream);
+size_t fathom_paged_attn_workspace_size(int64_t T, int S, int H, int G, int64_t max_new);
 
 /* Human-readable name of a status code (static storage). */
 const char* fathom_status_string(fathom_status s);

@@ -26,6 +26,7 @@ FATHOM_ERR_HIP = -4
 FATHOM_ERR_WORKSPACE = -5
 FATHOM_F32 = 0
 FATHOM_F16 = 1
+FATHOM_BF16 = 2
 FATHOM_WATERFILL = 0
 FATHOM_UNIFORM_TOPR = 1
 FATHOM_MAX_K = 8192
@@ -34,14 +35,25 @@ FATHOM_DEV_NONFINITE = 2
 FATHOM_DEV_TOPK_FALLBACK = 4
 FATHOM_DEV_TOPK_SHORT = 8
 FATHOM_DEV_BAD_N = 16
+FATHOM_DEV_BAD_PAGE = 32
+FATHOM_DEV_PAGES_SHORT = 64
+FATHOM_MAX_SEQS = 4096
 
 EXPORTED = (
     "fathom_pack", "fathom_pack_append", "fathom_gather_store", "fathom_alloc_depths", "fathom_scan", "fathom_topk", "fathom_topk_workspace_size",
     "fathom_scan_topk", "fathom_scan_topk_ex", "fathom_scan_topk_workspace_size", "fathom_scan_topk_noalloc",
     "fathom_scan_topk_noalloc_capacity", "fathom_sparse_attn",
     "fathom_sparse_attn_workspace_size", "fathom_klt_calibrate", "fathom_klt_calibrate_workspace_size",
-    "fathom_klt_rotate_keys", "fathom_klt_rotate_q", "fathom_status_string", "fathom_version",
+    "fathom_klt_rotate_keys", "fathom_klt_rotate_q", "fathom_paged_map", "fathom_paged_write", "fathom_paged_pack",
+    "fathom_paged_attn", "fathom_paged_attn_workspace_size", "fathom_paged_sparse_attn", "fathom_status_string",
+    "fathom_version",
 )
+
+
+class _Pages(C.Structure):
+    """fathom_pages (include/fathom.h)."""
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("dt", C.c_int), ("H", C.c_int), ("page", C.c_int),
+                ("P", C.c_int64), ("ld_page", C.c_int64), ("ld_head", C.c_int64), ("ld_tok", C.c_int64)]
 
 
 class FathomError(RuntimeError):
@@ -79,6 +91,13 @@ def lib() -> C.CDLL:
             "fathom_klt_calibrate": [P, i32, i64, i64, P, i64, i32, i32, P, P, P, P, C.c_size_t, P, P],
             "fathom_klt_rotate_keys": [P, i32, i64, i64, P, i64, i32, i32, P, P, P, i64, P, P],
             "fathom_klt_rotate_q": [P, i32, i32, i32, i32, P, P, P],
+            "fathom_paged_map": [P, P, i32, i32, i32, P, i64, P, i64, P, P, i64, P, P, P, P, P, P],
+            "fathom_paged_write": [P, P, i32, i64, i64, i64, i64, P, i64, i32, P, P, P],
+            "fathom_paged_pack": [P, P, i64, P, P, i64, i32, i32, i64, P, P, P, P],
+            "fathom_paged_sparse_attn": [P, i32, P, P, i64, P, i32, i32, i32, P, i32, i32, i32, C.c_float, P, P,
+                                         C.c_size_t, P, P],
+            "fathom_paged_attn": [P, i64, i64, P, P, i64, P, P, i32, i64, i64, i32, i32, C.c_float, C.c_float, P, P, P,
+                                  P, P, C.c_size_t, P, P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -94,6 +113,8 @@ def lib() -> C.CDLL:
         L.fathom_sparse_attn_workspace_size.restype = C.c_size_t
         L.fathom_klt_calibrate_workspace_size.argtypes = [i32]
         L.fathom_klt_calibrate_workspace_size.restype = C.c_size_t
+        L.fathom_paged_attn_workspace_size.argtypes = [i64, i32, i32, i32, i64]
+        L.fathom_paged_attn_workspace_size.restype = C.c_size_t
         L.fathom_status_string.argtypes = [st]
         L.fathom_status_string.restype = C.c_char_p
         L.fathom_version.argtypes = []
@@ -369,4 +390,164 @@ def fathom_klt_rotate_q(q, V, out=None, stream=None):
     if out is None:
         out = torch.empty((U, G, D), dtype=torch.float32, device=q.device)
     _check(lib().fathom_klt_rotate_q(_p(q), _dt(q), U, G, D, _p(V), _p(out), _stream(stream)), "fathom_klt_rotate_q")
+    return out
+
+
+# ---------------------------------------------------------------- paged cache
+def _paged_dt(t: torch.Tensor) -> int:
+    return FATHOM_BF16 if t.dtype == torch.bfloat16 else _dt(t)
+
+
+def _pages(K, V):
+    """fathom_pages of pools K and V [P][H][page][D] (any strides with channel stride 1; V None: keys only)."""
+    if K.dim() != 4 or K.stride(3) != 1 or K.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("pages are fp16 or bf16 [P][H][page][D] with channel stride 1")
+    if V is not None and (V.shape != K.shape or V.stride() != K.stride() or V.dtype != K.dtype):
+        raise ValueError("K and V pages need the same shape, strides and type")
+    P, H, page, _ = K.shape
+    return _Pages(K.data_ptr(), None if V is None else V.data_ptr(), _paged_dt(K), H, page, P, K.stride(0), K.stride(1),
+                  K.stride(2))
+
+
+def _table(table):
+    if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+        raise ValueError("table is contiguous int32 [S][pages]")
+    return table.shape[1]
+
+
+def _here(*ts):
+    """Device tensors of the current device: the launch goes to its stream."""
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in ts:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError("paged calls take tensors of the current device")
+
+
+def _int64(S, **ts):
+    for name, t in ts.items():
+        if t is not None and (t.dtype != torch.int64 or t.numel() != S or not t.is_contiguous()):
+            raise ValueError(f"{name} is contiguous int64 of {S} elements")
+
+
+def fathom_paged_map(n_old, n, page, table, ring, state, T, H=1, slots=None, start=None, n_now=None, n_unit=None,
+                     state_out=None, dev_status=None, stream=None):
+    """Block tables and slot maps: requests go from n_old [S] to n [S] tokens, taking pages from the ring of free ones
+    (ring [P] i32, state = (head, count)) into table [S][pages] i32 or returning them -> (slots [T], start [S + 1],
+    n_now [S], n_unit [S*H], state_out [2]).  table and ring are updated; a request that cannot be served keeps its
+    length (dev_status)."""
+    _here(n_old, n, table, ring, state, slots, start, n_now, n_unit, state_out, dev_status)
+    S, T, dev = table.shape[0], int(T), n.device
+    ld = _table(table)
+    i64 = dict(dtype=torch.int64, device=dev)
+    slots = torch.empty((T,), **i64) if slots is None else slots
+    start = torch.empty((S + 1,), **i64) if start is None else start
+    n_now = torch.empty((S,), **i64) if n_now is None else n_now
+    n_unit = torch.empty((S * H,), **i64) if n_unit is None else n_unit
+    state_out = torch.empty((2,), **i64) if state_out is None else state_out
+    _int64(S, n_old=n_old, n=n, n_now=n_now)
+    _int64(2, state=state, state_out=state_out)
+    _int64(T, slots=slots)
+    _int64(S + 1, start=start)
+    _int64(S * H, n_unit=n_unit)
+    if ring.dtype != torch.int32 or not ring.is_contiguous():
+        raise ValueError("ring is contiguous int32")
+    _check(lib().fathom_paged_map(_p(n_old), _p(n), S, int(H), int(page), _p(table), ld, _p(ring), ring.numel(),
+                                  _p(state), _p(slots), T, _p(start), _p(n_now), _p(n_unit), _p(state_out),
+                                  _p(dev_status), _stream(stream)), "fathom_paged_map")
+    return slots, start, n_now, n_unit, state_out
+
+
+def fathom_paged_write(K, V, slots, Kpages, Vpages, dev_status=None, stream=None):
+    """New rows K, V [T][H][D] (the pages' type, or fp32: rounded) to their slots [T] in the pages [P][H][page][D];
+    negative slots are skipped."""
+    _here(K, V, slots, Kpages, Vpages, dev_status)
+    pg = _pages(Kpages, Vpages)
+    T, H, D = K.shape
+    if V.shape != K.shape or V.dtype != K.dtype or H != pg.H or D != Kpages.shape[3]:
+        raise ValueError("K and V are [T][H][D] of one type, with the pages' H and D")
+    if K.stride(2) != 1 or V.stride(2) != 1:
+        raise ValueError("channel stride must be 1")
+    _int64(T, slots=slots)
+    _check(lib().fathom_paged_write(_p(K), _p(V), _paged_dt(K), K.stride(0), K.stride(1), V.stride(0), V.stride(1),
+                                    _p(slots), T, D, C.byref(pg), _p(dev_status), _stream(stream)),
+           "fathom_paged_write")
+    return Kpages, Vpages
+
+
+def fathom_paged_pack(Kpages, table, n, planes, scales, n_old=None, max_new=0, dev_status=None, stream=None):
+    """fathom_pack (n_old None) or fathom_pack_append over keys in pages: units s*H + h of planes [S*H][D][4][nb_cap] and
+    scales [S*H][D][nb_cap]; n and n_old [S] are per request."""
+    _here(Kpages, table, n, planes, scales, n_old, dev_status)
+    pg = _pages(Kpages, None)
+    S = table.shape[0]
+    ld = _table(table)
+    _int64(S, n=n, n_old=n_old)
+    U, D, _, nb_cap = planes.shape
+    if U != S * pg.H or tuple(scales.shape) != (U, D, nb_cap) or not planes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("planes and scales are contiguous [S*H][D][4][nb_cap] and [S*H][D][nb_cap]")
+    _check(lib().fathom_paged_pack(C.byref(pg), _p(table), ld, _p(n_old), _p(n), int(max_new), S, D, nb_cap, _p(planes),
+                                   _p(scales), _p(dev_status), _stream(stream)), "fathom_paged_pack")
+    return planes, scales
+
+
+def fathom_paged_sparse_attn(q, Kpages, Vpages, table, n, idx, n_sink=0, n_local=0, sm_scale=None, out=None,
+                             dev_status=None, stream=None, ws=None):
+    """fathom_sparse_attn over rows in pages: q [S*H][G][D], idx [S*H][G][k], n [S] per request -> out [S*H][G][D] fp32."""
+    _here(q, Kpages, Vpages, table, n, idx, out, ws, dev_status)
+    pg = _pages(Kpages, Vpages)
+    U, G, D = q.shape
+    S = table.shape[0]
+    ld = _table(table)
+    _int64(S, n=n)
+    if U != S * pg.H or not q.is_contiguous():
+        raise ValueError("q is contiguous [S*H][G][D]")
+    if idx is not None and (idx.dtype != torch.int32 or not idx.is_contiguous() or tuple(idx.shape[:2]) != (U, G)):
+        raise ValueError("idx is contiguous int32 [S*H][G][k]")
+    k = 0 if idx is None else idx.shape[-1]
+    sm_scale = 1.0 / (D ** 0.5) if sm_scale is None else sm_scale
+    if out is None:
+        out = torch.empty((U, G, D), dtype=torch.float32, device=q.device)
+    if out.dtype != torch.float32 or out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("out is contiguous fp32 [S*H][G][D]")
+    ws = _ws(fathom_sparse_attn_workspace_size(U, G, k, n_sink, n_local), ws, q.device)
+    _check(lib().fathom_paged_sparse_attn(_p(q), _paged_dt(q), C.byref(pg), _p(table), ld, _p(n), S, G, D, _p(idx), k,
+                                          int(n_sink), int(n_local), C.c_float(sm_scale), _p(out), _p(ws),
+                                          ws.numel() * ws.element_size(), _p(dev_status), _stream(stream)),
+           "fathom_paged_sparse_attn")
+    return out
+
+
+def fathom_paged_attn_workspace_size(T, S, H, G, max_new) -> int:
+    return int(lib().fathom_paged_attn_workspace_size(int(T), int(S), int(H), int(G), int(max_new)))
+
+
+def fathom_paged_attn(q, Kpages, Vpages, table, start, n, max_new, sm_scale=None, softcap=0.0, slopes=None, prefix=None,
+                      first=None, out=None, ws=None, dev_status=None, stream=None):
+    """Causal attention of the new tokens q [T][H*G][D] (request s: rows start[s] .. start[s + 1], the last ones of its
+    n[s] tokens) over the paged cache -> out [T][H*G][D] of the pages' type.  softcap: scores capped by
+    softcap * tanh(z / softcap); slopes [H*G] fp32: bias -slope * distance; prefix [S]: leading positions that every token
+    sees; first [T]: the first position that a token sees.  max_new bounds start[s + 1] - start[s]."""
+    _here(q, Kpages, Vpages, table, start, n, slopes, prefix, first, out, ws, dev_status)
+    pg = _pages(Kpages, Vpages)
+    T, HG, D = q.shape
+    S = table.shape[0]
+    ld = _table(table)
+    _int64(S, n=n, prefix=prefix)
+    _int64(S + 1, start=start)
+    _int64(T, first=first)
+    if q.dtype != Kpages.dtype or q.stride(2) != 1 or HG % pg.H:
+        raise ValueError("q is [T][H*G][D] of the pages' type with channel stride 1")
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.numel() != HG or not slopes.is_contiguous()):
+        raise ValueError("slopes is contiguous fp32 [H*G]")
+    G = HG // pg.H
+    sm_scale = 1.0 / (D ** 0.5) if sm_scale is None else sm_scale
+    if out is None:
+        out = torch.empty((T, HG, D), dtype=q.dtype, device=q.device)
+    if out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("out is contiguous [T][H*G][D] of the pages' type")
+    ws = _ws(fathom_paged_attn_workspace_size(T, S, pg.H, G, max_new), ws, q.device)
+    _check(lib().fathom_paged_attn(_p(q), q.stride(0), q.stride(1), C.byref(pg), _p(table), ld, _p(start), _p(n), S, T,
+                                   int(max_new), G, D, C.c_float(sm_scale), C.c_float(softcap), _p(slopes), _p(prefix),
+                                   _p(first), _p(out), _p(ws), ws.numel() * ws.element_size(), _p(dev_status),
+                                   _stream(stream)), "fathom_paged_attn")
     return out

@@ -1,6 +1,6 @@
 // C ABI of libfathom: host-side argument checks, then asynchronous launches.
 // Declarations and the meaning of every argument are in include/fathom.h.
-#include "common.hpp"
+#include "paged.hpp"
 
 namespace fathom {
 fathom_status launch_gather(const uint64_t*, const uint16_t*, const uint8_t*, int, int64_t, uint64_t*, uint16_t*,
@@ -31,6 +31,19 @@ fathom_status launch_klt_calibrate(const void*, fathom_dtype, int64_t, int64_t, 
 fathom_status launch_klt_rotate_keys(const void*, fathom_dtype, int64_t, int64_t, const int64_t*, int64_t, int,
                                      const float*, const float*, float*, int64_t, uint32_t*, hipStream_t);
 fathom_status launch_klt_rotate_q(const void*, fathom_dtype, int, int, const float*, float*, hipStream_t);
+fathom_status launch_paged_map(const int64_t*, const int64_t*, int, int, int, int32_t*, int64_t, int32_t*, int64_t,
+                               const int64_t*, int64_t*, int64_t, int64_t*, int64_t*, int64_t*, int64_t*, uint32_t*,
+                               hipStream_t);
+fathom_status launch_paged_write(const void*, const void*, fathom_dtype, int64_t, int64_t, int64_t, int64_t,
+                                 const int64_t*, int64_t, const fathom_pages&, uint32_t*, hipStream_t);
+fathom_status launch_paged_pack(const Paged&, bool, const int64_t*, const int64_t*, int64_t, int, int64_t, uint64_t*,
+                                uint16_t*, uint32_t*, hipStream_t);
+fathom_status launch_paged_sparse_attn(const void*, fathom_dtype, const Paged&, bool, const int64_t*, int, int,
+                                       const int32_t*, int, int, int, float, float*, void*, uint32_t*, hipStream_t);
+size_t paged_attn_ws_bytes(int64_t T, int S, int H, int G, int64_t max_new);
+fathom_status launch_paged_attn(const void*, int64_t, int64_t, const Paged&, bool, const int64_t*, const int64_t*, int,
+                                int64_t, int64_t, int, float, float, const float*, const int64_t*, const int64_t*,
+                                void*, void*, uint32_t*, hipStream_t);
 }  // namespace fathom
 
 using namespace fathom;
@@ -54,6 +67,24 @@ fathom_status check_store(const uint64_t* planes, const uint16_t* scales, const 
   if (!planes || !scales || !n || !q || !depths) return FATHOM_ERR_INVALID;
   if (!aligned(planes, 8) || !aligned(scales, 2) || !aligned(n, 8) || !aligned(q, dtype_size(qdt)))
     return FATHOM_ERR_INVALID;
+  return FATHOM_OK;
+}
+
+// Checks shared by the paged calls; *c is filled where they pass.
+fathom_status check_pages(const fathom_pages* p, int D, bool v, const int32_t* table, int64_t ld_table, int S, Paged* c) {
+  if (!p) return FATHOM_ERR_INVALID;
+  if (S < 0 || p->P < 0 || ld_table < 0) return FATHOM_ERR_INVALID;
+  if (D != kD || (p->dt != FATHOM_F16 && p->dt != FATHOM_BF16)) return FATHOM_ERR_UNSUPPORTED;
+  if (S > kMaxSeqs || p->H < 1 || p->H > 1024) return FATHOM_ERR_UNSUPPORTED;
+  if (p->page < 16 || p->page > 1024 || (p->page & (p->page - 1))) return FATHOM_ERR_UNSUPPORTED;
+  if (p->P > 0x7fffffff || ld_table > 0x7fffffff / p->page) return FATHOM_ERR_UNSUPPORTED;
+  if (p->ld_tok > ((int64_t)1 << 20)) return FATHOM_ERR_UNSUPPORTED;
+  if (p->ld_tok < D || p->ld_head < 0 || p->ld_page < 0) return FATHOM_ERR_INVALID;
+  if ((p->ld_tok | p->ld_head | p->ld_page) & 7) return FATHOM_ERR_INVALID;
+  if (p->P > 0 && (!p->K || (v && !p->V))) return FATHOM_ERR_INVALID;
+  if (!aligned(p->K, 16) || (v && !aligned(p->V, 16)) || !aligned(table, 4)) return FATHOM_ERR_INVALID;
+  *c = {reinterpret_cast<const uint16_t*>(p->K), reinterpret_cast<const uint16_t*>(p->V), p->H,
+        __builtin_ctz((unsigned)p->page), (int32_t)p->P, p->ld_page, p->ld_head, p->ld_tok, table, ld_table};
   return FATHOM_OK;
 }
 
@@ -297,6 +328,108 @@ fathom_status fathom_sparse_attn(const void* q, fathom_dtype qdt, const uint16_t
   if (ws_bytes < attn_ws_bytes(U, G, k, n_sink, n_local)) return FATHOM_ERR_WORKSPACE;
   return launch_sparse_attn(q, qdt, Krows, Vrows, ld_tok, ld_unit, n, U, G, idx, k, n_sink, n_local, sm_scale, out,
                             ws, dev_status, as_stream(stream));
+}
+
+fathom_status fathom_paged_map(const int64_t* n_old, const int64_t* n, int S, int H, int page, int32_t* table,
+                               int64_t ld_table, int32_t* ring, int64_t P, const int64_t* state, int64_t* slots,
+                               int64_t T, int64_t* start, int64_t* n_now, int64_t* n_unit, int64_t* state_out,
+                               uint32_t* dev_status, void* stream) {
+  if (S < 0 || ld_table < 0 || P < 0 || T < 0) return FATHOM_ERR_INVALID;
+  if (S > kMaxSeqs || H < 1 || H > 1024) return FATHOM_ERR_UNSUPPORTED;
+  if (page < 16 || page > 1024 || (page & (page - 1))) return FATHOM_ERR_UNSUPPORTED;
+  if (P > 0x7fffffff || T > 0x7fffffff || ld_table > 0x7fffffff / page) return FATHOM_ERR_UNSUPPORTED;
+  if (!state || !start || !state_out) return FATHOM_ERR_INVALID;
+  if (S > 0 && (!n_old || !n || !n_now)) return FATHOM_ERR_INVALID;
+  if ((S > 0 && ld_table > 0 && !table) || (P > 0 && !ring) || (T > 0 && !slots)) return FATHOM_ERR_INVALID;
+  if (!aligned(n_old, 8) || !aligned(n, 8) || !aligned(state, 8) || !aligned(slots, 8) || !aligned(start, 8) ||
+      !aligned(n_now, 8) || !aligned(n_unit, 8) || !aligned(state_out, 8) || !aligned(table, 4) || !aligned(ring, 4))
+    return FATHOM_ERR_INVALID;
+  return launch_paged_map(n_old, n, S, H, __builtin_ctz((unsigned)page), table, ld_table, ring, P, state, slots, T,
+                          start, n_now, n_unit, state_out, dev_status, as_stream(stream));
+}
+
+fathom_status fathom_paged_write(const void* Krows, const void* Vrows, fathom_dtype sdt, int64_t ldk_tok,
+                                 int64_t ldk_head, int64_t ldv_tok, int64_t ldv_head, const int64_t* slots, int64_t T,
+                                 int D, const fathom_pages* pages, uint32_t* dev_status, void* stream) {
+  Paged c;
+  const fathom_status e = check_pages(pages, D, true, nullptr, 0, 0, &c);
+  if (e != FATHOM_OK) return e;
+  if (T < 0) return FATHOM_ERR_INVALID;
+  if (sdt != FATHOM_F32 && sdt != pages->dt) return FATHOM_ERR_UNSUPPORTED;
+  if (T > ((int64_t)1 << 30) / c.H) return FATHOM_ERR_UNSUPPORTED;
+  const int64_t vec = sdt == FATHOM_F32 ? 4 : 8;  // elements per 16 bytes
+  if (ldk_tok < 0 || ldk_head < 0 || ldv_tok < 0 || ldv_head < 0) return FATHOM_ERR_INVALID;
+  if ((ldk_tok | ldk_head | ldv_tok | ldv_head) & (vec - 1)) return FATHOM_ERR_INVALID;
+  if (T == 0) return FATHOM_OK;
+  if (!Krows || !Vrows || !slots) return FATHOM_ERR_INVALID;
+  if (!aligned(Krows, 16) || !aligned(Vrows, 16) || !aligned(slots, 8)) return FATHOM_ERR_INVALID;
+  return launch_paged_write(Krows, Vrows, sdt, ldk_tok, ldk_head, ldv_tok, ldv_head, slots, T, *pages, dev_status,
+                            as_stream(stream));
+}
+
+fathom_status fathom_paged_pack(const fathom_pages* pages, const int32_t* table, int64_t ld_table,
+                                const int64_t* n_old, const int64_t* n, int64_t max_new, int S, int D, int64_t nb_cap,
+                                uint64_t* planes, uint16_t* scales, uint32_t* dev_status, void* stream) {
+  Paged c;
+  const fathom_status e = check_pages(pages, D, false, table, ld_table, S, &c);
+  if (e != FATHOM_OK) return e;
+  if (nb_cap < 0 || (n_old && max_new < 0)) return FATHOM_ERR_INVALID;
+  if (nb_cap > ((int64_t)1 << 25) || (int64_t)S * c.H > 65535) return FATHOM_ERR_UNSUPPORTED;
+  if (S == 0 || nb_cap == 0) return FATHOM_OK;
+  if (!n || !planes || !scales || (ld_table > 0 && !table)) return FATHOM_ERR_INVALID;
+  if (!aligned(planes, 8) || !aligned(scales, 2) || !aligned(n, 8) || !aligned(n_old, 8)) return FATHOM_ERR_INVALID;
+  return launch_paged_pack(c, pages->dt == FATHOM_BF16, n, n_old, max_new, S * c.H, nb_cap, planes, scales, dev_status,
+                           as_stream(stream));
+}
+
+fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fathom_pages* pages,
+                                       const int32_t* table, int64_t ld_table, const int64_t* n, int S, int G, int D,
+                                       const int32_t* idx, int k, int n_sink, int n_local, float sm_scale, float* out,
+                                       void* ws, size_t ws_bytes, uint32_t* dev_status, void* stream) {
+  if (k < 0 || n_sink < 0 || n_local < 0) return FATHOM_ERR_INVALID;
+  Paged c;
+  const fathom_status e = check_pages(pages, D, true, table, ld_table, S, &c);
+  if (e != FATHOM_OK) return e;
+  if (G < 1 || G > kMaxG || (!dtype_ok(qdt) && qdt != FATHOM_BF16)) return FATHOM_ERR_UNSUPPORTED;
+  if (k > FATHOM_MAX_K || (int64_t)n_sink + n_local > attn_max_sink_local() || (int64_t)S * c.H * G > 65535)
+    return FATHOM_ERR_UNSUPPORTED;
+  if (S == 0) return FATHOM_OK;
+  if (!q || !n || !out || (k > 0 && !idx) || (ld_table > 0 && !table)) return FATHOM_ERR_INVALID;
+  if (!aligned(q, dtype_size(qdt)) || !aligned(out, 4) || !aligned(n, 8) || !aligned(idx, 4))
+    return FATHOM_ERR_INVALID;
+  if (!ws || !aligned(ws, 256)) return FATHOM_ERR_INVALID;
+  if (ws_bytes < attn_ws_bytes(S * c.H, G, k, n_sink, n_local)) return FATHOM_ERR_WORKSPACE;
+  return launch_paged_sparse_attn(q, qdt, c, pages->dt == FATHOM_BF16, n, S * c.H, G, idx, k, n_sink, n_local,
+                                  sm_scale, out, ws, dev_status, as_stream(stream));
+}
+
+size_t fathom_paged_attn_workspace_size(int64_t T, int S, int H, int G, int64_t max_new) {
+  if (T <= 0 || S <= 0 || S > kMaxSeqs || H <= 0 || H > 1024 || G <= 0 || G > kMaxG || max_new <= 0) return 0;
+  if (T > ((int64_t)1 << 30) / (H * G)) return 0;
+  return paged_attn_ws_bytes(T, S, H, G, max_new);
+}
+
+fathom_status fathom_paged_attn(const void* q, int64_t ldq_tok, int64_t ldq_head, const fathom_pages* pages,
+                                const int32_t* table, int64_t ld_table, const int64_t* start, const int64_t* n, int S,
+                                int64_t T, int64_t max_new, int G, int D, float sm_scale, float softcap,
+                                const float* slopes, const int64_t* prefix, const int64_t* first, void* out, void* ws,
+                                size_t ws_bytes, uint32_t* dev_status, void* stream) {
+  Paged c;
+  const fathom_status e = check_pages(pages, D, true, table, ld_table, S, &c);
+  if (e != FATHOM_OK) return e;
+  if (T < 0 || max_new < 0) return FATHOM_ERR_INVALID;
+  if (G < 1 || G > kMaxG || T > ((int64_t)1 << 30) / (c.H * G)) return FATHOM_ERR_UNSUPPORTED;
+  if (!(sm_scale - sm_scale == 0.0f) || !(softcap >= 0.0f) || softcap - softcap != 0.0f) return FATHOM_ERR_INVALID;
+  if (ldq_tok < 0 || ldq_head < 0 || ((ldq_tok | ldq_head) & 7)) return FATHOM_ERR_INVALID;
+  if (S == 0 || T == 0 || max_new == 0) return FATHOM_OK;
+  if (!q || !start || !n || !out || !table || ld_table < 1 || pages->P < 1) return FATHOM_ERR_INVALID;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(start, 8) || !aligned(n, 8) || !aligned(slopes, 4) ||
+      !aligned(prefix, 8) || !aligned(first, 8))
+    return FATHOM_ERR_INVALID;
+  if (!ws || !aligned(ws, 256)) return FATHOM_ERR_INVALID;
+  if (ws_bytes < paged_attn_ws_bytes(T, S, c.H, G, max_new)) return FATHOM_ERR_WORKSPACE;
+  return launch_paged_attn(q, ldq_tok, ldq_head, c, pages->dt == FATHOM_BF16, start, n, S, T, max_new, G, sm_scale,
+                           softcap, slopes, prefix, first, out, ws, dev_status, as_stream(stream));
 }
 
 }  // extern "C"

@@ -12,7 +12,7 @@
 // partial output o = sum exp(z - m) V into the caller's workspace.  A second
 // kernel combines the chunks of each head:
 //   out = sum_c e^(m_c - M) o_c / sum_c e^(m_c - M) d_c.
-#include "common.hpp"
+#include "paged.hpp"
 
 namespace fathom {
 
@@ -51,13 +51,52 @@ __device__ __forceinline__ uint4 load8h(const uint16_t* p) {
   return make_uint4(gload_u32(p), gload_u32(p + 2), gload_u32(p + 4), gload_u32(p + 6));
 }
 
+// Where the rows of a unit lie, their types, and a request's tokens: rows one after
+// another, or in pages (their absent rows count as not selected).  VEC: 16-byte loads.
+template <bool VEC_>
+struct FlatRows {
+  static constexpr bool VEC = VEC_, BF = false;
+  using Off = int32_t;
+  const uint16_t *K, *V;
+  int64_t ld_tok, ld_unit;
+  const int64_t* n;
+  __device__ int64_t tokens(int u) const { return *(const __attribute__((address_space(1))) int64_t*)(n + u); }
+  __device__ int64_t limit() const { return INT64_MAX; }
+  __device__ int64_t base(int u) const { return (int64_t)u * ld_unit; }
+  __device__ Off row(int, int32_t i, uint32_t&) const { return i; }
+  __device__ int64_t at(Off o) const { return (int64_t)o * ld_tok; }
+  __device__ float query(const void* q, fathom_dtype t, int64_t i) const { return load_q(q, t, i); }
+};
+template <bool BF_>
+struct PagedRows {
+  static constexpr bool VEC = true, BF = BF_;
+  using Off = int64_t;
+  const uint16_t *K, *V;
+  Paged c;
+  const int64_t* n;
+  __device__ int64_t tokens(int u) const { return *(const __attribute__((address_space(1))) int64_t*)(n + u / c.H); }
+  __device__ int64_t limit() const { return c.ld_table << c.shift; }
+  __device__ int64_t base(int) const { return 0; }
+  __device__ Off row(int u, int32_t i, uint32_t& flags) const {
+    const int s = u / c.H;
+    return row_offset(c, s, u - s * c.H, i, flags);
+  }
+  __device__ int64_t at(Off o) const { return o; }
+  __device__ float query(const void* q, fathom_dtype t, int64_t i) const {
+    if (t == FATHOM_BF16) return bf16_bits_to_float(((const __attribute__((address_space(1))) uint16_t*)q)[i]);
+    return load_q(q, t, i);
+  }
+};
+template <bool BF>
+__device__ __forceinline__ float row_value(uint32_t w, int hi) {
+  if constexpr (BF) return __uint_as_float(hi ? w & 0xFFFF0000u : w << 16);
+  return half_bits_to_float((uint16_t)(hi ? w >> 16 : w & 0xFFFFu));
+}
+
 // What a wave needs of a call: head h of unit u, its row r = u G + h.
 struct AttnArgs {
   const void* q;
   fathom_dtype qdt;
-  const uint16_t *Krows, *Vrows;
-  int64_t ld_tok, ld_unit;
-  const int64_t* n;
   int G;
   const int32_t* idx;
   int k, n_sink, n_local;
@@ -66,13 +105,12 @@ struct AttnArgs {
 };
 
 // One chunk of row r by one wave: put(0, m), put(1, d) and put(2 + c, o_c).
-template <bool VEC, class Put>
-__device__ __forceinline__ void attn_chunk(const AttnArgs& a, int r, int c, Put put) {
+template <class Rows, class Put>
+__device__ __forceinline__ void attn_chunk(const AttnArgs& a, const Rows& rows, int r, int c, Put put) {
   const int u = r / a.G, h = r % a.G, lane = threadIdx.x & 63;
   const int n_sink = a.n_sink, n_local = a.n_local, k = a.k, G = a.G;
-  const int64_t ld_tok = a.ld_tok;
-  int64_t nu = *(const __attribute__((address_space(1))) int64_t*)(a.n + u);
-  if (nu < 0) {
+  int64_t nu = rows.tokens(u);
+  if (nu < 0 || nu > rows.limit()) {
     if (lane == 0 && c == 0) set_status(a.st, FATHOM_DEV_BAD_N);
     nu = 0;
   }
@@ -92,28 +130,34 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs& a, int r, int c, Put 
       if (v >= ns && v < l0) myrow = v;
     }
   }
+  typename Rows::Off myoff = -1;  // where it is in the unit's rows (or the pages)
+  if (myrow >= 0) {
+    uint32_t flags = 0;
+    myoff = rows.row(u, myrow, flags);
+    if (flags) set_status(a.st, flags);
+  }
   // ---- K and V of the rows: lane group g = lane / 16 takes position 4 s + g,
   // lane x = lane mod 16 channels 8x .. 8x + 7 ----
   const int g = lane >> 4, x = lane & 15;
-  const uint16_t* Ku = a.Krows + (int64_t)u * a.ld_unit + 8 * x;
-  const uint16_t* Vu = a.Vrows + (int64_t)u * a.ld_unit + 8 * x;
-  int32_t row[kRowSteps];
+  const uint16_t* Ku = rows.K + rows.base(u) + 8 * x;
+  const uint16_t* Vu = rows.V + rows.base(u) + 8 * x;
+  typename Rows::Off row[kRowSteps];
   uint4 kv[kRowSteps], vv[kRowSteps];
 #pragma unroll
   for (int s = 0; s < kRowSteps; ++s) {
-    row[s] = __shfl(myrow, 4 * s + g, kWave);
+    row[s] = __shfl(myoff, 4 * s + g, kWave);
     kv[s] = make_uint4(0u, 0u, 0u, 0u);
     vv[s] = make_uint4(0u, 0u, 0u, 0u);
     if (row[s] >= 0) {
-      kv[s] = load8h<VEC>(Ku + (int64_t)row[s] * ld_tok);
-      vv[s] = load8h<VEC>(Vu + (int64_t)row[s] * ld_tok);
+      kv[s] = load8h<Rows::VEC>(Ku + rows.at(row[s]));
+      vv[s] = load8h<Rows::VEC>(Vu + rows.at(row[s]));
     }
   }
   float qv[8];
   {
     const int64_t qo = ((int64_t)u * G + h) * kD + 8 * x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) qv[e] = load_q(a.q, a.qdt, qo + e);
+    for (int e = 0; e < 8; ++e) qv[e] = rows.query(a.q, a.qdt, qo + e);
   }
   // ---- logits ----
   float z[kRowSteps];
@@ -124,8 +168,8 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs& a, int r, int c, Put 
     float d = 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      d = __fmaf_rn(qv[2 * e], half_bits_to_float((uint16_t)(w[e] & 0xFFFFu)), d);
-      d = __fmaf_rn(qv[2 * e + 1], half_bits_to_float((uint16_t)(w[e] >> 16)), d);
+      d = __fmaf_rn(qv[2 * e], row_value<Rows::BF>(w[e], 0), d);
+      d = __fmaf_rn(qv[2 * e + 1], row_value<Rows::BF>(w[e], 1), d);
     }
 #pragma unroll
     for (int m = 1; m < 16; m <<= 1) d = __fadd_rn(d, __shfl_xor(d, m, kWave));
@@ -152,8 +196,8 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs& a, int r, int c, Put 
     const uint32_t w[4] = {vv[s].x, vv[s].y, vv[s].z, vv[s].w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      o[2 * e] = __fmaf_rn(pz, half_bits_to_float((uint16_t)(w[e] & 0xFFFFu)), o[2 * e]);
-      o[2 * e + 1] = __fmaf_rn(pz, half_bits_to_float((uint16_t)(w[e] >> 16)), o[2 * e + 1]);
+      o[2 * e] = __fmaf_rn(pz, row_value<Rows::BF>(w[e], 0), o[2 * e]);
+      o[2 * e + 1] = __fmaf_rn(pz, row_value<Rows::BF>(w[e], 1), o[2 * e + 1]);
     }
   }
   // the four lane groups hold disjoint rows: sum across them
@@ -174,12 +218,13 @@ __device__ __forceinline__ void attn_chunk(const AttnArgs& a, int r, int c, Put 
   }
 }
 
-template <bool VEC>
-__global__ __launch_bounds__(kAttnThreads) void attn_chunk_kernel(AttnArgs a, int S, float* __restrict__ ws) {
+template <class Rows>
+__global__ __launch_bounds__(kAttnThreads) void attn_chunk_kernel(AttnArgs a, Rows rows, int S,
+                                                                 float* __restrict__ ws) {
   const int r = blockIdx.y, c = blockIdx.x * kAttnWaves + (threadIdx.x >> 6);  // this wave's chunk
   if (c >= S) return;
   float* wp = ws + ((int64_t)r * S + c) * kPart;
-  attn_chunk<VEC>(a, r, c, [&](int i, float v) { gstore_f(wp + i, v); });
+  attn_chunk(a, rows, r, c, [&](int i, float v) { gstore_f(wp + i, v); });
 }
 
 // Rows of at most kRowChunks chunks (one wave each; the launch's rule): one
@@ -190,13 +235,13 @@ __global__ __launch_bounds__(kAttnThreads) void attn_chunk_kernel(AttnArgs a, in
 // 11.0.
 constexpr int kRowChunks = 16;
 constexpr int kRowThreads = 1024;
-template <bool VEC>
-__global__ __launch_bounds__(kRowThreads) void attn_row_kernel(AttnArgs a, int S, float* __restrict__ out) {
+template <class Rows>
+__global__ __launch_bounds__(kRowThreads) void attn_row_kernel(AttnArgs a, Rows rows, int S, float* __restrict__ out) {
   __shared__ float part[kRowChunks][kPart];
   __shared__ float em[kRowChunks], po[kCombGroups][kD];
   const int r = blockIdx.x, tid = threadIdx.x, nt = blockDim.x;
   for (int c = tid >> 6; c < S; c += nt >> 6)
-    attn_chunk<VEC>(a, r, c, [&](int i, float v) { part[c][i] = v; });
+    attn_chunk(a, rows, r, c, [&](int i, float v) { part[c][i] = v; });
   __syncthreads();
   float M = -__builtin_huge_valf();
   for (int c = 0; c < S; ++c) M = fmaxf(M, part[c][0]);
@@ -285,17 +330,11 @@ __global__ __launch_bounds__(kCombThreads) void attn_combine_kernel(const float*
   }
 }
 
-fathom_status launch_sparse_attn(const void* q, fathom_dtype qdt, const uint16_t* Krows, const uint16_t* Vrows,
-                                 int64_t ld_tok, int64_t ld_unit, const int64_t* n, int U, int G,
-                                 const int32_t* idx, int k, int n_sink, int n_local, float sm_scale, float* out,
-                                 void* ws, uint32_t* st, hipStream_t s) {
-  if (U == 0) return FATHOM_OK;
-  int S = attn_chunks(k, n_sink, n_local);
+template <class Rows>
+static fathom_status launch_rows(const AttnArgs& a, const Rows& rows_at, int U, float* out, void* ws, hipStream_t s) {
+  const int G = a.G;
+  int S = attn_chunks(a.k, a.n_sink, a.n_local);
   if (S < 1) S = 1;
-  const AttnArgs a = {q, qdt, Krows, Vrows, ld_tok, ld_unit, n, G, idx, k, n_sink, n_local, sm_scale, st};
-  // 16-byte row loads when every row start is 16-byte aligned
-  const bool vec = ((reinterpret_cast<uintptr_t>(Krows) | reinterpret_cast<uintptr_t>(Vrows)) & 15) == 0 &&
-                   (ld_tok & 7) == 0 && (ld_unit & 7) == 0;
   // With more rows than CUs a 16-wave workgroup per row gains nothing (512 rows of
   // 16 chunks: 29.2 us against 28.1 in two launches), and with few rows the chunks
   // of a row are better spread over the idle CUs from some length on (4 or 32 rows:
@@ -305,18 +344,38 @@ fathom_status launch_sparse_attn(const void* q, fathom_dtype qdt, const uint16_t
   const int rows = U * G;
   if (S <= kRowChunks / 2 || (S <= kRowChunks && rows <= 256 && S <= 9 + rows / 22)) {
     const dim3 threads(S <= 4 ? 256 : S <= 8 ? 512 : kRowThreads);
-    if (vec) hipLaunchKernelGGL(attn_row_kernel<true>, dim3((unsigned)(U * G)), threads, 0, s, a, S, out);
-    else hipLaunchKernelGGL(attn_row_kernel<false>, dim3((unsigned)(U * G)), threads, 0, s, a, S, out);
+    hipLaunchKernelGGL(attn_row_kernel<Rows>, dim3((unsigned)(U * G)), threads, 0, s, a, rows_at, S, out);
     FATHOM_LAUNCH_CHECK();
     return FATHOM_OK;
   }
   float* w = reinterpret_cast<float*>(ws);
   const dim3 grid((unsigned)((S + kAttnWaves - 1) / kAttnWaves), (unsigned)(U * G));
-  if (vec) hipLaunchKernelGGL(attn_chunk_kernel<true>, grid, dim3(kAttnThreads), 0, s, a, S, w);
-  else hipLaunchKernelGGL(attn_chunk_kernel<false>, grid, dim3(kAttnThreads), 0, s, a, S, w);
+  hipLaunchKernelGGL(attn_chunk_kernel<Rows>, grid, dim3(kAttnThreads), 0, s, a, rows_at, S, w);
   hipLaunchKernelGGL(attn_combine_kernel, dim3((unsigned)(U * G)), dim3(kCombThreads), 0, s, w, S, out);
   FATHOM_LAUNCH_CHECK();
   return FATHOM_OK;
+}
+
+fathom_status launch_sparse_attn(const void* q, fathom_dtype qdt, const uint16_t* Krows, const uint16_t* Vrows,
+                                 int64_t ld_tok, int64_t ld_unit, const int64_t* n, int U, int G,
+                                 const int32_t* idx, int k, int n_sink, int n_local, float sm_scale, float* out,
+                                 void* ws, uint32_t* st, hipStream_t s) {
+  if (U == 0) return FATHOM_OK;
+  const AttnArgs a = {q, qdt, G, idx, k, n_sink, n_local, sm_scale, st};
+  // 16-byte row loads when every row start is 16-byte aligned
+  const bool vec = ((reinterpret_cast<uintptr_t>(Krows) | reinterpret_cast<uintptr_t>(Vrows)) & 15) == 0 &&
+                   (ld_tok & 7) == 0 && (ld_unit & 7) == 0;
+  if (vec) return launch_rows(a, FlatRows<true>{Krows, Vrows, ld_tok, ld_unit, n}, U, out, ws, s);
+  return launch_rows(a, FlatRows<false>{Krows, Vrows, ld_tok, ld_unit, n}, U, out, ws, s);
+}
+
+fathom_status launch_paged_sparse_attn(const void* q, fathom_dtype qdt, const Paged& c, bool bf16, const int64_t* n,
+                                       int U, int G, const int32_t* idx, int k, int n_sink, int n_local,
+                                       float sm_scale, float* out, void* ws, uint32_t* st, hipStream_t s) {
+  if (U == 0) return FATHOM_OK;
+  const AttnArgs a = {q, qdt, G, idx, k, n_sink, n_local, sm_scale, st};
+  if (bf16) return launch_rows(a, PagedRows<true>{c.K, c.V, c, n}, U, out, ws, s);
+  return launch_rows(a, PagedRows<false>{c.K, c.V, c, n}, U, out, ws, s);
 }
 
 int attn_max_sink_local() { return kMaxSinkLocal; }

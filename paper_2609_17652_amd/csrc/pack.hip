@@ -29,11 +29,15 @@
 // appends and the packs whose 16-block workgroups would leave CUs idle (below).
 // pack_append_kernel: a token a lane; it serves the appends of a decode step.
 //
+// The keys are a unit's rows one after another, or rows in pages (PagedKeys): 16
+// tokens from a multiple of 16 lie in one page, so a lane of an item looks up one
+// page number; an append's lane its own.
+//
 // Append (n_old given): a block's fp16 scale depends on every token in it, so
 // a unit growing from n_old to n tokens re-packs blocks floor(n_old/64) ..
 // ceil(n/64)-1 from the keys (the last partial block together with the new
 // tokens); the grid then covers at most max_blocks blocks per unit.
-#include "common.hpp"
+#include "paged.hpp"
 
 namespace fathom {
 
@@ -56,6 +60,35 @@ struct PackItem {
   static constexpr int kPerBlock = kD / (16 * kCh);    // items per block
 };
 
+typedef __bf16 bf16_t;
+template <typename KT>
+constexpr bool kIsBf16 = __is_same(KT, bf16_t);
+
+// Where a unit's keys lie.  rows(): the address of row 0 of a lane's 16 rows from
+// token tok (a multiple of 16 in the unit), nullptr where they are absent.
+template <typename KT>
+struct FlatKeys {
+  using Key = KT;
+  const KT* K;
+  int64_t ld_tok, ld_unit;
+  __device__ int len_index(int u) const { return u; }
+  __device__ int64_t limit(int64_t cap) const { return cap; }
+  __device__ const KT* rows(int u, int64_t tok, uint32_t&) const { return K + (int64_t)u * ld_unit + tok * ld_tok; }
+};
+template <typename KT>
+struct PagedKeys {
+  using Key = KT;
+  Paged c;
+  int64_t ld_tok;
+  __device__ int len_index(int u) const { return u / c.H; }
+  __device__ int64_t limit(int64_t cap) const { return min(cap, c.ld_table << c.shift); }
+  __device__ const KT* rows(int u, int64_t tok, uint32_t& flags) const {
+    const int s = u / c.H;
+    const int64_t o = row_offset(c, s, u - s * c.H, tok, flags);
+    return o < 0 ? nullptr : reinterpret_cast<const KT*>(c.K) + o;
+  }
+};
+
 typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
 typedef _Float16 v2f16 __attribute__((ext_vector_type(2)));
 
@@ -76,6 +109,7 @@ template <typename KT>
 __device__ __forceinline__ float item_value(const uint4& r, int e) {
   const uint32_t w[4] = {r.x, r.y, r.z, r.w};
   if constexpr (sizeof(KT) == 4) return __uint_as_float(w[e]);
+  if constexpr (kIsBf16<KT>) return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
   return half_bits_to_float((uint16_t)(w[e >> 1] >> (16 * (e & 1))));
 }
 
@@ -110,9 +144,10 @@ __device__ __forceinline__ bool item_max(const uint4 (&r)[kRows], float (&m)[Pac
         const uint32_t w = i == 0 ? r[t].x : i == 1 ? r[t].y : i == 2 ? r[t].z : r[t].w;
         a = __builtin_elementwise_max(a, __builtin_bit_cast(v2u16, w & 0x7FFF7FFFu));
       }
-      m[2 * i] = half_bits_to_float(a[0]);
-      m[2 * i + 1] = half_bits_to_float(a[1]);
-      bad |= a[0] >= 0x7C00u || a[1] >= 0x7C00u;
+      m[2 * i] = kIsBf16<KT> ? bf16_bits_to_float(a[0]) : half_bits_to_float(a[0]);
+      m[2 * i + 1] = kIsBf16<KT> ? bf16_bits_to_float(a[1]) : half_bits_to_float(a[1]);
+      constexpr uint32_t inf = kIsBf16<KT> ? 0x7F80u : 0x7C00u;
+      bad |= a[0] >= inf || a[1] >= inf;
     }
   }
   return bad;
@@ -125,6 +160,9 @@ __device__ __forceinline__ void add_zero(uint4& r) {
   for (int i = 0; i < 4; ++i) {
     if constexpr (sizeof(KT) == 4) {
       w[i] = __float_as_uint(__fadd_rn(__uint_as_float(w[i]), 0.0f));
+    } else if constexpr (kIsBf16<KT>) {
+      const uint32_t lo = w[i] << 16, hi = w[i] & 0xFFFF0000u;
+      w[i] = (lo == 0x80000000u ? 0u : lo >> 16) | (hi == 0x80000000u ? 0u : hi);
     } else {
       const v2f16 zero = {(_Float16)0.0f, (_Float16)0.0f};
       w[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2f16, w[i]) + zero);
@@ -134,20 +172,26 @@ __device__ __forceinline__ void add_zero(uint4& r) {
 }
 
 // The item's rows: row t of a lane is token tok0 + 16g + t, channels from c
-// (tokens past nu read as zero).
-template <typename KT>
-__device__ __forceinline__ void load_item(const KT* __restrict__ Ku, int64_t ld_tok, int64_t tok0, int64_t nu, int c,
-                                          uint4 (&r)[kRows]) {
+// (tokens past nu, and rows that are absent, read as zero).  tok0 < nu.
+template <class Keys>
+__device__ __forceinline__ void load_item(const Keys& k, int u, int64_t tok0, int64_t nu, int c, uint4 (&r)[kRows],
+                                          uint32_t& flags) {
   const int g = (threadIdx.x & 63) >> 4;
-  const KT* p = Ku + (tok0 + kRows * g) * ld_tok + c;
+  const int left = nu - tok0 >= kBlockTokens ? kRows : (int)(nu - tok0) - kRows * g;  // valid rows of this lane
+  const auto* p = k.rows(u, left > 0 ? tok0 + kRows * g : tok0, flags);
+  if (!p) {
+#pragma unroll
+    for (int t = 0; t < kRows; ++t) r[t] = make_uint4(0u, 0u, 0u, 0u);
+    return;
+  }
+  p += c;
   if (tok0 + kBlockTokens <= nu) {
 #pragma unroll
-    for (int t = 0; t < kRows; ++t) r[t] = *reinterpret_cast<const uint4*>(p + t * ld_tok);
+    for (int t = 0; t < kRows; ++t) r[t] = *reinterpret_cast<const uint4*>(p + t * k.ld_tok);
   } else {
-    const int left = (int)(nu - tok0) - kRows * g;  // valid rows of this lane, when in 1 .. 15
 #pragma unroll
-    for (int t = 0; t < kRows; ++t) {  // rows past the end re-read the last token and drop it
-      r[t] = *reinterpret_cast<const uint4*>(p + (int64_t)min(t, left - 1) * ld_tok);
+    for (int t = 0; t < kRows; ++t) {  // rows past the end re-read the last one (or the block's first) and drop it
+      r[t] = *reinterpret_cast<const uint4*>(p + (int64_t)max(min(t, left - 1), 0) * k.ld_tok);
       if (t >= left) r[t] = make_uint4(0u, 0u, 0u, 0u);
     }
   }
@@ -201,7 +245,7 @@ __device__ __forceinline__ void quantise_item(uint4 (&r)[kRows], uint64_t vmask,
         const float t1 = __builtin_copysignf(s4, v);
         const float d1 = __fsub_rn(v, t1);
         float d2, d3;
-        if constexpr (sizeof(KT) == 4) {
+        if constexpr (sizeof(KT) == 4 || kIsBf16<KT>) {
           const float t2 = __fadd_rn(t1, __builtin_copysignf(s2, d1));
           d2 = __fsub_rn(v, t2);
           const float t3 = __fadd_rn(t2, __builtin_copysignf(s1, d2));
@@ -266,21 +310,20 @@ __device__ __forceinline__ uint64_t valid_mask(int64_t left) {
   return left >= kBlockTokens ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1;
 }
 
-template <typename KT>
-__global__ __launch_bounds__(kPackThreads, 4) void pack_tile_kernel(const KT* __restrict__ K, int64_t ld_tok,
-                                                                   int64_t ld_unit, const int64_t* __restrict__ n,
+template <class Keys>
+__global__ __launch_bounds__(kPackThreads, 4) void pack_tile_kernel(Keys keys, const int64_t* __restrict__ n,
                                                                    int64_t nb_cap, uint64_t* __restrict__ planes,
                                                                    uint16_t* __restrict__ scales,
                                                                    uint32_t* __restrict__ st) {
+  using KT = typename Keys::Key;
   using P = PackItem<KT>;
   __shared__ __attribute__((aligned(16))) uint32_t outw[kD * kTilePitch];
   __shared__ uint16_t outs[kD * kTileBlocks];
   const int u = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int x = lane & 15, g = lane >> 4;
-  const int64_t nu = unit_tokens(n, u, nb_cap * kBlockTokens, tid == 0 ? st : nullptr);
+  const int64_t nu = unit_tokens(n, keys.len_index(u), keys.limit(nb_cap * kBlockTokens), tid == 0 ? st : nullptr);
   const int64_t b0 = (int64_t)blockIdx.x * kTileBlocks;
   const int nbw = nb_cap - b0 < kTileBlocks ? (int)(nb_cap - b0) : kTileBlocks;
-  const KT* Ku = K + (int64_t)u * ld_unit;
   uint32_t flags = 0;
   for (int it = wave; it < nbw * P::kPerBlock; it += kPackWaves) {
     const int bb = it / P::kPerBlock, c = (it % P::kPerBlock) * 16 * P::kCh + x * P::kCh;
@@ -289,7 +332,7 @@ __global__ __launch_bounds__(kPackThreads, 4) void pack_tile_kernel(const KT* __
     uint16_t a16[P::kSets];
     if (tok0 < nu) {
       uint4 r[kRows];
-      load_item<KT>(Ku, ld_tok, tok0, nu, c, r);
+      load_item(keys, u, tok0, nu, c, r, flags);
       quantise_item<KT, 0, P::kSets>(r, valid_mask(nu - tok0), w, a16, flags);
     } else {
 #pragma unroll
@@ -328,9 +371,9 @@ __global__ __launch_bounds__(kPackThreads, 4) void pack_tile_kernel(const KT* __
 }
 
 // Sets S0 .. S0 + SN - 1 of the item of block b from channel c of unit u, stored as they are.
-template <typename KT, int S0, int SN>
-__device__ __forceinline__ void direct_item(const KT* Ku, int64_t ld_tok, int64_t b, int64_t nu, int u, int c,
-                                            int64_t nb_cap, uint64_t* __restrict__ planes, uint16_t* __restrict__ scales,
+template <int S0, int SN, class Keys>
+__device__ __forceinline__ void direct_item(const Keys& keys, int64_t b, int64_t nu, int u, int c, int64_t nb_cap,
+                                            uint64_t* __restrict__ planes, uint16_t* __restrict__ scales,
                                             uint32_t& flags) {
   const int g = (threadIdx.x & 63) >> 4;
   const int64_t tok0 = b * kBlockTokens;
@@ -338,8 +381,8 @@ __device__ __forceinline__ void direct_item(const KT* Ku, int64_t ld_tok, int64_
   uint16_t a16[SN] = {};
   if (tok0 < nu) {
     uint4 r[kRows];
-    load_item<KT>(Ku, ld_tok, tok0, nu, c, r);
-    quantise_item<KT, S0, SN>(r, valid_mask(nu - tok0), w, a16, flags);
+    load_item(keys, u, tok0, nu, c, r, flags);
+    quantise_item<typename Keys::Key, S0, SN>(r, valid_mask(nu - tok0), w, a16, flags);
   }
 #pragma unroll
   for (int s = 0; s < SN; ++s) {
@@ -352,10 +395,12 @@ __device__ __forceinline__ void direct_item(const KT* Ku, int64_t ld_tok, int64_
 
 // Tokens of a unit and the blocks [bs, be) that an append re-packs, from the first
 // block holding a new token; false leaves the unit as it was.
-__device__ __forceinline__ bool append_range(const int64_t* n, const int64_t* n_old, int u, int64_t max_blocks,
-                                             int64_t nb_cap, uint32_t* st, int64_t* nu, int64_t* bs, int64_t* be) {
-  const int64_t no = n_old[u];
-  *nu = unit_tokens(n, u, nb_cap * kBlockTokens, st);
+template <class Keys>
+__device__ __forceinline__ bool append_range(const Keys& keys, const int64_t* n, const int64_t* n_old, int u,
+                                             int64_t max_blocks, int64_t nb_cap, uint32_t* st, int64_t* nu, int64_t* bs,
+                                             int64_t* be) {
+  const int64_t no = n_old[keys.len_index(u)];
+  *nu = unit_tokens(n, keys.len_index(u), keys.limit(nb_cap * kBlockTokens), st);
   *bs = no / kBlockTokens;
   *be = (*nu + kBlockTokens - 1) / kBlockTokens;
   if (no >= 0 && no <= *nu && *be - *bs <= max_blocks) return true;
@@ -368,26 +413,30 @@ __device__ __forceinline__ bool append_range(const int64_t* n, const int64_t* n_
 // the loads to the stores is short: it is one wave's latency.  8 units' one token:
 // fp32 2.7 us, fp16 3.4 (16 tokens a lane, in one or two waves an item: 4.3 and 4.5;
 // a tile in LDS with wave-wide shuffles: 4.3 and 4.3).
-template <typename KT>
-__global__ __launch_bounds__(kWave) void pack_append_kernel(const KT* __restrict__ K, int64_t ld_tok, int64_t ld_unit,
-                                                           const int64_t* __restrict__ n,
+template <class Keys>
+__global__ __launch_bounds__(kWave) void pack_append_kernel(Keys keys, const int64_t* __restrict__ n,
                                                            const int64_t* __restrict__ n_old, int64_t max_blocks,
                                                            int64_t nb_cap, uint64_t* __restrict__ planes,
                                                            uint16_t* __restrict__ scales, uint32_t* __restrict__ st) {
+  using KT = typename Keys::Key;
   constexpr int kCh = PackItem<KT>::kCh, kItems = kD / kCh;
   const int u = blockIdx.y, lane = threadIdx.x;
   int64_t nu, bs, be;
-  if (!append_range(n, n_old, u, max_blocks, nb_cap, lane == 0 ? st : nullptr, &nu, &bs, &be)) return;
+  if (!append_range(keys, n, n_old, u, max_blocks, nb_cap, lane == 0 ? st : nullptr, &nu, &bs, &be)) return;
   const int64_t b = bs + blockIdx.x / kItems;
   if (b >= be) return;
   const int c = (int)(blockIdx.x % kItems) * kCh;
   const int64_t tok = b * kBlockTokens + lane;
   const bool valid = tok < nu;
   uint4 r = make_uint4(0u, 0u, 0u, 0u);
-  if (valid) r = *reinterpret_cast<const uint4*>(K + (int64_t)u * ld_unit + tok * ld_tok + c);
+  uint32_t flags = 0;
+  if (valid) {
+    const KT* p = keys.rows(u, tok, flags);
+    if (p) r = *reinterpret_cast<const uint4*>(p + c);
+  }
   add_zero<KT>(r);  // -0 counts as +0
   const uint64_t vm = __ballot(valid);
-  uint32_t mx[kCh / 4][4], flags = 0;
+  uint32_t mx[kCh / 4][4];
 #pragma unroll
   for (int e = 0; e < kCh; ++e) {  // NaN keys leave the maximum (and take code 8 below)
     const float a = fabsf(item_value<KT>(r, e));
@@ -428,37 +477,36 @@ __global__ __launch_bounds__(kWave) void pack_append_kernel(const KT* __restrict
 
 // SPLIT: an item's sets of 4 channels a lane go to waves of their own.  An append
 // is one wave's latency: one unit's fp16 block takes 4.1 us, 5.7 in one wave.
-template <typename KT, bool SPLIT>
-__global__ __launch_bounds__(kWave) void pack_direct_kernel(const KT* __restrict__ K, int64_t ld_tok, int64_t ld_unit,
-                                                           const int64_t* __restrict__ n,
+template <class Keys, bool SPLIT>
+__global__ __launch_bounds__(kWave) void pack_direct_kernel(Keys keys, const int64_t* __restrict__ n,
                                                            const int64_t* __restrict__ n_old, int64_t max_blocks,
                                                            int64_t nb_cap, uint64_t* __restrict__ planes,
                                                            uint16_t* __restrict__ scales, uint32_t* __restrict__ st) {
-  using P = PackItem<KT>;
+  using P = PackItem<typename Keys::Key>;
   constexpr int kParts = SPLIT ? P::kSets : 1;  // waves per item
   const int u = blockIdx.y, lane = threadIdx.x, x = lane & 15;
   int64_t nu, bs = 0, be = nb_cap;
-  if (!n_old) nu = unit_tokens(n, u, nb_cap * kBlockTokens, lane == 0 ? st : nullptr);
-  else if (!append_range(n, n_old, u, max_blocks, nb_cap, lane == 0 ? st : nullptr, &nu, &bs, &be)) return;
+  if (!n_old)
+    nu = unit_tokens(n, keys.len_index(u), keys.limit(nb_cap * kBlockTokens), lane == 0 ? st : nullptr);
+  else if (!append_range(keys, n, n_old, u, max_blocks, nb_cap, lane == 0 ? st : nullptr, &nu, &bs, &be)) return;
   const int it = (int)(blockIdx.x / kParts), part = (int)(blockIdx.x % kParts);
   const int64_t b = bs + it / P::kPerBlock;
   if (b >= be) return;
   const int c = (it % P::kPerBlock) * 16 * P::kCh + x * P::kCh;
-  const KT* Ku = K + (int64_t)u * ld_unit;
   uint32_t flags = 0;
   if constexpr (kParts == 1)
-    direct_item<KT, 0, P::kSets>(Ku, ld_tok, b, nu, u, c, nb_cap, planes, scales, flags);
+    direct_item<0, P::kSets>(keys, b, nu, u, c, nb_cap, planes, scales, flags);
   else if (part == 0)
-    direct_item<KT, 0, 1>(Ku, ld_tok, b, nu, u, c, nb_cap, planes, scales, flags);
+    direct_item<0, 1>(keys, b, nu, u, c, nb_cap, planes, scales, flags);
   else
-    direct_item<KT, 1, 1>(Ku, ld_tok, b, nu, u, c, nb_cap, planes, scales, flags);
+    direct_item<1, 1>(keys, b, nu, u, c, nb_cap, planes, scales, flags);
   wave_status(st, flags);
 }
 
-template <typename KT>
-static void launch_pack_t(const KT* K, int64_t ld_tok, int64_t ld_unit, const int64_t* n, const int64_t* n_old,
-                          int64_t max_new, int U, int64_t nb_cap, uint64_t* planes, uint16_t* scales, uint32_t* st,
-                          hipStream_t s) {
+template <class Keys>
+static void launch_pack_t(const Keys& keys, const int64_t* n, const int64_t* n_old, int64_t max_new, int U,
+                          int64_t nb_cap, uint64_t* planes, uint16_t* scales, uint32_t* st, hipStream_t s) {
+  using P = PackItem<typename Keys::Key>;
   // append: new tokens span at most ceil(max_new / 64) + 1 blocks per unit
   int64_t mb = nb_cap;
   if (n_old) {
@@ -466,34 +514,44 @@ static void launch_pack_t(const KT* K, int64_t ld_tok, int64_t ld_unit, const in
     if (mb > nb_cap) mb = nb_cap;
   }
   const int64_t tiles = (nb_cap + kTileBlocks - 1) / kTileBlocks;
-  const unsigned items = (unsigned)(mb * PackItem<KT>::kPerBlock);
+  const unsigned items = (unsigned)(mb * P::kPerBlock);
   // An append's rows are read 16 bytes at a time by 16 (fp32: 32) waves a token each
   // lane, which up to about 100 blocks is the faster (32 units' 128 tokens, 96 blocks: fp32
   // 3.8 us against 4.9, fp16 4.8 and 5.1; 256 tokens, 160 blocks: 6.5 and 5.5, 6.1 and 5.6).
   if (n_old && mb * U <= 96)
-    hipLaunchKernelGGL(pack_append_kernel<KT>, dim3((unsigned)(mb * (kD / PackItem<KT>::kCh)), (unsigned)U), dim3(kWave), 0,
-                       s, K, ld_tok, ld_unit, n, n_old, mb, nb_cap, planes, scales, st);
+    hipLaunchKernelGGL(pack_append_kernel<Keys>, dim3((unsigned)(mb * (kD / P::kCh)), (unsigned)U), dim3(kWave), 0, s,
+                       keys, n, n_old, mb, nb_cap, planes, scales, st);
   else if (n_old)
-    hipLaunchKernelGGL((pack_direct_kernel<KT, true>), dim3(items * PackItem<KT>::kSets, (unsigned)U), dim3(kWave), 0, s,
-                       K, ld_tok, ld_unit, n, n_old, mb, nb_cap, planes, scales, st);
-  else if (tiles * U < kDirectTiles)
-    hipLaunchKernelGGL((pack_direct_kernel<KT, false>), dim3(items, (unsigned)U), dim3(kWave), 0, s, K, ld_tok, ld_unit,
+    hipLaunchKernelGGL((pack_direct_kernel<Keys, true>), dim3(items * P::kSets, (unsigned)U), dim3(kWave), 0, s, keys,
                        n, n_old, mb, nb_cap, planes, scales, st);
+  else if (tiles * U < kDirectTiles)
+    hipLaunchKernelGGL((pack_direct_kernel<Keys, false>), dim3(items, (unsigned)U), dim3(kWave), 0, s, keys, n, n_old,
+                       mb, nb_cap, planes, scales, st);
   else
-    hipLaunchKernelGGL(pack_tile_kernel<KT>, dim3((unsigned)tiles, (unsigned)U), dim3(kPackThreads), 0, s, K, ld_tok,
-                       ld_unit, n, nb_cap, planes, scales, st);
+    hipLaunchKernelGGL(pack_tile_kernel<Keys>, dim3((unsigned)tiles, (unsigned)U), dim3(kPackThreads), 0, s, keys, n,
+                       nb_cap, planes, scales, st);
 }
 
 fathom_status launch_pack(const void* K, fathom_dtype kdt, int64_t ld_tok, int64_t ld_unit,
                           const int64_t* n, const int64_t* n_old, int64_t max_new, int U, int64_t nb_cap,
                           uint64_t* planes, uint16_t* scales, uint32_t* st, hipStream_t s) {
   if (U == 0 || nb_cap == 0) return FATHOM_OK;
-  if (kdt == FATHOM_F32)
-    launch_pack_t(reinterpret_cast<const float*>(K), ld_tok, ld_unit, n, n_old, max_new, U, nb_cap, planes, scales,
-                  st, s);
-  else
-    launch_pack_t(reinterpret_cast<const __half*>(K), ld_tok, ld_unit, n, n_old, max_new, U, nb_cap, planes, scales,
-                  st, s);
+  if (kdt == FATHOM_F32) {
+    const FlatKeys<float> k = {reinterpret_cast<const float*>(K), ld_tok, ld_unit};
+    launch_pack_t(k, n, n_old, max_new, U, nb_cap, planes, scales, st, s);
+  } else {
+    const FlatKeys<__half> k = {reinterpret_cast<const __half*>(K), ld_tok, ld_unit};
+    launch_pack_t(k, n, n_old, max_new, U, nb_cap, planes, scales, st, s);
+  }
+  FATHOM_LAUNCH_CHECK();
+  return FATHOM_OK;
+}
+
+fathom_status launch_paged_pack(const Paged& c, bool bf16, const int64_t* n, const int64_t* n_old, int64_t max_new,
+                                int U, int64_t nb_cap, uint64_t* planes, uint16_t* scales, uint32_t* st,
+                                hipStream_t s) {
+  if (bf16) launch_pack_t(PagedKeys<bf16_t>{c, c.ld_tok}, n, n_old, max_new, U, nb_cap, planes, scales, st, s);
+  else launch_pack_t(PagedKeys<__half>{c, c.ld_tok}, n, n_old, max_new, U, nb_cap, planes, scales, st, s);
   FATHOM_LAUNCH_CHECK();
   return FATHOM_OK;
 }

@@ -1,0 +1,346 @@
+// fathom_paged_map and fathom_paged_write: block tables, slot maps and the new
+// rows of a paged cache.
+//
+// Map.  All that a request needs of the others are three prefix sums over the
+// requests: of its new rows, of the pages it takes and of those it returns.  A
+// workgroup computes them in registers (up to 4 requests a thread, wave scans
+// joined through LDS) and keeps them in LDS, where every slot and every moved
+// page finds its request by binary search; so slots and pages are spread over
+// threads evenly however uneven the requests are.  The ring is read at its front
+// and written behind its end, the table's read and written entries are disjoint,
+// so nothing waits for anything.  A small call is one workgroup and one launch;
+// a large one spreads slots and pages over workgroups that each recompute the
+// sums (16 bytes a request from L2), and a second launch of one workgroup writes
+// what the first one still reads (state, lengths: the caller's may be in place).
+//
+// Write.  A copy of rows: 16 lanes take a row's 256 bytes of output, the row's
+// slot gives the page.  Bound by bytes where they are many and by one trip to
+// memory after another (slot, row, store) where they are few.
+#include "paged.hpp"
+
+namespace fathom {
+
+constexpr int kMapThreads = 1024;
+constexpr int kMapPer = kMaxSeqs / kMapThreads;  // requests per thread
+static_assert(kMapPer * kMapThreads == kMaxSeqs, "requests divide over the threads");
+
+struct MapArgs {
+  const int64_t *n_old, *n;
+  int S, H, shift;
+  int32_t* table;
+  int64_t ld_table;
+  int32_t* ring;
+  int64_t P;
+  const int64_t* state;
+  int64_t* slots;
+  int64_t T;
+  int64_t *start, *n_now, *n_unit, *state_out;
+  uint32_t* st;
+};
+
+// Inclusive sums of three values over the workgroup (each thread's own sum given).
+__device__ __forceinline__ void block_scan3(int64_t (&v)[3], int64_t (&part)[3][kMapThreads / kWave]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up(v[i], o, kWave);
+      if (lane >= o) v[i] += x;
+    }
+    if (lane == 63) part[i][wave] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    int64_t before = 0;
+    for (int w = 0; w < wave; ++w) before += part[i][w];
+    v[i] += before;
+  }
+}
+
+// The last of `count` non-decreasing entries that is at most x (the first is).
+__device__ __forceinline__ int last_at_most(const int32_t* a, int count, int32_t x) {
+  int lo = 0, len = count;
+  while (len > 1) {
+    const int half = len >> 1;
+    if (a[lo + half] <= x) {
+      lo += half;
+      len -= half;
+    } else {
+      len = half;
+    }
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int32_t clip31(int64_t x) { return (int32_t)(x < 0x7fffffff ? x : 0x7fffffff); }
+
+// FILL: slots, table and ring.  FINISH: start, lengths and state, after every read.
+template <bool FILL, bool FINISH>
+__global__ __launch_bounds__(kMapThreads) void paged_map_kernel(MapArgs a) {
+  extern __shared__ int32_t sm[];
+  __shared__ int64_t part[3][kMapThreads / kWave];
+  __shared__ int64_t tot[4];  // rows, pages returned; pages taken by those served
+  const int S = a.S, tid = threadIdx.x;
+  int32_t* s_start = sm;        // [S] first new row
+  int32_t* s_taken = sm + S;    // [S] pages taken before
+  int32_t* s_back = sm + 2 * S; // [S] pages returned before
+  int32_t* s_old = sm + 3 * S;  // [S] old length; ~old where the request is not served
+  int32_t* s_after = sm + 4 * S;  // [S] pages after
+  const int64_t cap = a.ld_table << a.shift, rnd = (1 << a.shift) - 1;
+  int64_t head = a.state[0], count = a.state[1];
+  uint32_t flags = 0;
+  const bool bad_state = head < 0 || head >= a.P || count < 0 || count > a.P;
+  if (bad_state) {
+    flags |= FATHOM_DEV_BAD_PAGE;
+    count = 0;
+  }
+  if (tid == 0) tot[2] = 0;
+  int64_t no[kMapPer], nn[kMapPer], sum[3] = {0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kMapPer; ++i) {
+    const int s = tid * kMapPer + i;
+    no[i] = s < S ? a.n_old[s] : 0;
+    nn[i] = s < S ? a.n[s] : 0;
+  }
+  int64_t add[kMapPer][3];
+#pragma unroll
+  for (int i = 0; i < kMapPer; ++i) {
+    const bool ok = no[i] >= 0 && no[i] <= cap && nn[i] >= 0 && nn[i] <= cap;
+    const int64_t before = (no[i] + rnd) >> a.shift, after = (nn[i] + rnd) >> a.shift;
+    add[i][0] = ok && nn[i] > no[i] ? nn[i] - no[i] : 0;
+    add[i][1] = ok && after > before ? after - before : 0;
+    add[i][2] = ok && before > after ? before - after : 0;
+#pragma unroll
+    for (int x = 0; x < 3; ++x) sum[x] += add[i][x];
+  }
+  int64_t inc[3] = {sum[0], sum[1], sum[2]};
+  block_scan3(inc, part);
+  if (tid == kMapThreads - 1) {
+    tot[0] = inc[0];
+    tot[1] = inc[2];
+  }
+  int64_t at[3] = {inc[0] - sum[0], inc[1] - sum[1], inc[2] - sum[2]}, mine = 0;
+  int64_t first[kMapPer];
+  bool served[kMapPer];
+#pragma unroll
+  for (int i = 0; i < kMapPer; ++i) {
+    const int s = tid * kMapPer + i;
+    const bool ok_old = no[i] >= 0 && no[i] <= cap, ok = ok_old && nn[i] >= 0 && nn[i] <= cap;
+    first[i] = at[0];
+    const bool fits = at[0] + add[i][0] <= a.T, pages = add[i][1] == 0 || at[1] + add[i][1] <= count;
+    served[i] = ok && fits && pages;
+    if (s < S) {
+      if (!ok || !fits) flags |= FATHOM_DEV_BAD_N;
+      else if (!pages) flags |= FATHOM_DEV_PAGES_SHORT;
+      s_start[s] = clip31(at[0]);
+      s_taken[s] = clip31(at[1]);
+      s_back[s] = clip31(at[2]);
+      s_old[s] = served[i] ? (int32_t)no[i] : -1;
+      s_after[s] = ok ? (int32_t)((nn[i] + rnd) >> a.shift) : 0;
+      if (served[i]) mine += add[i][1];
+    }
+    if (!ok_old) no[i] = 0;
+#pragma unroll
+    for (int x = 0; x < 3; ++x) at[x] += add[i][x];
+  }
+  __syncthreads();
+  if (mine) atomicAdd((unsigned long long*)&tot[2], (unsigned long long)mine);  // whole numbers: any order
+  __syncthreads();
+  const int64_t taken = tot[2], rows = tot[0];
+  int64_t back = tot[1];
+  if (bad_state) back = 0;
+  if (count + back > a.P) {
+    flags |= FATHOM_DEV_BAD_PAGE;
+    back = 0;
+  }
+  if constexpr (FILL) {
+    const int64_t gt = (int64_t)blockIdx.x * kMapThreads + tid, step = (int64_t)gridDim.x * kMapThreads;
+    for (int64_t t = gt; t < a.T; t += step) {
+      int64_t slot = -1;
+      if (t < rows) {
+        const int s = last_at_most(s_start, S, (int32_t)t);
+        const int32_t old = s_old[s];
+        if (old >= 0) {
+          const int32_t p = old + (int32_t)(t - s_start[s]), before = (int32_t)(((int64_t)old + rnd) >> a.shift);
+          const int32_t e = p >> a.shift;
+          int32_t id;
+          if (e >= before) {
+            int64_t r = head + s_taken[s] + (e - before);
+            if (r >= a.P) r -= a.P;
+            id = a.ring[r];
+          } else {
+            id = a.table[(int64_t)s * a.ld_table + e];
+          }
+          if (id >= 0 && id < a.P) slot = ((int64_t)id << a.shift) + (p & rnd);
+          else flags |= FATHOM_DEV_BAD_PAGE;
+        }
+      }
+      a.slots[t] = slot;
+    }
+    for (int64_t j = gt; j < taken; j += step) {
+      const int s = last_at_most(s_taken, S, (int32_t)j);
+      int64_t r = head + j;
+      if (r >= a.P) r -= a.P;
+      const int32_t id = a.ring[r];
+      if (id < 0 || id >= a.P) flags |= FATHOM_DEV_BAD_PAGE;
+      const int64_t before = ((int64_t)s_old[s] + rnd) >> a.shift;
+      a.table[(int64_t)s * a.ld_table + before + (j - s_taken[s])] = id;
+    }
+    for (int64_t j = gt; j < back; j += step) {
+      const int s = last_at_most(s_back, S, (int32_t)j);
+      int64_t r = head + count + j;
+      while (r >= a.P) r -= a.P;
+      const int32_t id = a.table[(int64_t)s * a.ld_table + s_after[s] + (j - s_back[s])];
+      if (id < 0 || id >= a.P) flags |= FATHOM_DEV_BAD_PAGE;
+      a.ring[r] = id;
+    }
+  }
+  if constexpr (FINISH) {
+#pragma unroll
+    for (int i = 0; i < kMapPer; ++i) {
+      const int s = tid * kMapPer + i;
+      if (s >= S) break;
+      const int64_t now = served[i] ? nn[i] : no[i];
+      a.start[s] = first[i];
+      a.n_now[s] = now;
+      if (a.n_unit)
+        for (int h = 0; h < a.H; ++h) a.n_unit[(int64_t)s * a.H + h] = now;
+    }
+    if (tid == 0) {
+      a.start[S] = rows;
+      const int64_t h1 = head + taken;
+      a.state_out[0] = bad_state ? head : h1 >= a.P ? h1 - a.P : h1;
+      a.state_out[1] = bad_state ? a.state[1] : count - taken + back;
+    }
+  }
+  if (flags) set_status(a.st, flags);
+}
+
+fathom_status launch_paged_map(const int64_t* n_old, const int64_t* n, int S, int H, int shift, int32_t* table,
+                               int64_t ld_table, int32_t* ring, int64_t P, const int64_t* state, int64_t* slots,
+                               int64_t T, int64_t* start, int64_t* n_now, int64_t* n_unit, int64_t* state_out,
+                               uint32_t* st, hipStream_t s) {
+  const MapArgs a = {n_old, n,     S, H,     shift, table, ld_table, ring, P,
+                     state, slots, T, start, n_now, n_unit, state_out, st};
+  const size_t lds = (size_t)5 * S * sizeof(int32_t);
+  const int64_t items = T + (int64_t)S * ld_table;  // an upper bound on slots and moved pages
+  if (items <= 32 * kMapThreads) {
+    hipLaunchKernelGGL((paged_map_kernel<true, true>), dim3(1), dim3(kMapThreads), lds, s, a);
+  } else {
+    const int64_t wgs = items / (8 * kMapThreads) + 1;
+    hipLaunchKernelGGL((paged_map_kernel<true, false>), dim3((unsigned)(wgs < 256 ? wgs : 256)), dim3(kMapThreads), lds,
+                       s, a);
+    hipLaunchKernelGGL((paged_map_kernel<false, true>), dim3(1), dim3(kMapThreads), lds, s, a);
+  }
+  FATHOM_LAUNCH_CHECK();
+  return FATHOM_OK;
+}
+
+// ---------------------------------------------------------------- write
+constexpr int kWriteThreads = 256;
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+struct WriteArgs {
+  const void *K, *V;
+  int64_t ldk_tok, ldk_head, ldv_tok, ldv_head;
+  const int64_t* slots;
+  uint32_t rows;  // T*H
+  uint16_t *Kp, *Vp;
+  int H, shift;
+  int64_t cap;  // slots of the pool
+  int64_t ld_page, ld_head, ld_tok;
+  uint32_t* st;
+};
+
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, bool bf) {
+  if (bf) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    const b2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, v);
+  }
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  const h2 v = {(_Float16)a, (_Float16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// F32: fp32 rows, rounded; otherwise a copy.  ROWS rows (of 16 lanes) per lane group.
+template <bool F32, bool BF, int ROWS>
+__global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(WriteArgs a) {
+  const int x = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const bool v_side = blockIdx.y != 0;
+  const void* src = v_side ? a.V : a.K;
+  uint16_t* dst = v_side ? a.Vp : a.Kp;
+  const int64_t ls_tok = v_side ? a.ldv_tok : a.ldk_tok, ls_head = v_side ? a.ldv_head : a.ldk_head;
+  constexpr int kGroups = kWriteThreads / 16;
+  int64_t slot[ROWS];
+  uint32_t head[ROWS];
+  u32x4 w[ROWS], w2[ROWS];
+  const uint32_t r0 = blockIdx.x * (uint32_t)(kGroups * ROWS) + g;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const uint32_t r = r0 + i * kGroups;
+    slot[i] = -1;
+    head[i] = 0;
+    if (r < a.rows) {
+      const uint32_t t = r / (uint32_t)a.H, h = r - t * (uint32_t)a.H;
+      slot[i] = a.slots[t];
+      head[i] = h;
+      const int64_t o = (int64_t)t * ls_tok + (int64_t)h * ls_head + 8 * x;
+      if constexpr (F32) {
+        const u32x4* p = reinterpret_cast<const u32x4*>(reinterpret_cast<const float*>(src) + o);
+        w[i] = p[0];
+        w2[i] = p[1];
+      } else {
+        w[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(src) + o);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    if (slot[i] < 0) continue;
+    if (slot[i] >= a.cap) {
+      if (x == 0) set_status(a.st, FATHOM_DEV_BAD_PAGE);
+      continue;
+    }
+    u32x4 v = w[i];
+    if constexpr (F32) {
+      const u32x4 lo = w[i], hi = w2[i];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        v[e] = pack_pair(__uint_as_float(lo[2 * e]), __uint_as_float(lo[2 * e + 1]), BF);
+        v[2 + e] = pack_pair(__uint_as_float(hi[2 * e]), __uint_as_float(hi[2 * e + 1]), BF);
+      }
+    }
+    const int64_t o = (slot[i] >> a.shift) * a.ld_page + (int64_t)head[i] * a.ld_head +
+                      (slot[i] & ((1 << a.shift) - 1)) * a.ld_tok + 8 * x;
+    *reinterpret_cast<u32x4*>(dst + o) = v;
+  }
+}
+
+template <int ROWS>
+static void launch_write(const WriteArgs& a, bool f32, bool bf, hipStream_t s) {
+  constexpr uint32_t per = kWriteThreads / 16 * ROWS;
+  const dim3 grid((a.rows + per - 1) / per, 2);
+  if (!f32) hipLaunchKernelGGL((paged_write_kernel<false, false, ROWS>), grid, dim3(kWriteThreads), 0, s, a);
+  else if (bf) hipLaunchKernelGGL((paged_write_kernel<true, true, ROWS>), grid, dim3(kWriteThreads), 0, s, a);
+  else hipLaunchKernelGGL((paged_write_kernel<true, false, ROWS>), grid, dim3(kWriteThreads), 0, s, a);
+}
+
+fathom_status launch_paged_write(const void* K, const void* V, fathom_dtype sdt, int64_t ldk_tok, int64_t ldk_head,
+                                 int64_t ldv_tok, int64_t ldv_head, const int64_t* slots, int64_t T,
+                                 const fathom_pages& p, uint32_t* st, hipStream_t s) {
+  const int shift = __builtin_ctz((unsigned)p.page);
+  const WriteArgs a = {K, V, ldk_tok, ldk_head, ldv_tok, ldv_head, slots, (uint32_t)(T * p.H),
+                       reinterpret_cast<uint16_t*>(p.K), reinterpret_cast<uint16_t*>(p.V), p.H, shift, p.P << shift,
+                       p.ld_page, p.ld_head, p.ld_tok, st};
+  // few rows: one a lane group, so that they reach more CUs; many: four in flight
+  if (a.rows <= 16384) launch_write<1>(a, sdt == FATHOM_F32, p.dt == FATHOM_BF16, s);
+  else launch_write<4>(a, sdt == FATHOM_F32, p.dt == FATHOM_BF16, s);
+  FATHOM_LAUNCH_CHECK();
+  return FATHOM_OK;
+}
+
+}  // namespace fathom

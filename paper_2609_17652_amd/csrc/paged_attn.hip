@@ -1,0 +1,1163 @@
+// fathom_paged_attn: dense attention of new tokens over a paged cache.
+//
+// The query rows of a (request, KV head) are its new tokens' G heads, row r =
+// token*G + g, so the G heads share every K and V row that is loaded.  Scores are
+// computed transposed, S^T = K Q^T: an accumulator lane then holds scores of ONE
+// query row, so the softmax of a row needs one exchange between lane groups, and
+// the lane's probabilities are already the B operand of O^T = V^T P^T, with the
+// keys of a 16-key step in the order that the accumulator holds them; V^T is
+// read from row-major LDS rows by transposing loads in the same key order.  The
+// running maximum and sum and both products are fp32.
+//
+// K and V rows go from the pages to LDS without registers, 1 KB (4 rows) an
+// instruction; 16 rows from a multiple of 16 lie in one page, so a page number is
+// uniform and comes over the scalar path.  LDS rows are 256 bytes (every bank
+// once); 16-byte chunks are permuted by the row so that the 16 rows of a K
+// fragment (chunk ^ row) and the 4 rows of a V read (chunk ^ 4 row) spread over
+// the banks.
+//
+// Two kernels.  attn_few_kernel takes requests of at most 32 query rows (decode,
+// drafted tokens): bound by reading the cache, so the 32-key blocks of all
+// requests and heads are cut into equal shares, one per wave, whatever the
+// lengths are; each wave runs its share through two private LDS stages without
+// meeting the others, and pieces of a request join in attn_join_kernel.
+// attn_many_kernel takes the others, 256 query rows a workgroup, bound by the
+// matrix cores; keys are split over workgroups where the tiles are few.
+//
+// Rows that a query must not see get a probability of 0, but 0 * Inf is not 0:
+// V rows behind the end are cleared in LDS, and in steps with masked places
+// the non-finite values of V are taken out of the product and added for the rows
+// that see them.
+#include "paged.hpp"
+
+namespace fathom {
+
+#define LDS_PTR(T) __attribute__((address_space(3))) T*
+// 32-bit LDS offsets as pointers
+#define LDS_AT(T, at) ((LDS_PTR(T))(uintptr_t)(at))
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kRowBytes = 2 * kD;
+constexpr int kFewRows = 32;      // query rows of a request and head that attn_few_kernel takes
+constexpr int kFewKeys = 32;      // keys a step of a wave
+constexpr int kFewWaves = 4;
+constexpr int kFewWorkers = 1024; // waves: one workgroup of 128 KB of LDS on each of 256 CUs
+constexpr int kFewStage = 2 * kFewKeys * kRowBytes;
+constexpr int kManyRows = 256;    // query rows of a workgroup, 64 a wave
+constexpr int kManyKeys = 64;
+constexpr int kManyStage = 2 * kManyKeys * kRowBytes;
+constexpr int kManyStages = 4;
+constexpr int kNone = -(1 << 30);
+
+struct PagedAttnArgs {
+  const uint16_t* q;
+  int64_t ldq_tok, ldq_head;
+  Paged c;
+  const int64_t *start, *n;
+  int S, G, few;        // few: query rows up to which a request goes to attn_few_kernel
+  int64_t T, max_new;
+  float sm_scale, softcap;
+  const float* slopes;
+  const int64_t *prefix, *first;
+  uint16_t* out;
+  float *part_o, *part_ml;  // partial results: rows of kD sums, and (maximum, sum) of each
+  int tiles, nsplit;        // attn_many_kernel: row tiles launched, parts of their keys
+  uint32_t* st;
+};
+
+// What no kernel of a call writes, over the scalar path where the index is uniform (a
+// vector load in the loop would wait for every load in flight).
+template <typename T>
+__device__ __forceinline__ T fixed(const T* p, int64_t i) {
+  return ((const __attribute__((address_space(4))) T*)p)[i];
+}
+__device__ __forceinline__ int page_uniform(const Paged& c, int s, int e) {
+  return fixed(c.table + (int64_t)s * c.ld_table, e);
+}
+
+// New tokens of request s, their first row in *a and its tokens in *n; 0 (with
+// BAD_N) where the lengths do not fit together.
+__device__ __forceinline__ int request_rows(const PagedAttnArgs& p, int s, int64_t* a, int64_t* n, uint32_t& flags) {
+  const int64_t b = fixed(p.start, s), e = fixed(p.start, s + 1), m = fixed(p.n, s);
+  *a = b;
+  *n = m;
+  const bool ok = b >= 0 && e >= b && e <= p.T && m >= 0 && m <= (p.c.ld_table << p.c.shift) && e - b <= m &&
+                  e - b <= p.max_new;
+  if (!ok) {
+    flags |= FATHOM_DEV_BAD_N;
+    return 0;
+  }
+  return (int)(e - b);
+}
+
+// What a query token sees: [lo, hi).
+__device__ __forceinline__ void token_range(const PagedAttnArgs& p, int s, int64_t row, int pos, int n, int* lo,
+                                            int* hi) {
+  *lo = 0;
+  *hi = pos + 1;
+  if (p.prefix) {
+    const int64_t v = fixed(p.prefix, s), x = v < n ? v : n;
+    if (x > *hi) *hi = (int)x;
+  }
+  if (p.first) {
+    const int64_t x = p.first[row];
+    *lo = x < 0 ? 0 : x > n ? n : (int)x;
+  }
+}
+
+// ---------------------------------------------------------------- tools
+// 64 lanes x 16 bytes: from base + voff (a lane's) to LDS at `lds` + 16 lane.  The
+// wait is the caller's (vmcnt); no register is written.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base) : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// 16-byte chunk of an LDS row of K or V where the row's chunk `c` is kept.
+__device__ __forceinline__ int k_chunk(int row, int c) { return c ^ (row & 15); }
+__device__ __forceinline__ int v_chunk(int row, int c) { return c ^ ((row & 3) << 2); }
+
+template <bool BF>
+struct Mx;
+template <>
+struct Mx<false> {
+  typedef f16x8 v8;
+  typedef _Float16 t;
+  static constexpr uint16_t kInf = 0x7C00, kOne = 0x3C00;
+  static constexpr float kShift = 14.0f;  // probabilities are kept times 2^14: no subnormals down to 2^-28
+  static __device__ __forceinline__ f32x4 mfma16(v8 a, v8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16 mfma32(v8 a, v8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mx<true> {
+  typedef bf16x8 v8;
+  typedef __bf16 t;
+  static constexpr uint16_t kInf = 0x7F80, kOne = 0x3F80;
+  static constexpr float kShift = 0.0f;
+  static __device__ __forceinline__ f32x4 mfma16(v8 a, v8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x16 mfma32(v8 a, v8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+
+template <class V8>
+__device__ __forceinline__ V8 lds_v8(uint32_t at) {
+  return *LDS_AT(const V8, at);
+}
+// Four rows' values of a lane's channel: rows and channels as the callers' lanes give them.
+__device__ __forceinline__ s16x4 lds_tr(uint32_t at) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_AT(s16x4, at));
+}
+template <class V8>
+__device__ __forceinline__ V8 join4(s16x4 a, s16x4 b) {
+  return __builtin_bit_cast(V8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Whether BYTES (a multiple of 1024) of V at `at` hold a value that is not finite; uniform.
+template <bool BF, int BYTES>
+__device__ __forceinline__ bool any_nonfinite(uint32_t at) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 top = {0, 0};
+  const uint32_t mine = at + 16 * (threadIdx.x & 63);
+#pragma unroll
+  for (int i = 0; i < BYTES; i += 1024) {
+    const u32x4 w = *LDS_AT(const u32x4, mine + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[e] & 0x7FFF7FFFu));
+  }
+  return __ballot(top[0] >= Mx<BF>::kInf || top[1] >= Mx<BF>::kInf) != 0;
+}
+
+// Such values leave the product, and are added (as they are: Inf and NaN do what the sum
+// would) to the four sums of a lane's channels where its query sees their key.
+template <bool BF>
+__device__ __forceinline__ bool nonfinite_bits(short x) {
+  return ((uint16_t)x & Mx<BF>::kInf) == Mx<BF>::kInf;
+}
+template <bool BF>
+__device__ __forceinline__ s16x8 finite_part(s16x8 v) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (nonfinite_bits<BF>(v[e])) v[e] = 0;
+  return v;
+}
+template <bool BF>
+__device__ __forceinline__ float nonfinite_part(short x) {
+  return nonfinite_bits<BF>(x) ? (float)__builtin_bit_cast(typename Mx<BF>::t, x) : 0.0f;
+}
+
+// z in units of log2: the scaled score, capped, less the distance's bias.
+struct ScoreMap {
+  float c1;         // sm_scale log2e, or 2 log2e sm_scale / softcap
+  float cap;        // softcap log2e, 0: none
+  float slope;      // the row's slope times log2e
+};
+__device__ __forceinline__ float mapped(const ScoreMap& m, float s, int dist) {
+  float z = s * m.c1;
+  if (m.cap != 0.0f) {  // tanh x = 1 - 2 / (e^2x + 1)
+    const float t = __builtin_amdgcn_exp2f(z);
+    z = m.cap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(t + 1.0f));
+  }
+  return z - m.slope * (float)dist;
+}
+__device__ __forceinline__ ScoreMap score_map(const PagedAttnArgs& p, float slope) {
+  ScoreMap m;
+  m.c1 = p.softcap > 0.0f ? 2.0f * kLog2e * (p.sm_scale / p.softcap) : p.sm_scale * kLog2e;
+  m.cap = p.softcap > 0.0f ? p.softcap * kLog2e : 0.0f;
+  m.slope = slope * kLog2e;
+  return m;
+}
+
+// The first and last of the keys that any new token of a request may see, as [lo, n)
+// with lo a multiple of 32 (few tokens: attn_few_kernel).
+__device__ __forceinline__ int few_lo(const PagedAttnArgs& p, int64_t a, int rows, int64_t n) {
+  if (!p.first) return 0;
+  int64_t lo = n;
+  for (int i = 0; i < rows; ++i) {
+    const int64_t x = p.first[a + i];
+    lo = x < lo ? x : lo;
+  }
+  lo = lo < 0 ? 0 : lo;
+  return (int)(lo & ~(int64_t)(kFewKeys - 1));
+}
+
+// Blocks of 32 keys of the requests: before[s] those of the requests before s (of one
+// head), before[S] all.  Every thread of the workgroup; `part` one entry a wave.
+__device__ __forceinline__ void few_plan(const PagedAttnArgs& p, int* before, int* part, uint32_t& flags) {
+  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (p.S + nt - 1) / nt;
+  int sum = 0;
+  for (int i = 0; i < per; ++i) {
+    const int s = tid * per + i;
+    int nb = 0;
+    if (s < p.S) {
+      int64_t a, n;
+      const int rows = request_rows(p, s, &a, &n, flags);
+      if (rows > 0 && rows * p.G <= p.few)  // one block at least, for rows that see nothing
+        nb = max(((int)n - few_lo(p, a, rows, n) + kFewKeys - 1) / kFewKeys, 1);
+      before[s] = sum;
+    }
+    sum += nb;
+  }
+  int inc = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(inc, o, kWave);
+    if (lane >= o) inc += x;
+  }
+  if (lane == 63) part[wave] = inc;
+  __syncthreads();
+  int base = inc - sum;
+  for (int w = 0; w < wave; ++w) base += part[w];
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < p.S) before[tid * per + i] += base;
+  if (tid == nt - 1) before[p.S] = base + sum;
+  __syncthreads();
+}
+
+// The last s with before[s] <= x (x < before[S]): the request of block x.
+__device__ __forceinline__ int request_of(const int* before, int S, int x) {
+  int lo = 0, len = S;
+  while (len > 1) {
+    const int half = len >> 1;
+    const bool up = before[lo + half] <= x;
+    lo += up ? half : 0;
+    len = up ? len - half : half;
+  }
+  return lo;
+}
+
+// Share of worker w: blocks [share(w), share(w + 1)) of W.
+__device__ __forceinline__ int64_t share(int64_t w, int64_t W) { return w * W / kFewWorkers; }
+__device__ __forceinline__ int worker_of(int64_t g, int64_t W) { return (int)(((g + 1) * kFewWorkers - 1) / W); }
+
+// A wave's place in the blocks of all requests and heads.
+struct Place {
+  int s, h, b, nb, lo, n;  // request, head, block of nb, the request's first key and tokens
+};
+
+template <bool BF, int CT>
+__global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAttnArgs p) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  typedef typename Mx<BF>::v8 v8;
+  constexpr int R = 16 * CT;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  int* before = reinterpret_cast<int*>(smem + kFewWaves * 2 * kFewStage);
+  int* part = before + p.S + 1;
+  uint32_t flags = 0;
+  few_plan(p, before, part, flags);
+  if (flags && blockIdx.x == 0) set_status(p.st, flags);
+  flags = 0;
+  const int S = p.S, H = p.c.H, G = p.G;
+  const int64_t W = (int64_t)before[S] * H;
+  const int worker = uniform((int)blockIdx.x * kFewWaves + wave);
+  const int64_t g0 = share(worker, W), g1 = share(worker + 1, W);
+  if (g0 >= g1) return;
+  const int steps = uniform((int)(g1 - g0));
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))smem + wave * 2 * kFewStage;
+  const int quad = lane >> 4, lr = lane & 15;
+  // a lane's place in an instruction's four rows of the pages (K and V chunks permuted)
+  const uint32_t row_step = (uint32_t)p.c.ld_tok * 2;
+  uint32_t koff[4], voff[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 4 * i + quad;
+    koff[i] = row * row_step + 16 * k_chunk(row, lr);
+    voff[i] = row * row_step + 16 * v_chunk(row, lr);
+  }
+  auto lowest = [&](int s) -> int {  // few_lo of request s, by the wave
+    if (!p.first) return 0;
+    const int64_t a = fixed(p.start, s), e = fixed(p.start, s + 1), n = fixed(p.n, s);
+    int64_t lo = a + lane < e ? p.first[a + lane] : n;
+    lo = lo < 0 ? 0 : lo > n ? n : lo;
+    int x = (int)lo;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) x = min(x, __shfl_xor(x, o, kWave));
+    return uniform(x & ~(kFewKeys - 1));
+  };
+  auto place = [&](int64_t g) {
+    Place x;
+    x.s = uniform(request_of(before, S, (int)(g / H)));
+    x.nb = uniform(before[x.s + 1] - before[x.s]);
+    const int64_t rem = g - (int64_t)before[x.s] * H;
+    x.h = uniform((int)(rem / x.nb));
+    x.b = uniform((int)(rem % x.nb));
+    x.lo = lowest(x.s);
+    x.n = uniform((int)fixed(p.n, x.s));
+    return x;
+  };
+  auto next = [&](Place& x) {  // the next block; not past the last of all
+    if (++x.b < x.nb) return;
+    x.b = 0;
+    if (++x.h < H) return;
+    x.h = 0;
+    do {
+      ++x.s;
+      x.nb = x.s < S ? uniform(before[x.s + 1] - before[x.s]) : 1;
+    } while (x.nb == 0);
+    if (x.s < S) {
+      x.lo = lowest(x.s);
+      x.n = uniform((int)fixed(p.n, x.s));
+    }
+  };
+  // page numbers of the 16-key groups of a place's block (-1: behind the end or absent)
+  auto pages = [&](const Place& x, int (&id)[2]) {
+    const int key = x.lo + kFewKeys * x.b;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k = key + 16 * i;
+      id[i] = k < x.n ? page_uniform(p.c, x.s, k >> p.c.shift) : kNone;
+    }
+  };
+  auto issue = [&](const Place& x, const int (&id)[2], int stage) {
+    const uint32_t at = lds0 + stage * kFewStage;
+    const int key = x.lo + kFewKeys * x.b;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bool ok = (uint32_t)id[i] < (uint32_t)p.c.P;
+      const int64_t o = (int64_t)(ok ? id[i] : 0) * p.c.ld_page + (int64_t)x.h * p.c.ld_head +
+                        (int64_t)((key + 16 * i) & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
+      const void *kb = p.c.K + o, *vb = p.c.V + o;  // absent: rows of page 0, which no one uses
+#pragma unroll
+      for (int y = 0; y < 4; ++y) load_to_lds(at + i * 4096 + y * 1024, kb, koff[y]);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) load_to_lds(at + kFewStage / 2 + i * 4096 + y * 1024, vb, voff[y]);
+    }
+  };
+
+  Place now = place(g0), ahead = now;
+  int id[3][2];  // page numbers of this step, the next and the one after
+  pages(ahead, id[0]);
+  issue(ahead, id[0], 0);
+  if (steps > 1) {
+    next(ahead);
+    pages(ahead, id[1]);
+    issue(ahead, id[1], 1);
+  }
+  // ---- a piece of a request and head at a time ----
+  int step = 0;
+  while (step < steps) {
+    const int s = now.s, h = now.h, b_first = now.b, b_end = uniform(min(now.nb, now.b + steps - step));
+    const int64_t a = fixed(p.start, s);
+    const int n = now.n, rows = uniform((int)(fixed(p.start, s + 1) - a)) * G, lo_key = now.lo;
+    v8 qf[CT][4];
+    int pos[CT], lo[CT], hi[CT], lo_max = 0, hi_min = n;
+    ScoreMap sm[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      const int r = 16 * t + lr, tok = r / G, g = r - tok * G;
+      pos[t] = 0;
+      lo[t] = 0;
+      hi[t] = n;
+      float slope = 0.0f;
+      s16x8 z = {};
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) qf[t][kk] = __builtin_bit_cast(v8, z);
+      if (r < rows) {
+        pos[t] = n - rows / G + tok;
+        token_range(p, s, a + tok, pos[t], n, &lo[t], &hi[t]);
+        if (p.slopes) slope = p.slopes[h * G + g];
+        const uint16_t* qp = p.q + (a + tok) * p.ldq_tok + (int64_t)(h * G + g) * p.ldq_head + 8 * quad;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) qf[t][kk] = *reinterpret_cast<const v8*>(qp + 32 * kk);
+      }
+      sm[t] = score_map(p, slope);
+      lo_max = max(lo_max, lo[t]);
+      hi_min = min(hi_min, hi[t]);
+    }
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1) {
+      lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
+      hi_min = min(hi_min, __shfl_xor(hi_min, o, kWave));
+    }
+    lo_max = uniform(lo_max);
+    hi_min = uniform(hi_min);
+    f32x4 o[CT][8];
+    float m[CT], l[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      m[t] = -__builtin_huge_valf();
+      l[t] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[t][c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    for (int b = b_first; b < b_end; ++b, ++step) {
+      const int stage = step & 1;
+      const uint32_t at = lds0 + stage * kFewStage, vat = at + kFewStage / 2;
+      if (step + 2 < steps) {  // its page numbers arrive during this step
+        next(ahead);
+        pages(ahead, id[2]);
+      }
+      if (step + 1 < steps) wait_vm<16>();
+      else wait_vm<0>();
+      const int key = lo_key + kFewKeys * b;
+      const int cur0 = id[0][0], cur1 = id[0][1];
+      const bool in0 = (uint32_t)cur0 < (uint32_t)p.c.P, in1 = (uint32_t)cur1 < (uint32_t)p.c.P;
+      if ((!in0 && cur0 != kNone) || (!in1 && cur1 != kNone)) flags |= FATHOM_DEV_BAD_PAGE;
+      const bool masked = key < lo_max || key + kFewKeys > hi_min || !in0 || !in1;
+      if (masked && (key + kFewKeys > n || !in0 || !in1)) {  // rows that are not there: V is cleared
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const int row = 4 * y + quad;
+          if (key + row >= n || !(row < 16 ? in0 : in1))
+            *LDS_AT(u32x4, vat + row * kRowBytes + 16 * lr) = (u32x4){0u, 0u, 0u, 0u};
+        }
+      }
+      // ---- S^T: two groups of 16 keys ----
+      f32x4 sc[CT][2];
+#pragma unroll
+      for (int gk = 0; gk < 2; ++gk) {
+        v8 kf[4];
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          kf[kk] = lds_v8<v8>(at + (16 * gk + lr) * kRowBytes + 16 * k_chunk(lr, 4 * kk + quad));
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+          if (16 * t < rows) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) x = Mx<BF>::mfma16(kf[kk], qf[t][kk], x);
+          }
+          sc[t][gk] = x;
+        }
+      }
+      // ---- softmax, probabilities as two values of the pages' type ----
+      v8 ph[CT], pl[CT];
+#pragma unroll
+      for (int t = 0; t < CT; ++t) {
+        if (16 * t >= rows) continue;
+        float z[8], mx = -__builtin_huge_valf();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int k = key + 16 * (e >> 2) + 4 * quad + (e & 3);
+          z[e] = mapped(sm[t], sc[t][e >> 2][e & 3], abs(pos[t] - k));
+          if (masked) {
+            if (!(k >= lo[t] && k < hi[t] && (e < 4 ? in0 : in1))) z[e] = -__builtin_huge_valf();
+          }
+          mx = fmaxf(mx, z[e]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        if (__ballot(mx > m[t])) {
+          const float mn = fmaxf(m[t], mx);
+          const float f = mn == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f(m[t] - mn);
+          m[t] = mn;
+          l[t] *= f;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) o[t][c] *= f;
+        }
+        const float ref = m[t] == -__builtin_huge_valf() ? 0.0f : m[t] - Mx<BF>::kShift;
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = __builtin_amdgcn_exp2f(z[e] - ref);
+          sum += x;
+          const typename Mx<BF>::t xh = (typename Mx<BF>::t)x;
+          ph[t][e] = xh;
+          pl[t][e] = (typename Mx<BF>::t)(x - (float)xh);
+        }
+        l[t] += sum;
+      }
+      // ---- O^T += V^T P^T, 16 channels at a time ----
+      const int r0 = 4 * quad + (lr >> 2);  // row and 8-byte piece that this lane names
+      auto v_at = [&](int c) -> s16x8 {
+        const uint32_t va = vat + r0 * kRowBytes + 16 * v_chunk(r0, 2 * c + ((lr & 3) >> 1)) + 8 * (lr & 1);
+        return __builtin_shufflevector(lds_tr(va), lds_tr(va + 16 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      const bool clean = masked && any_nonfinite<BF, kFewStage / 2>(vat);
+      if (clean) {
+#pragma unroll 1
+        for (int row = 0; row < kFewKeys; ++row) {
+          const int k = key + row;
+          const bool in = row < 16 ? in0 : in1;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const s16x4 x = *LDS_AT(const s16x4, vat + row * kRowBytes + 16 * v_chunk(row, 2 * c + (quad >> 1)) + 8 * (quad & 1));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int t = 0; t < CT; ++t)
+                if (in && k >= lo[t] && k < hi[t]) o[t][c][e] += nonfinite_part<BF>(x[e]);
+          }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        s16x8 x = v_at(c);
+        if (clean) x = finite_part<BF>(x);
+        const v8 vf = __builtin_bit_cast(v8, x);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          if (16 * t >= rows) continue;
+          o[t][c] = Mx<BF>::mfma16(vf, ph[t], o[t][c]);
+          o[t][c] = Mx<BF>::mfma16(vf, pl[t], o[t][c]);
+        }
+      }
+      // this stage is read: its next block
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        id[0][i] = id[1][i];
+        id[1][i] = id[2][i];
+      }
+      if (step + 2 < steps) issue(ahead, id[1], stage);
+    }
+    // ---- the piece's result: the output where it is the whole, or a part ----
+    const bool whole = b_first == 0 && b_end == now.nb;
+    const int slot = step - (b_end - b_first) == 0 ? 0 : 1;
+    const int64_t pr = ((int64_t)worker * 2 + slot) * R;
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      const int r = 16 * t + lr;
+      float lt = l[t];
+      lt += __shfl_xor(lt, 16, kWave);
+      lt += __shfl_xor(lt, 32, kWave);
+      if (r >= rows) continue;
+      if (whole) {
+        const int tok = r / G, g = r - tok * G;
+        uint16_t* op = p.out + ((a + tok) * H * G + h * G + g) * kD + 4 * quad;
+        const float f = lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          typename Mx<BF>::t y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(lt == 0.0f ? 0.0f : o[t][c][e] * f);
+          *reinterpret_cast<u32x2*>(op + 16 * c) = *reinterpret_cast<u32x2*>(y);
+        }
+      } else {
+        float* op = p.part_o + (pr + r) * kD + 4 * quad;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4*>(op + 16 * c) = o[t][c];
+        if (quad == 0) {
+          p.part_ml[(pr + r) * 2] = m[t];
+          p.part_ml[(pr + r) * 2 + 1] = lt;
+        }
+      }
+    }
+    const int taken = b_end - b_first;
+    now.b += taken - 1;
+    if (step < steps) next(now);
+  }
+  if (flags && lane == 0) set_status(p.st, flags);
+}
+
+// Joins the parts of one query row: out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c
+// over `count` parts, part c's row at row_of(c) (negative: none).  256 threads: 8
+// groups of 32 take every eighth part, 4 channels a thread.
+template <bool BF, class RowOf>
+__device__ __forceinline__ void join_row(const PagedAttnArgs& p, int count, RowOf row_of, uint16_t* out) {
+  __shared__ float red[4], sum_l[8];
+  __shared__ f32x4 acc[8][32];
+  const int tid = threadIdx.x, x = tid & 31, g = tid >> 5;
+  float M = -__builtin_huge_valf();
+  for (int c = tid; c < count; c += 256) {
+    const int64_t r = row_of(c);
+    if (r >= 0) M = fmaxf(M, p.part_ml[2 * r]);
+  }
+  M = wave_max(M);
+  if ((tid & 63) == 0) red[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  float l = 0.0f;
+  for (int c = g; c < count; c += 8) {
+    const int64_t r = row_of(c);
+    if (r < 0) continue;
+    const float m = p.part_ml[2 * r];
+    if (m == -__builtin_huge_valf()) continue;
+    const float w = __builtin_amdgcn_exp2f(m - M);
+    l += w * p.part_ml[2 * r + 1];
+    o += w * *reinterpret_cast<const f32x4*>(p.part_o + r * kD + 4 * x);
+  }
+  acc[g][x] = o;
+  if (x == 0) sum_l[g] = l;
+  __syncthreads();
+  if (tid < 32) {
+    float den = 0.0f;
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      den += sum_l[i];
+      s += acc[i][tid];
+    }
+    typename Mx<BF>::t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(den == 0.0f ? 0.0f : s[e] / den);
+    *reinterpret_cast<u32x2*>(out + 4 * tid) = *reinterpret_cast<u32x2*>(y);
+  }
+}
+
+// The requests of attn_few_kernel whose blocks went to more than one wave: a workgroup a
+// query row.  Block counts are recomputed from the lengths.
+template <bool BF>
+__global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  int* before = reinterpret_cast<int*>(smem);
+  uint32_t flags = 0;
+  few_plan(p, before, before + p.S + 1, flags);
+  const int s = blockIdx.x, h = blockIdx.y / R, r = blockIdx.y % R, H = p.c.H, G = p.G;
+  const int nb = before[s + 1] - before[s];
+  if (nb == 0) return;
+  const int64_t a = p.start[s];
+  if (r >= (int)(p.start[s + 1] - a) * G) return;
+  const int64_t W = (int64_t)before[p.S] * H, g0 = (int64_t)before[s] * H + (int64_t)h * nb;
+  const int w0 = worker_of(g0, W), w1 = worker_of(g0 + nb - 1, W);
+  if (w0 == w1) return;
+  const int tok = r / G;
+  join_row<BF>(
+      p, w1 - w0 + 1,
+      [&](int c) -> int64_t {
+        const int64_t b = share(w0 + c, W);
+        if (b == share(w0 + c + 1, W)) return -1;  // a wave without blocks
+        return ((int64_t)(w0 + c) * 2 + (b < g0 ? 1 : 0)) * R + r;
+      },
+      p.out + ((a + tok) * H * G + h * G + (r - tok * G)) * kD);
+}
+
+// ---------------------------------------------------------------- many query rows
+// Row tiles of the requests with more than `few` query rows: before[s] those of the
+// requests before s.
+__device__ __forceinline__ void many_plan(const PagedAttnArgs& p, int* before, int* part, uint32_t& flags) {
+  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (p.S + nt - 1) / nt, tm = kManyRows / p.G;
+  int sum = 0;
+  for (int i = 0; i < per; ++i) {
+    const int s = tid * per + i;
+    if (s >= p.S) break;
+    int64_t a, n;
+    const int rows = request_rows(p, s, &a, &n, flags);
+    before[s] = sum;
+    if (rows * p.G > p.few) sum += (rows + tm - 1) / tm;
+  }
+  int inc = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(inc, o, kWave);
+    if (lane >= o) inc += x;
+  }
+  if (lane == 63) part[wave] = inc;
+  __syncthreads();
+  int base = inc - sum;
+  for (int w = 0; w < wave; ++w) base += part[w];
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < p.S) before[tid * per + i] += base;
+  if (tid == nt - 1) before[p.S] = base + sum;
+  __syncthreads();
+}
+
+// Parts that a tile of nb key blocks is cut into, of at least 4 blocks each.
+__device__ __forceinline__ int parts_of(int nb, int nsplit) { return max(min(nsplit, nb / 4), 1); }
+
+struct ManyTile {
+  int s, h, tok0, toks, n, lo, hi;  // tokens of the tile and the union of their ranges
+  int64_t a;
+};
+
+// Tile and head of a workgroup index (later tiles, which see more, first).  Every thread of
+// 256; red[8] is LDS.
+__device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int* before, int tile, int h, int* red) {
+  ManyTile t;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tm = kManyRows / p.G;
+  const int x = before[p.S] - 1 - tile;
+  t.s = uniform(request_of(before, p.S, x));
+  t.h = h;
+  t.a = fixed(p.start, t.s);
+  t.n = uniform((int)fixed(p.n, t.s));
+  const int total = uniform((int)(fixed(p.start, t.s + 1) - t.a));
+  t.tok0 = (x - uniform(before[t.s])) * tm;
+  t.toks = min(tm, total - t.tok0);
+  int lo = t.n, hi = 0;
+  if (tid < t.toks) token_range(p, t.s, t.a + t.tok0 + tid, t.n - total + t.tok0 + tid, t.n, &lo, &hi);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    lo = min(lo, __shfl_xor(lo, o, kWave));
+    hi = max(hi, __shfl_xor(hi, o, kWave));
+  }
+  if (lane == 0) {
+    red[wave] = lo;
+    red[4 + wave] = hi;
+  }
+  __syncthreads();
+  t.lo = uniform(min(min(red[0], red[1]), min(red[2], red[3]))) & ~(kManyKeys - 1);
+  t.hi = uniform(max(max(red[4], red[5]), max(red[6], red[7])));
+  __syncthreads();
+  return t;
+}
+
+template <bool BF, bool MAPPED>
+__global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  typedef typename Mx<BF>::v8 v8;
+  typedef typename Mx<BF>::t vt;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5, lr = lane & 31;
+  int* before = reinterpret_cast<int*>(smem + kManyStages * kManyStage);
+  int* red = before + p.S + 1;
+  uint32_t flags = 0;
+  many_plan(p, before, red, flags);
+  if (flags && blockIdx.x == 0) set_status(p.st, flags);
+  flags = 0;
+  const int H = p.c.H, G = p.G;
+  const int bid = blockIdx.x, h = bid % H, part = (bid / H) % p.nsplit, tile = bid / H / p.nsplit;
+  if (tile >= before[p.S]) return;
+  const ManyTile t = many_tile(p, before, tile, h, red);
+  const int all = max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 0), parts = parts_of(all, p.nsplit);
+  if (part >= parts) return;
+  const int b0 = (int)((int64_t)all * part / parts), nb = (int)((int64_t)all * (part + 1) / parts) - b0;
+  const int key0 = t.lo + b0 * kManyKeys, n = t.n;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))smem;
+  const int total = uniform((int)(fixed(p.start, t.s + 1) - t.a)), rows = t.toks * G;
+
+  // ---- the wave's 64 query rows: column tiles of 32 ----
+  v8 qf[2][8];
+  int pos[2], lo[2], hi[2], lo_min = n, lo_max = 0, hi_min = n, hi_max = 0;
+  ScoreMap sm[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int r = wave * 64 + c * 32 + lr, tok = r / G, g = r - tok * G;
+    pos[c] = 0;
+    lo[c] = 0;
+    hi[c] = n;
+    float slope = 0.0f;
+    s16x8 z = {};
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) qf[c][kk] = __builtin_bit_cast(v8, z);
+    if (r < rows) {
+      const int64_t row = t.a + t.tok0 + tok;
+      pos[c] = n - total + t.tok0 + tok;
+      token_range(p, t.s, row, pos[c], n, &lo[c], &hi[c]);
+      if (p.slopes) slope = p.slopes[h * G + g];
+      const uint16_t* qp = p.q + row * p.ldq_tok + (int64_t)(h * G + g) * p.ldq_head + 8 * half;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) qf[c][kk] = *reinterpret_cast<const v8*>(qp + 16 * kk);
+      lo_min = min(lo_min, lo[c]);
+      hi_max = max(hi_max, hi[c]);
+      lo_max = max(lo_max, lo[c]);
+      hi_min = min(hi_min, hi[c]);
+    }
+    sm[c] = score_map(p, slope);
+  }
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) {
+    lo_min = min(lo_min, __shfl_xor(lo_min, o, kWave));
+    lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
+    hi_min = min(hi_min, __shfl_xor(hi_min, o, kWave));
+    hi_max = max(hi_max, __shfl_xor(hi_max, o, kWave));
+  }
+  lo_min = uniform(lo_min);
+  lo_max = uniform(lo_max);
+  hi_min = uniform(hi_min);
+  hi_max = uniform(hi_max);
+
+  // ---- loads: wave w takes keys 16w .. 16w + 15 of a block, K and V ----
+  const uint32_t row_step = (uint32_t)p.c.ld_tok * 2;
+  uint32_t koff[4], voff[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 4 * i + (lane >> 4);
+    koff[i] = row * row_step + 16 * k_chunk(row, lane & 15);
+    voff[i] = row * row_step + 16 * v_chunk(row, lane & 15);
+  }
+  auto page = [&](int b) -> int {  // of the wave's keys of block b
+    const int k = key0 + b * kManyKeys + 16 * wave;
+    return b < nb && k < n ? page_uniform(p.c, t.s, k >> p.c.shift) : kNone;
+  };
+  auto issue = [&](int b, int id) {
+    const bool ok = (uint32_t)id < (uint32_t)p.c.P;
+    if (!ok && id != kNone) flags |= FATHOM_DEV_BAD_PAGE;
+    const int k = key0 + b * kManyKeys + 16 * wave;
+    const int64_t o = (int64_t)(ok ? id : 0) * p.c.ld_page + (int64_t)h * p.c.ld_head + (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
+    const void *kb = p.c.K + o, *vb = p.c.V + o;  // absent: rows of page 0, which no one uses
+    const uint32_t at = lds0 + (b % kManyStages) * kManyStage + wave * 4096;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) load_to_lds(at + y * 1024, kb, koff[y]);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) load_to_lds(at + kManyStage / 2 + y * 1024, vb, voff[y]);
+  };
+
+  // LDS places of a lane's part of K fragments (of key lr, channels 16 kk + 8 half ..: chunk
+  // 2 kk + half, permuted) and of V^T fragments (groups of 16 lanes name channels 0..15 and
+  // 16..31 of 32 and keys 4 half ..)
+  const uint32_t klane = lr * kRowBytes, kswap = 16 * k_chunk(lr, half);
+  uint32_t vlane[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const int r0 = 4 * half + ((lane & 15) >> 2), ch = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    vlane[d] = r0 * kRowBytes + 16 * v_chunk(r0, ch) + 8 * (lane & 1);
+  }
+  f32x16 o[2][4];
+  float m[2], l[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    m[c] = -__builtin_huge_valf();
+    l[c] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[c][d][e] = 0.0f;
+  }
+  // every block is issued, the ones behind the last with rows that no one reads, so
+  // that the number of loads in flight is always the same
+  int id = page(0);
+#pragma unroll
+  for (int b = 0; b < kManyStages - 1; ++b) {
+    const int nxt = page(b + 1);
+    issue(b, id);
+    id = nxt;
+  }
+  for (int b = 0; b < nb; ++b) {
+    wait_vm<8 * (kManyStages - 2)>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last block's reads, before its stage is loaded anew
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int nxt = page(b + kManyStages);
+    issue(b + kManyStages - 1, id);
+    id = nxt;
+    const int key = key0 + b * kManyKeys;
+    const uint32_t at = lds0 + (b % kManyStages) * kManyStage, vat = at + kManyStage / 2;
+    // absent pages of this block: a bit per 16 keys
+    uint32_t absent = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = key + 16 * i;
+      if (k < n && (uint32_t)page_uniform(p.c, t.s, k >> p.c.shift) >= (uint32_t)p.c.P) absent |= 1u << i;
+    }
+    if (key + kManyKeys > n || absent) {  // rows that are not there: V is cleared, a wave its 16
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int row = 16 * wave + 4 * y + (lane >> 4);
+        if (key + row >= n || ((absent >> wave) & 1))
+          *LDS_AT(u32x4, vat + row * kRowBytes + 16 * (lane & 15)) = (u32x4){0u, 0u, 0u, 0u};
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    }
+    if (key >= hi_max || key + kManyKeys <= lo_min) continue;  // none of the wave's rows sees the block
+    const bool masked = key < lo_max || key + kManyKeys > hi_min || absent;
+    // ---- S^T: two groups of 32 keys ----
+    f32x16 sc[2][2];
+#pragma unroll
+    for (int gk = 0; gk < 2; ++gk) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[c][gk][e] = 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {
+        const v8 kf = lds_v8<v8>(at + klane + (kswap ^ (32 * kk)) + 32 * gk * kRowBytes);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) sc[c][gk] = Mx<BF>::mfma32(kf, qf[c][kk], sc[c][gk]);
+      }
+    }
+    // ---- softmax ----
+    v8 pf[2][4];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      float mx = -__builtin_huge_valf();
+      if constexpr (MAPPED) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const int k = key + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * half + (e & 3);
+          sc[c][e >> 4][e & 15] = mapped(sm[c], sc[c][e >> 4][e & 15], abs(pos[c] - k));
+        }
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const int j = 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * half + (e & 3), k = key + j;
+          if (!(k >= lo[c] && k < hi[c] && !((absent >> (j >> 4)) & 1))) sc[c][e >> 4][e & 15] = -__builtin_huge_valf();
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sc[c][e >> 4][e & 15]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      const float c1 = MAPPED ? 1.0f : sm[c].c1;
+      if (__ballot(mx > m[c])) {
+        const float mn = fmaxf(m[c], mx);
+        const float f = mn == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f((m[c] - mn) * c1);
+        m[c] = mn;
+        l[c] *= f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[c][d] *= f;
+      }
+      const float ref = m[c] == -__builtin_huge_valf() ? 0.0f : m[c] * c1 - Mx<BF>::kShift;
+      float sum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][e >> 4][e & 15], c1, -ref));
+        sum += x;
+        pf[c][e >> 3][e & 7] = (vt)x;
+      }
+      l[c] += sum;
+    }
+    // ---- O^T += V^T P^T: 32 channels, 16 keys at a time ----
+    const bool clean = masked && any_nonfinite<BF, kManyStage / 2>(vat);
+    if (clean) {
+#pragma unroll 1
+      for (int row = 0; row < kManyKeys; ++row) {
+        const int k = key + row;
+        const bool in = !((absent >> (row >> 4)) & 1);
+#pragma unroll
+        for (int y = 0; y < 16; ++y) {  // channels 8 y + 4 half ..
+          const s16x4 x = *LDS_AT(const s16x4, vat + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              if (in && k >= lo[c] && k < hi[c]) o[c][y >> 2][4 * (y & 3) + e] += nonfinite_part<BF>(x[e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const uint32_t va = vat + vlane[d] + 16 * i * kRowBytes;
+        s16x8 x = __builtin_shufflevector(lds_tr(va), lds_tr(va + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7);
+        if (clean) x = finite_part<BF>(x);
+        const v8 vf = __builtin_bit_cast(v8, x);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) o[c][d] = Mx<BF>::mfma32(vf, pf[c][i], o[c][d]);
+      }
+    }
+  }
+  // ---- the output, or a part of it ----
+  wait_vm<0>();
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int r = wave * 64 + c * 32 + lr;
+    float lt = l[c] + __shfl_xor(l[c], 32, kWave);
+    if (r >= rows) continue;
+    if (parts == 1) {
+      const int tok = r / G, g = r - tok * G;
+      uint16_t* op = p.out + ((t.a + t.tok0 + tok) * H * G + h * G + g) * kD + 4 * half;
+      const float f = 1.0f / lt;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          vt y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = (vt)(lt == 0.0f ? 0.0f : o[c][d][e + i] * f);
+          *reinterpret_cast<u32x2*>(op + 32 * d + 2 * e) = *reinterpret_cast<u32x2*>(y);
+        }
+    } else {
+      const int64_t pr = (((int64_t)tile * H + h) * p.nsplit + part) * kManyRows + r;
+      float* op = p.part_o + pr * kD + 4 * half;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<f32x4*>(op + 32 * d + 2 * e) = (f32x4){o[c][d][e], o[c][d][e + 1], o[c][d][e + 2], o[c][d][e + 3]};
+      if (half == 0) {
+        p.part_ml[pr * 2] = MAPPED ? m[c] : m[c] * sm[c].c1;
+        p.part_ml[pr * 2 + 1] = lt;
+      }
+    }
+  }
+  if (flags && lane == 0) set_status(p.st, flags);
+}
+
+// The tiles whose keys were split, a workgroup 16 query rows.
+constexpr int kManyJoin = 16;
+template <bool BF>
+__global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  int* before = reinterpret_cast<int*>(smem);
+  int* red = before + p.S + 1;
+  uint32_t flags = 0;
+  many_plan(p, before, red, flags);
+  const int H = p.c.H, G = p.G, tile = blockIdx.x / H, h = blockIdx.x % H;
+  if (tile >= before[p.S]) return;
+  const ManyTile t = many_tile(p, before, tile, h, red);
+  const int parts = parts_of(max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 0), p.nsplit), rows = t.toks * G;
+  if (parts == 1) return;
+  const int64_t base = ((int64_t)tile * H + h) * p.nsplit * kManyRows;
+  // 8 rows at a time, 32 threads and 4 channels a thread each
+  const int x = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < kManyJoin; i += 8) {
+    const int r = blockIdx.y * kManyJoin + i + (threadIdx.x >> 5);
+    if (r >= rows) return;
+    float M = -__builtin_huge_valf();
+    for (int c = 0; c < parts; ++c) M = fmaxf(M, p.part_ml[2 * (base + (int64_t)c * kManyRows + r)]);
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    float l = 0.0f;
+    for (int c = 0; c < parts; ++c) {
+      const int64_t pr = base + (int64_t)c * kManyRows + r;
+      const float m = p.part_ml[2 * pr];
+      if (m == -__builtin_huge_valf()) continue;
+      const float w = __builtin_amdgcn_exp2f(m - M);
+      l += w * p.part_ml[2 * pr + 1];
+      o += w * *reinterpret_cast<const f32x4*>(p.part_o + pr * kD + 4 * x);
+    }
+    const int tok = r / G, g = r - tok * G;
+    typename Mx<BF>::t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(l == 0.0f ? 0.0f : o[e] / l);
+    *reinterpret_cast<u32x2*>(p.out + ((t.a + t.tok0 + tok) * H * G + h * G + g) * kD + 4 * x) =
+        *reinterpret_cast<u32x2*>(y);
+  }
+}
+
+// ---------------------------------------------------------------- launches
+struct PagedAttnPlan {
+  int few, R;         // rows up to which a request goes to attn_few_kernel; the rows it is built for
+  bool run_few, run_many;
+  int64_t tiles;      // bound on attn_many_kernel's row tiles
+  int nsplit;
+  int64_t part_rows;  // rows of partial results
+};
+
+static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) {
+  PagedAttnPlan a = {};
+  const int64_t most = (max_new < T ? max_new : T) * G;  // query rows of a request and head, at most
+  a.few = kFewRows;
+  a.R = most <= 16 ? 16 : kFewRows;
+  a.run_many = most > kFewRows;
+  // one request whose rows are all there are is known to be large; more may be of either kind
+  a.run_few = !a.run_many || S > 1 || T <= kFewRows / G;
+  const int tm = kManyRows / G;
+  a.nsplit = 1;
+  if (a.run_many) {
+    const int64_t large = T / (kFewRows / G + 1) < S ? T / (kFewRows / G + 1) : S;  // requests that can be large
+    a.tiles = T / tm + large;
+    // fill 256 CUs: the fewest parts that leave at most a tenth of them idle in the last round
+    const int64_t wgs = (T + tm - 1) / tm * H;
+    for (int ns = 1; ns <= 8; ++ns) {
+      const int64_t rounds = (wgs * ns + 255) / 256;
+      a.nsplit = ns;
+      if (wgs * ns * 10 >= rounds * 256 * 9 || wgs * ns > 2048) break;
+    }
+  }
+  const int64_t few_rows = a.run_few ? (int64_t)kFewWorkers * 2 * a.R : 0;
+  const int64_t many_rows = a.run_many && a.nsplit > 1 ? a.tiles * H * a.nsplit * kManyRows : 0;
+  a.part_rows = few_rows > many_rows ? few_rows : many_rows;
+  return a;
+}
+
+size_t paged_attn_ws_bytes(int64_t T, int S, int H, int G, int64_t max_new) {
+  const PagedAttnPlan a = attn_plan(T, S, H, G, max_new);
+  return (size_t)a.part_rows * (kD + 2) * sizeof(float) + 1024;
+}
+
+template <bool BF>
+static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) {
+  const size_t plan = (size_t)(p.S + 1 + 8) * sizeof(int);
+  p.tiles = (int)a.tiles;
+  p.nsplit = a.nsplit;
+  p.few = a.few;
+  if (a.run_many) {
+    const dim3 grid((unsigned)(a.tiles * a.nsplit * p.c.H));
+    const size_t lds = (size_t)kManyStages * kManyStage + plan;
+    if (p.softcap > 0.0f || p.slopes || !(p.sm_scale > 0.0f))
+      hipLaunchKernelGGL((attn_many_kernel<BF, true>), grid, dim3(256), lds, s, p);
+    else
+      hipLaunchKernelGGL((attn_many_kernel<BF, false>), grid, dim3(256), lds, s, p);
+    if (a.nsplit > 1)
+      hipLaunchKernelGGL((attn_many_join_kernel<BF>), dim3((unsigned)(a.tiles * p.c.H), kManyRows / kManyJoin),
+                         dim3(256), plan, s, p);
+  }
+  if (a.run_few) {
+    const dim3 grid(kFewWorkers / kFewWaves), threads(kFewWaves * kWave);
+    const size_t lds = (size_t)kFewWaves * 2 * kFewStage + plan;
+    if (a.R == 16) hipLaunchKernelGGL((attn_few_kernel<BF, 1>), grid, threads, lds, s, p);
+    else hipLaunchKernelGGL((attn_few_kernel<BF, kFewRows / 16>), grid, threads, lds, s, p);
+    hipLaunchKernelGGL((attn_join_kernel<BF>), dim3((unsigned)p.S, (unsigned)(p.c.H * a.R)), dim3(256), plan, s, p,
+                       a.R);
+  }
+}
+
+fathom_status launch_paged_attn(const void* q, int64_t ldq_tok, int64_t ldq_head, const Paged& c, bool bf16,
+                                const int64_t* start, const int64_t* n, int S, int64_t T, int64_t max_new, int G,
+                                float sm_scale, float softcap, const float* slopes, const int64_t* prefix,
+                                const int64_t* first, void* out, void* ws, uint32_t* st, hipStream_t s) {
+  const PagedAttnPlan a = attn_plan(T, S, c.H, G, max_new);
+  PagedAttnArgs p = {};
+  p.q = reinterpret_cast<const uint16_t*>(q);
+  p.ldq_tok = ldq_tok;
+  p.ldq_head = ldq_head;
+  p.c = c;
+  p.start = start;
+  p.n = n;
+  p.S = S;
+  p.G = G;
+  p.T = T;
+  p.max_new = max_new;
+  p.sm_scale = sm_scale;
+  p.softcap = softcap;
+  p.slopes = slopes;
+  p.prefix = prefix;
+  p.first = first;
+  p.out = reinterpret_cast<uint16_t*>(out);
+  p.part_o = reinterpret_cast<float*>(ws);
+  p.part_ml = p.part_o + a.part_rows * kD;
+  p.st = st;
+  if (bf16) launch_attn<true>(p, a, s);
+  else launch_attn<false>(p, a, s);
+  FATHOM_LAUNCH_CHECK();
+  return FATHOM_OK;
+}
+
+}  // namespace fathom
