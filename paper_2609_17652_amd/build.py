@@ -11,6 +11,7 @@ import glob
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -21,11 +22,16 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 FLAGS = [
-    f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared",
+    f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off", "-fno-fast-math",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
+
+
+# Per source: attn_many_kernel's accumulators are worked on by the vector unit, so its matrix
+# instructions write vector registers (the default moves each to and from accumulation registers).
+SOURCE_FLAGS = {"paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def sources():
@@ -33,8 +39,24 @@ def sources():
 
 
 def _hipcc(out: str, srcs, verbose: bool) -> None:
+    """Compiles the sources side by side and links them to `out`."""
     tmp = out + ".tmp"
-    cmd = [HIPCC, *FLAGS, "-o", tmp, *srcs]
+    objects = [f"{out}.{os.path.basename(src)}.o" for src in srcs]
+
+    def one(src, obj):
+        extra = SOURCE_FLAGS.get(os.path.basename(src), [])
+        _run([HIPCC, *FLAGS, *extra, "-c", "-o", obj, src], verbose)
+
+    with ThreadPoolExecutor(max_workers=8) as pool:
+        for job in [pool.submit(one, src, obj) for src, obj in zip(srcs, objects)]:
+            job.result()
+    _run([HIPCC, f"--offload-arch={ARCH}", "-fPIC", "-shared", "-o", tmp, *objects], verbose)
+    for obj in objects:
+        os.remove(obj)
+    os.replace(tmp, out)
+
+
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -44,7 +66,6 @@ def _hipcc(out: str, srcs, verbose: bool) -> None:
         raise RuntimeError(f"hipcc failed ({res.returncode}):\n{err}")
     if err.strip() and verbose:
         print(err, file=sys.stderr)
-    os.replace(tmp, out)
 
 
 def build(verbose: bool = False) -> str:

@@ -28,6 +28,8 @@
 // V rows behind the end are cleared in LDS, and in steps with masked places
 // the non-finite values of V are taken out of the product and added for the rows
 // that see them.
+#include <type_traits>
+
 #include "paged.hpp"
 
 namespace fathom {
@@ -114,10 +116,18 @@ __device__ __forceinline__ void token_range(const PagedAttnArgs& p, int s, int64
 }
 
 // ---------------------------------------------------------------- tools
-// 64 lanes x 16 bytes: from base + voff (a lane's) to LDS at `lds` + 16 lane.  The
-// wait is the caller's (vmcnt); no register is written.
-__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint32_t voff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base) : "memory");
+// 16 rows, four of 64 lanes x 16 bytes at a time: rows 4y .. 4y + 3 from base + 1024 y + off[y]
+// (a lane's) to LDS at `lds` + 1024 y + 16 lane; an instruction's offset counts on both sides.
+// The wait is the caller's (vmcnt); no register is written.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, const uint32_t (&off)[4]) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %5\n\t"
+      "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+      "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+      "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds),
+      "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base)
+      : "memory");
 }
 
 template <int N>
@@ -136,19 +146,26 @@ struct Mx;
 template <>
 struct Mx<false> {
   typedef f16x8 v8;
+  typedef _Float16 v2 __attribute__((ext_vector_type(2)));
   typedef _Float16 t;
   static constexpr uint16_t kInf = 0x7C00, kOne = 0x3C00;
-  static constexpr float kShift = 14.0f;  // probabilities are kept times 2^14: no subnormals down to 2^-28
+  static constexpr float kShift = 8.0f;  // probabilities are kept times 2^8: no subnormals down to 2^-22
   static __device__ __forceinline__ f32x4 mfma16(v8 a, v8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
   static __device__ __forceinline__ f32x16 mfma32(v8 a, v8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
+  // sum + a[0] + a[1], in 32 bits
+  static __device__ __forceinline__ float add_pair(v2 a, float sum) {
+    const v2 one = {(_Float16)1.0f, (_Float16)1.0f};
+    return __builtin_amdgcn_fdot2(a, one, sum, false);
+  }
 };
 template <>
 struct Mx<true> {
   typedef bf16x8 v8;
+  typedef __bf16 v2 __attribute__((ext_vector_type(2)));
   typedef __bf16 t;
   static constexpr uint16_t kInf = 0x7F80, kOne = 0x3F80;
   static constexpr float kShift = 0.0f;
@@ -157,6 +174,10 @@ struct Mx<true> {
   }
   static __device__ __forceinline__ f32x16 mfma32(v8 a, v8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ float add_pair(v2 a, float sum) {
+    const v2 one = {(__bf16)1.0f, (__bf16)1.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(a, one, sum, false);
   }
 };
 
@@ -323,8 +344,8 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = 4 * i + quad;
-    koff[i] = row * row_step + 16 * k_chunk(row, lr);
-    voff[i] = row * row_step + 16 * v_chunk(row, lr);
+    koff[i] = row * row_step + 16 * k_chunk(row, lr) - 1024 * i;  // 4 rows are 1024 bytes at least
+    voff[i] = row * row_step + 16 * v_chunk(row, lr) - 1024 * i;
   }
   auto lowest = [&](int s) -> int {  // few_lo of request s, by the wave
     if (!p.first) return 0;
@@ -379,10 +400,8 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
       const int64_t o = (int64_t)(ok ? id[i] : 0) * p.c.ld_page + (int64_t)x.h * p.c.ld_head +
                         (int64_t)((key + 16 * i) & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
       const void *kb = p.c.K + o, *vb = p.c.V + o;  // absent: rows of page 0, which no one uses
-#pragma unroll
-      for (int y = 0; y < 4; ++y) load_to_lds(at + i * 4096 + y * 1024, kb, koff[y]);
-#pragma unroll
-      for (int y = 0; y < 4; ++y) load_to_lds(at + kFewStage / 2 + i * 4096 + y * 1024, vb, voff[y]);
+      load_to_lds(at + i * 4096, kb, koff);
+      load_to_lds(at + kFewStage / 2 + i * 4096, vb, voff);
     }
   };
 
@@ -745,6 +764,14 @@ __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int*
   return t;
 }
 
+// A block of 64 keys is two halves of 32.  While the matrix cores form the scores of the
+// next half and add the last half's products with V, the vector unit takes the exponentials
+// of this half: three halves are under way at a time, in registers S (two), P (two) and O.
+// The maximum that the exponentials are taken against is raised only when a score exceeds
+// it by more than kSlack (a factor of 2^kSlack is no loss in 32-bit sums, and
+// Mx::kShift leaves room for it in the probabilities), so the sums are rarely rescaled.
+constexpr float kSlack = 6.0f;
+
 template <bool BF, bool MAPPED>
 __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -756,7 +783,6 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   uint32_t flags = 0;
   many_plan(p, before, red, flags);
   if (flags && blockIdx.x == 0) set_status(p.st, flags);
-  flags = 0;
   const int H = p.c.H, G = p.G;
   const int bid = blockIdx.x, h = bid % H, part = (bid / H) % p.nsplit, tile = bid / H / p.nsplit;
   if (tile >= before[p.S]) return;
@@ -768,9 +794,62 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))smem;
   const int total = uniform((int)(fixed(p.start, t.s + 1) - t.a)), rows = t.toks * G;
 
+  // ---- absent pages among the keys: their blocks are masked throughout ----
+  bool absent = false;
+  {
+    const int e1 = min(key0 + nb * kManyKeys, n);
+    for (int k = key0 + 16 * tid; k < e1; k += 16 * 256)
+      absent |= (uint32_t)page_of(p.c, t.s, k >> p.c.shift) >= (uint32_t)p.c.P;
+    if (lane == 0) red[wave] = 0;
+    const bool any = __ballot(absent) != 0;
+    if (lane == 0) red[wave] = any;
+    __syncthreads();
+    absent = uniform(red[0] | red[1] | red[2] | red[3]) != 0;
+    if (absent && tid == 0) set_status(p.st, FATHOM_DEV_BAD_PAGE);
+  }
+  // whether key k's page is there
+  auto there = [&](int k) -> bool {
+    return !absent || (uint32_t)page_of(p.c, t.s, min(k, n - 1) >> p.c.shift) < (uint32_t)p.c.P;
+  };
+
+  // ---- loads: wave w takes keys 16w .. 16w + 15 of a block ----
+  const uint32_t row_step = (uint32_t)p.c.ld_tok * 2;
+  uint32_t koff[4], voff[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 4 * i + (lane >> 4);
+    koff[i] = row * row_step + 16 * k_chunk(row, lane & 15) - 1024 * i;  // 4 rows are 1024 bytes at least
+    voff[i] = row * row_step + 16 * v_chunk(row, lane & 15) - 1024 * i;
+  }
+  // Where the wave's keys of block b begin in a pool; page 0 where there is none.
+  const uint16_t *Kh = p.c.K + (int64_t)h * p.c.ld_head, *Vh = p.c.V + (int64_t)h * p.c.ld_head;
+  auto page = [&](int b) -> int {
+    const int k = key0 + b * kManyKeys + 16 * wave;
+    return b < nb && k < n ? page_uniform(p.c, t.s, k >> p.c.shift) : 0;
+  };
+  auto place = [&](int b, int id) -> int64_t {
+    const int k = key0 + b * kManyKeys + 16 * wave;
+    return (int64_t)((uint32_t)id < (uint32_t)p.c.P ? id : 0) * p.c.ld_page +
+           (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
+  };
+  auto stage = [](int b) -> uint32_t { return (uint32_t)(b % kManyStages) * (kManyStage / 2); };
+  constexpr uint32_t kVRing = kManyStages * (kManyStage / 2);  // V's stages behind K's
+  const uint32_t mine = lds0 + wave * 4096;
+  // K runs three blocks ahead of what is in use, V two: a block's V is read half a block
+  // after its K.  Blocks behind the last are loaded from page 0 and not used, so that the
+  // number of loads in flight is always the same.
+  int64_t from = place(0, page(0)), from_next = place(1, page(1));
+  load_to_lds(mine + stage(0), Kh + from, koff);
+  load_to_lds(mine + stage(1), Kh + from_next, koff);
+  load_to_lds(mine + kVRing + stage(0), Vh + from, voff);
+  from = place(2, page(2));
+  load_to_lds(mine + stage(2), Kh + from, koff);
+  load_to_lds(mine + kVRing + stage(1), Vh + from_next, voff);
+  int id_next = page(3);
+
   // ---- the wave's 64 query rows: column tiles of 32 ----
   v8 qf[2][8];
-  int pos[2], lo[2], hi[2], lo_min = n, lo_max = 0, hi_min = n, hi_max = 0;
+  int pos[2], lo[2], hi[2], lo_max = 0, hi_min = n;
   ScoreMap sm[2];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
@@ -790,8 +869,6 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
       const uint16_t* qp = p.q + row * p.ldq_tok + (int64_t)(h * G + g) * p.ldq_head + 8 * half;
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) qf[c][kk] = *reinterpret_cast<const v8*>(qp + 16 * kk);
-      lo_min = min(lo_min, lo[c]);
-      hi_max = max(hi_max, hi[c]);
       lo_max = max(lo_max, lo[c]);
       hi_min = min(hi_min, hi[c]);
     }
@@ -799,53 +876,28 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   }
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) {
-    lo_min = min(lo_min, __shfl_xor(lo_min, o, kWave));
     lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
     hi_min = min(hi_min, __shfl_xor(hi_min, o, kWave));
-    hi_max = max(hi_max, __shfl_xor(hi_max, o, kWave));
   }
-  lo_min = uniform(lo_min);
   lo_max = uniform(lo_max);
   hi_min = uniform(hi_min);
-  hi_max = uniform(hi_max);
-
-  // ---- loads: wave w takes keys 16w .. 16w + 15 of a block, K and V ----
-  const uint32_t row_step = (uint32_t)p.c.ld_tok * 2;
-  uint32_t koff[4], voff[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = 4 * i + (lane >> 4);
-    koff[i] = row * row_step + 16 * k_chunk(row, lane & 15);
-    voff[i] = row * row_step + 16 * v_chunk(row, lane & 15);
-  }
-  auto page = [&](int b) -> int {  // of the wave's keys of block b
-    const int k = key0 + b * kManyKeys + 16 * wave;
-    return b < nb && k < n ? page_uniform(p.c, t.s, k >> p.c.shift) : kNone;
-  };
-  auto issue = [&](int b, int id) {
-    const bool ok = (uint32_t)id < (uint32_t)p.c.P;
-    if (!ok && id != kNone) flags |= FATHOM_DEV_BAD_PAGE;
-    const int k = key0 + b * kManyKeys + 16 * wave;
-    const int64_t o = (int64_t)(ok ? id : 0) * p.c.ld_page + (int64_t)h * p.c.ld_head + (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
-    const void *kb = p.c.K + o, *vb = p.c.V + o;  // absent: rows of page 0, which no one uses
-    const uint32_t at = lds0 + (b % kManyStages) * kManyStage + wave * 4096;
-#pragma unroll
-    for (int y = 0; y < 4; ++y) load_to_lds(at + y * 1024, kb, koff[y]);
-#pragma unroll
-    for (int y = 0; y < 4; ++y) load_to_lds(at + kManyStage / 2 + y * 1024, vb, voff[y]);
-  };
+  const float c1 = MAPPED ? 1.0f : sm[0].c1;
 
   // LDS places of a lane's part of K fragments (of key lr, channels 16 kk + 8 half ..: chunk
   // 2 kk + half, permuted) and of V^T fragments (groups of 16 lanes name channels 0..15 and
   // 16..31 of 32 and keys 4 half ..)
-  const uint32_t klane = lr * kRowBytes, kswap = 16 * k_chunk(lr, half);
-  uint32_t vlane[4];
+  uint32_t kaddr[8], vlane[4];
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) kaddr[kk] = lds0 + lr * kRowBytes + 16 * k_chunk(lr, 2 * kk + half);
 #pragma unroll
   for (int d = 0; d < 4; ++d) {
     const int r0 = 4 * half + ((lane & 15) >> 2), ch = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    vlane[d] = r0 * kRowBytes + 16 * v_chunk(r0, ch) + 8 * (lane & 1);
+    vlane[d] = lds0 + kVRing + r0 * kRowBytes + 16 * v_chunk(r0, ch) + 8 * (lane & 1);
   }
-  f32x16 o[2][4];
+  constexpr uint32_t kHalf = 32 * kRowBytes;
+
+  f32x16 o[2][4], sa[2], sb[2];
+  u32x4 pa[2][2], pb[2][2];
   float m[2], l[2];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
@@ -856,111 +908,143 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[c][d][e] = 0.0f;
   }
-  // every block is issued, the ones behind the last with rows that no one reads, so
-  // that the number of loads in flight is always the same
-  int id = page(0);
+  // S^T of the 32 keys at byte `at` of K's ring
+  auto scores = [&](uint32_t at, f32x16 (&s)[2]) {
 #pragma unroll
-  for (int b = 0; b < kManyStages - 1; ++b) {
-    const int nxt = page(b + 1);
-    issue(b, id);
-    id = nxt;
-  }
-  for (int b = 0; b < nb; ++b) {
-    wait_vm<8 * (kManyStages - 2)>();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last block's reads, before its stage is loaded anew
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[c][e] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const v8 kf = lds_v8<v8>(kaddr[kk] + at);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) s[c] = Mx<BF>::mfma32(kf, qf[c][kk], s[c]);
+    }
+  };
+  // O^T += V^T P^T of the 32 keys at byte `at` of V's ring
+  auto product = [&](uint32_t at, const u32x4 (&pr)[2][2], auto clean) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const uint32_t va = vlane[d] + at + 16 * i * kRowBytes;
+        s16x8 x = __builtin_shufflevector(lds_tr(va), lds_tr(va + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7);
+        if constexpr (decltype(clean)::value) x = finite_part<BF>(x);
+        const v8 vf = __builtin_bit_cast(v8, x);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) o[c][d] = Mx<BF>::mfma32(vf, __builtin_bit_cast(v8, pr[c][i]), o[c][d]);
+      }
+  };
+  auto exponentials = [&](const f32x16 (&s)[2], u32x4 (&pr)[2][2]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const float neg = m[c] == -__builtin_huge_valf() ? 0.0f : Mx<BF>::kShift - m[c] * c1;
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, neg));
+        const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, neg));
+        const typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
+        l[c] = Mx<BF>::add_pair(pair, l[c]);
+        pr[c][e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, pair);
+      }
+    }
+  };
+  auto map_scores = [&](f32x16 (&s)[2], int key) {
+    if constexpr (MAPPED) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          s[c][e] = mapped(sm[c], s[c][e], abs(pos[c] - (key + 8 * (e >> 2) + 4 * half + (e & 3))));
+    }
+  };
+  // The maximum of a half's scores: where it is raised, the sums' factor in f (and true).
+  auto raise = [&](const f32x16 (&s)[2], float (&f)[2]) -> bool {
+    float mx[2];
+    bool up = false;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      mx[c] = fmaxf(s[c][0], s[c][1]);
+#pragma unroll
+      for (int e = 2; e < 16; e += 2) mx[c] = fmaxf(fmaxf(mx[c], s[c][e]), s[c][e + 1]);
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx[c]), __float_as_uint(mx[c]), false, false);
+      mx[c] = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      up |= (mx[c] - m[c]) * c1 > kSlack;  // -Inf less -Inf is no reason
+    }
+    if (!__ballot(up)) return false;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const float mn = fmaxf(m[c], mx[c]);
+      f[c] = mn == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f((m[c] - mn) * c1);
+      m[c] = mn;
+      l[c] *= f[c];
+    }
+    return true;
+  };
+  auto rescale = [&](const float (&f)[2]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) o[c][d] *= f[c];
+  };
+  // K of block b + 1 and V of block b are in LDS once all but the last 8 loads are done; what
+  // this wave has read of K's stage b - 1 and V's b - 2 is read.
+  auto advance = [&](int b) {
+    wait_vm<8>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    const int nxt = page(b + kManyStages);
-    issue(b + kManyStages - 1, id);
-    id = nxt;
-    const int key = key0 + b * kManyKeys;
-    const uint32_t at = lds0 + (b % kManyStages) * kManyStage, vat = at + kManyStage / 2;
-    // absent pages of this block: a bit per 16 keys
-    uint32_t absent = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int k = key + 16 * i;
-      if (k < n && (uint32_t)page_uniform(p.c, t.s, k >> p.c.shift) >= (uint32_t)p.c.P) absent |= 1u << i;
-    }
-    if (key + kManyKeys > n || absent) {  // rows that are not there: V is cleared, a wave its 16
+    from_next = place(b + 3, id_next);
+    id_next = page(b + 4);
+    load_to_lds(mine + stage(b + 3), Kh + from_next, koff);
+    load_to_lds(mine + kVRing + stage(b + 2), Vh + from, voff);
+    from = from_next;
+  };
+
+  // Blocks that some query of the wave does not see whole: a half at a time, without overlap.
+  auto masked_block = [&](int b) {
+    const int key_b = key0 + b * kManyKeys;
+    advance(b);
+    if (key_b + kManyKeys > n || absent) {  // rows that are not there: V is cleared, a wave its 16
+      const bool in = there(key_b + 16 * wave);
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
         const int row = 16 * wave + 4 * y + (lane >> 4);
-        if (key + row >= n || ((absent >> wave) & 1))
-          *LDS_AT(u32x4, vat + row * kRowBytes + 16 * (lane & 15)) = (u32x4){0u, 0u, 0u, 0u};
+        if (key_b + row >= n || !in)
+          *LDS_AT(u32x4, lds0 + kVRing + stage(b) + row * kRowBytes + 16 * (lane & 15)) = (u32x4){0u, 0u, 0u, 0u};
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     }
-    if (key >= hi_max || key + kManyKeys <= lo_min) continue;  // none of the wave's rows sees the block
-    const bool masked = key < lo_max || key + kManyKeys > hi_min || absent;
-    // ---- S^T: two groups of 32 keys ----
-    f32x16 sc[2][2];
-#pragma unroll
-    for (int gk = 0; gk < 2; ++gk) {
+#pragma unroll 1
+    for (int hf = 0; hf < 2; ++hf) {
+      const int key = key_b + 32 * hf;
+      const uint32_t at = stage(b) + hf * kHalf;
+      scores(at, sa);
+      map_scores(sa, key);
+      const bool in0 = there(key), in1 = there(key + 16);
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[c][gk][e] = 0.0f;
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        const v8 kf = lds_v8<v8>(at + klane + (kswap ^ (32 * kk)) + 32 * gk * kRowBytes);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) sc[c][gk] = Mx<BF>::mfma32(kf, qf[c][kk], sc[c][gk]);
-      }
-    }
-    // ---- softmax ----
-    v8 pf[2][4];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      float mx = -__builtin_huge_valf();
-      if constexpr (MAPPED) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const int k = key + 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * half + (e & 3);
-          sc[c][e >> 4][e & 15] = mapped(sm[c], sc[c][e >> 4][e & 15], abs(pos[c] - k));
+        for (int e = 0; e < 16; ++e) {
+          const int k = key + 8 * (e >> 2) + 4 * half + (e & 3);
+          if (!(k >= lo[c] && k < hi[c] && (e < 8 ? in0 : in1))) sa[c][e] = -__builtin_huge_valf();
         }
+      float f[2];
+      if (raise(sa, f)) rescale(f);
+      exponentials(sa, pa);
+      if (!any_nonfinite<BF, kHalf>(lds0 + kVRing + at)) {
+        product(at, pa, std::false_type());
+        continue;
       }
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const int j = 32 * (e >> 4) + 8 * ((e & 15) >> 2) + 4 * half + (e & 3), k = key + j;
-          if (!(k >= lo[c] && k < hi[c] && !((absent >> (j >> 4)) & 1))) sc[c][e >> 4][e & 15] = -__builtin_huge_valf();
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sc[c][e >> 4][e & 15]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-      const float c1 = MAPPED ? 1.0f : sm[c].c1;
-      if (__ballot(mx > m[c])) {
-        const float mn = fmaxf(m[c], mx);
-        const float f = mn == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f((m[c] - mn) * c1);
-        m[c] = mn;
-        l[c] *= f;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) o[c][d] *= f;
-      }
-      const float ref = m[c] == -__builtin_huge_valf() ? 0.0f : m[c] * c1 - Mx<BF>::kShift;
-      float sum = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[c][e >> 4][e & 15], c1, -ref));
-        sum += x;
-        pf[c][e >> 3][e & 7] = (vt)x;
-      }
-      l[c] += sum;
-    }
-    // ---- O^T += V^T P^T: 32 channels, 16 keys at a time ----
-    const bool clean = masked && any_nonfinite<BF, kManyStage / 2>(vat);
-    if (clean) {
 #pragma unroll 1
-      for (int row = 0; row < kManyKeys; ++row) {
+      for (int row = 0; row < 32; ++row) {
         const int k = key + row;
-        const bool in = !((absent >> (row >> 4)) & 1);
+        const bool in = there(k);
 #pragma unroll
         for (int y = 0; y < 16; ++y) {  // channels 8 y + 4 half ..
-          const s16x4 x = *LDS_AT(const s16x4, vat + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
+          const s16x4 x = *LDS_AT(const s16x4, lds0 + kVRing + at + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -968,20 +1052,132 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
               if (in && k >= lo[c] && k < hi[c]) o[c][y >> 2][4 * (y & 3) + e] += nonfinite_part<BF>(x[e]);
         }
       }
+      product(at, pa, std::true_type());
     }
+  };
+
+  // A half step: the exponentials of `s` to P, the scores of the next half (K at byte `kat`) to
+  // `sn` and their maxima, the product of the last half (P in `pp`, V at byte `vat`).  16
+  // pieces of two matrix instructions with one LDS fragment, read two pieces ahead (the last
+  // two, in `ka` and `kb`, for the step after, K at `kafter`), and of two exponentials with
+  // what belongs to them: a wave alone on its SIMD issues about as long as the two matrix
+  // instructions run.
+  float neg_ref[2], above[2], mx[2];  // -maximum, the score that raises it, maxima of `sn` in the lane
+  auto reference = [&]() {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int c = 0; c < 2; ++c) {
+      neg_ref[c] = m[c] == -__builtin_huge_valf() ? 0.0f : Mx<BF>::kShift - m[c] * c1;
+      above[c] = m[c] + kSlack / c1;
+    }
+  };
+  auto k_frag = [&](uint32_t at, int kk) { return lds_v8<v8>(kaddr[kk] + at); };
+  auto v_frag = [&](uint32_t at, int j) {
+    const uint32_t va = vlane[j & 3] + at + 16 * (j >> 2) * kRowBytes;
+    return join4<v8>(lds_tr(va), lds_tr(va + 8 * kRowBytes));
+  };
+  auto half_step = [&](const f32x16 (&s)[2], u32x4 (&pr)[2][2], uint32_t kat, f32x16 (&sn)[2], int key_next, uint32_t vat,
+                       const u32x4 (&pp)[2][2], v8& ka, v8& kb, uint32_t kafter) {
+    v8 fr[18];
+    fr[0] = ka;
+    fr[1] = kb;
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const uint32_t va = vat + vlane[d] + 16 * i * kRowBytes;
-        s16x8 x = __builtin_shufflevector(lds_tr(va), lds_tr(va + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7);
-        if (clean) x = finite_part<BF>(x);
-        const v8 vf = __builtin_bit_cast(v8, x);
+    for (int j = 0; j < 16; ++j) {
+      fr[j + 2] = j < 6 ? k_frag(kat, j + 2) : j < 14 ? v_frag(vat, j - 6) : k_frag(kafter, j - 14);
+      const f32x16 zero = {};
 #pragma unroll
-        for (int c = 0; c < 2; ++c) o[c][d] = Mx<BF>::mfma32(vf, pf[c][i], o[c][d]);
+      for (int c = 0; c < 2; ++c) {
+        if (j < 8) sn[c] = Mx<BF>::mfma32(fr[j], qf[c][j], j == 0 ? zero : sn[c]);
+        else o[c][(j - 8) & 3] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[c][(j - 8) >> 2]), o[c][(j - 8) & 3]);
       }
+      const int c = j >> 3, e = 2 * (j & 7);
+      const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, neg_ref[c]));
+      const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, neg_ref[c]));
+      typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
+      l[c] = Mx<BF>::add_pair(pair, l[c]);
+      // pinned: the compiler would move it to where it is used, behind the branch
+      uint32_t word = __builtin_bit_cast(uint32_t, pair);
+      asm volatile("" : "+v"(word), "+v"(l[c]));
+      pr[c][e >> 3][(e & 7) >> 1] = word;
+      if (j >= 10) {  // the scores are complete: map, and the lane's maxima
+        constexpr int kFrom[7] = {0, 6, 12, 18, 24, 28, 32};
+#pragma unroll
+        for (int y = 0; y < 32; y += 2) {
+          if (y < kFrom[j - 10] || y >= kFrom[j - 9]) continue;
+          const int cc = y >> 4, ee = y & 15;
+          if constexpr (MAPPED) {
+#pragma unroll
+            for (int z = ee; z < ee + 2; ++z)
+              sn[cc][z] = mapped(sm[cc], sn[cc][z], abs(pos[cc] - (key_next + 8 * (z >> 2) + 4 * half + (z & 3))));
+          }
+          mx[cc] = ee == 0 ? fmaxf(sn[cc][0], sn[cc][1]) : fmaxf(fmaxf(mx[cc], sn[cc][ee]), sn[cc][ee + 1]);
+          asm volatile("" : "+v"(mx[cc]));
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
+    ka = fr[16];
+    kb = fr[17];
+  };
+  // Raises the maximum to that of both halves of the lanes, where one exceeds it by kSlack.
+  auto check = [&](float (&f)[2]) -> bool {
+    if (!__ballot(mx[0] > above[0] || mx[1] > above[1])) return false;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const float mn = fmaxf(m[c], fmaxf(mx[c], __shfl_xor(mx[c], 32, kWave)));
+      f[c] = mn == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f((m[c] - mn) * c1);
+      m[c] = mn;
+      l[c] *= f[c];
+    }
+    reference();
+    return true;
+  };
+
+  // Blocks [f0, f1) are seen whole by every query of the wave; f0 at stage 0 of the rings, so
+  // that the four copies of the loop know their stages.
+  const int f0 = absent ? nb : min((max((lo_max - key0 + kManyKeys - 1) / kManyKeys, 0) + 3) & ~3, nb);
+  const int f1 = max(f0, min((hi_min - key0) / kManyKeys, nb));
+  for (int b = 0; b < f0; ++b) masked_block(b);
+  if (f0 < f1) {
+    constexpr uint32_t kStage = kManyStage / 2;
+    float f[2];
+    const int key = key0 + f0 * kManyKeys;
+    advance(f0);
+    scores(0, sa);
+    map_scores(sa, key);
+    if (raise(sa, f)) rescale(f);
+    reference();
+    scores(kHalf, sb);
+    exponentials(sa, pa);
+    map_scores(sb, key + 32);
+    // where it is raised, the product that is still to come is in the old scale: O follows after it
+    bool up = raise(sb, f);
+    reference();
+    v8 ka = k_frag(kStage, 0), kb = k_frag(kStage, 1);
+    int b = f0;
+    auto block = [&](auto at) {  // second half of block b at stage `at`, first half of block b + 1
+      constexpr uint32_t s0 = decltype(at)::value * kStage, s1 = (decltype(at)::value + 1) % kManyStages * kStage;
+      half_step(sb, pb, s1, sa, key0 + (b + 1) * kManyKeys, s0, pa, ka, kb, s1 + kHalf);
+      if (up) rescale(f);
+      up = check(f);
+      advance(b + 1);
+      constexpr uint32_t s2 = (decltype(at)::value + 2) % kManyStages * kStage;
+      half_step(sa, pa, s1 + kHalf, sb, key0 + (b + 1) * kManyKeys + 32, s0 + kHalf, pb, ka, kb, s2);
+      if (up) rescale(f);
+      up = check(f);
+      ++b;
+      return b + 1 < f1;
+    };
+    if (b + 1 < f1)
+      while (block(std::integral_constant<int, 0>()) && block(std::integral_constant<int, 1>()) &&
+             block(std::integral_constant<int, 2>()) && block(std::integral_constant<int, 3>())) {
+      }
+    product(stage(f1 - 1), pa, std::false_type());
+    if (up) rescale(f);
+    exponentials(sb, pb);
+    product(stage(f1 - 1) + kHalf, pb, std::false_type());
   }
+  for (int b = f1; b < nb; ++b) masked_block(b);
+
   // ---- the output, or a part of it ----
   wait_vm<0>();
 #pragma unroll
@@ -1011,12 +1207,11 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
         for (int e = 0; e < 16; e += 4)
           *reinterpret_cast<f32x4*>(op + 32 * d + 2 * e) = (f32x4){o[c][d][e], o[c][d][e + 1], o[c][d][e + 2], o[c][d][e + 3]};
       if (half == 0) {
-        p.part_ml[pr * 2] = MAPPED ? m[c] : m[c] * sm[c].c1;
+        p.part_ml[pr * 2] = m[c] * c1;
         p.part_ml[pr * 2 + 1] = lt;
       }
     }
   }
-  if (flags && lane == 0) set_status(p.st, flags);
 }
 
 // The tiles whose keys were split, a workgroup 16 query rows.
