@@ -181,6 +181,15 @@ struct Mx<true> {
   }
 };
 
+// f(integral_constant<int, i>) for i = A .. B - 1: indices known to the compiler whatever a loop's size
+template <int A, int B, class Fn>
+__device__ __forceinline__ void static_for(Fn f) {
+  if constexpr (A < B) {
+    f(std::integral_constant<int, A>());
+    static_for<A + 1, B>(f);
+  }
+}
+
 template <class V8>
 __device__ __forceinline__ V8 lds_v8(uint32_t at) {
   return *LDS_AT(const V8, at);
@@ -230,23 +239,22 @@ __device__ __forceinline__ float nonfinite_part(short x) {
 
 // z in units of log2: the scaled score, capped, less the distance's bias.
 struct ScoreMap {
-  float c1;         // sm_scale log2e, or 2 log2e sm_scale / softcap
-  float cap;        // softcap log2e, 0: none
-  float slope;      // the row's slope times log2e
+  float c1;   // sm_scale log2e, or 2 log2e sm_scale / softcap
+  float cap;  // softcap log2e, 0: none
 };
-__device__ __forceinline__ float mapped(const ScoreMap& m, float s, int dist) {
+template <bool CAP>
+__device__ __forceinline__ float mapped(const ScoreMap& m, float slope, float s, int dist) {
   float z = s * m.c1;
-  if (m.cap != 0.0f) {  // tanh x = 1 - 2 / (e^2x + 1)
+  if constexpr (CAP) {  // tanh x = 1 - 2 / (e^2x + 1)
     const float t = __builtin_amdgcn_exp2f(z);
-    z = m.cap * (1.0f - 2.0f * __builtin_amdgcn_rcpf(t + 1.0f));
+    z = __builtin_fmaf(__builtin_amdgcn_rcpf(t + 1.0f), -2.0f * m.cap, m.cap);
   }
-  return z - m.slope * (float)dist;
+  return __builtin_fmaf(-slope, fabsf((float)dist), z);  // the row's slope times log2e
 }
-__device__ __forceinline__ ScoreMap score_map(const PagedAttnArgs& p, float slope) {
+__device__ __forceinline__ ScoreMap score_map(const PagedAttnArgs& p) {
   ScoreMap m;
   m.c1 = p.softcap > 0.0f ? 2.0f * kLog2e * (p.sm_scale / p.softcap) : p.sm_scale * kLog2e;
   m.cap = p.softcap > 0.0f ? p.softcap * kLog2e : 0.0f;
-  m.slope = slope * kLog2e;
   return m;
 }
 
@@ -331,6 +339,8 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
   if (flags && blockIdx.x == 0) set_status(p.st, flags);
   flags = 0;
   const int S = p.S, H = p.c.H, G = p.G;
+  const bool capped = p.softcap > 0.0f;
+  const ScoreMap sm = score_map(p);
   const int64_t W = (int64_t)before[S] * H;
   const int worker = uniform((int)blockIdx.x * kFewWaves + wave);
   const int64_t g0 = share(worker, W), g1 = share(worker + 1, W);
@@ -422,26 +432,25 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
     const int n = now.n, rows = uniform((int)(fixed(p.start, s + 1) - a)) * G, lo_key = now.lo;
     v8 qf[CT][4];
     int pos[CT], lo[CT], hi[CT], lo_max = 0, hi_min = n;
-    ScoreMap sm[CT];
+    float slope[CT];
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
       const int r = 16 * t + lr, tok = r / G, g = r - tok * G;
       pos[t] = 0;
       lo[t] = 0;
       hi[t] = n;
-      float slope = 0.0f;
+      slope[t] = 0.0f;
       s16x8 z = {};
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) qf[t][kk] = __builtin_bit_cast(v8, z);
       if (r < rows) {
         pos[t] = n - rows / G + tok;
         token_range(p, s, a + tok, pos[t], n, &lo[t], &hi[t]);
-        if (p.slopes) slope = p.slopes[h * G + g];
+        if (p.slopes) slope[t] = p.slopes[h * G + g] * kLog2e;
         const uint16_t* qp = p.q + (a + tok) * p.ldq_tok + (int64_t)(h * G + g) * p.ldq_head + 8 * quad;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) qf[t][kk] = *reinterpret_cast<const v8*>(qp + 32 * kk);
       }
-      sm[t] = score_map(p, slope);
       lo_max = max(lo_max, lo[t]);
       hi_min = min(hi_min, hi[t]);
     }
@@ -510,7 +519,8 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int k = key + 16 * (e >> 2) + 4 * quad + (e & 3);
-          z[e] = mapped(sm[t], sc[t][e >> 2][e & 3], abs(pos[t] - k));
+          z[e] = capped ? mapped<true>(sm, slope[t], sc[t][e >> 2][e & 3], pos[t] - k)
+                        : mapped<false>(sm, slope[t], sc[t][e >> 2][e & 3], pos[t] - k);
           if (masked) {
             if (!(k >= lo[t] && k < hi[t] && (e < 4 ? in0 : in1))) z[e] = -__builtin_huge_valf();
           }
@@ -772,7 +782,17 @@ __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int*
 // Mx::kShift leaves room for it in the probabilities), so the sums are rarely rescaled.
 constexpr float kSlack = 6.0f;
 
-template <bool BF, bool MAPPED>
+// A half's scores between two half steps: as the matrix instructions leave them, or, mapped,
+// as values of their own (values put back into an accumulator cost copies of all of it).
+struct Scores16 {
+  float v[16];
+  __device__ __forceinline__ float& operator[](int i) { return v[i]; }
+  __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+
+// MAP: 0 the scaled score, 1 with a bias (and for scales below 0), 2 capped.
+
+template <bool BF, int MAP>
 __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef typename Mx<BF>::v8 v8;
@@ -808,7 +828,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     if (absent && tid == 0) set_status(p.st, FATHOM_DEV_BAD_PAGE);
   }
   // whether key k's page is there
-  auto there = [&](int k) -> bool {
+  auto there = [&](int k) __attribute__((always_inline)) -> bool {
     return !absent || (uint32_t)page_of(p.c, t.s, min(k, n - 1) >> p.c.shift) < (uint32_t)p.c.P;
   };
 
@@ -823,16 +843,16 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   }
   // Where the wave's keys of block b begin in a pool; page 0 where there is none.
   const uint16_t *Kh = p.c.K + (int64_t)h * p.c.ld_head, *Vh = p.c.V + (int64_t)h * p.c.ld_head;
-  auto page = [&](int b) -> int {
+  auto page = [&](int b) __attribute__((always_inline)) -> int {
     const int k = key0 + b * kManyKeys + 16 * wave;
     return b < nb && k < n ? page_uniform(p.c, t.s, k >> p.c.shift) : 0;
   };
-  auto place = [&](int b, int id) -> int64_t {
+  auto place = [&](int b, int id) __attribute__((always_inline)) -> int64_t {
     const int k = key0 + b * kManyKeys + 16 * wave;
     return (int64_t)((uint32_t)id < (uint32_t)p.c.P ? id : 0) * p.c.ld_page +
            (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
   };
-  auto stage = [](int b) -> uint32_t { return (uint32_t)(b % kManyStages) * (kManyStage / 2); };
+  auto stage = [](int b) __attribute__((always_inline)) -> uint32_t { return (uint32_t)(b % kManyStages) * (kManyStage / 2); };
   constexpr uint32_t kVRing = kManyStages * (kManyStage / 2);  // V's stages behind K's
   const uint32_t mine = lds0 + wave * 4096;
   // K runs three blocks ahead of what is in use, V two: a block's V is read half a block
@@ -850,14 +870,15 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   // ---- the wave's 64 query rows: column tiles of 32 ----
   v8 qf[2][8];
   int pos[2], lo[2], hi[2], lo_max = 0, hi_min = n;
-  ScoreMap sm[2];
+  float slope[2];
+  const ScoreMap sm = score_map(p);
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
     const int r = wave * 64 + c * 32 + lr, tok = r / G, g = r - tok * G;
     pos[c] = 0;
     lo[c] = 0;
     hi[c] = n;
-    float slope = 0.0f;
+    slope[c] = 0.0f;
     s16x8 z = {};
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) qf[c][kk] = __builtin_bit_cast(v8, z);
@@ -865,14 +886,13 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
       const int64_t row = t.a + t.tok0 + tok;
       pos[c] = n - total + t.tok0 + tok;
       token_range(p, t.s, row, pos[c], n, &lo[c], &hi[c]);
-      if (p.slopes) slope = p.slopes[h * G + g];
+      if (p.slopes) slope[c] = p.slopes[h * G + g] * kLog2e;
       const uint16_t* qp = p.q + row * p.ldq_tok + (int64_t)(h * G + g) * p.ldq_head + 8 * half;
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) qf[c][kk] = *reinterpret_cast<const v8*>(qp + 16 * kk);
       lo_max = max(lo_max, lo[c]);
-      hi_min = min(hi_min, hi[c]);
+      hi_min = min(hi_min, MAP != 0 ? min(hi[c], pos[c] + 1) : hi[c]);  // (map_seen)
     }
-    sm[c] = score_map(p, slope);
   }
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) {
@@ -881,27 +901,28 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   }
   lo_max = uniform(lo_max);
   hi_min = uniform(hi_min);
-  const float c1 = MAPPED ? 1.0f : sm[0].c1;
+  const float c1 = MAP != 0 ? 1.0f : sm.c1;
 
-  // LDS places of a lane's part of K fragments (of key lr, channels 16 kk + 8 half ..: chunk
-  // 2 kk + half, permuted) and of V^T fragments (groups of 16 lanes name channels 0..15 and
-  // 16..31 of 32 and keys 4 half ..)
-  uint32_t kaddr[8], vlane[4];
-#pragma unroll
-  for (int kk = 0; kk < 8; ++kk) kaddr[kk] = lds0 + lr * kRowBytes + 16 * k_chunk(lr, 2 * kk + half);
-#pragma unroll
-  for (int d = 0; d < 4; ++d) {
-    const int r0 = 4 * half + ((lane & 15) >> 2), ch = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    vlane[d] = lds0 + kVRing + r0 * kRowBytes + 16 * v_chunk(r0, ch) + 8 * (lane & 1);
+  // LDS places of a lane's part of K fragments (of key lr, channels 8 half ..: chunk
+  // `half`, permuted) and of V^T fragments (groups of 16 lanes name channels 0..15 and 16..31
+  // and keys 4 half ..); channels 16 kk and 32 d on, the chunk differs in bits of its own
+  uint32_t kaddr = lds0 + lr * kRowBytes + 16 * k_chunk(lr, half), vaddr;
+  {
+    const int r0 = 4 * half + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    vaddr = lds0 + kVRing + r0 * kRowBytes + 16 * v_chunk(r0, ch) + 8 * (lane & 1);
   }
   constexpr uint32_t kHalf = 32 * kRowBytes;
 
-  f32x16 o[2][4], sa[2], sb[2];
+  typedef std::conditional_t<MAP == 0, f32x16, Scores16> Sv;
+  f32x16 o[2][4];
+  Sv sa[2], sb[2];
   u32x4 pa[2][2], pb[2][2];
-  float m[2], l[2];
+  // l: sums of the probabilities; nr: kShift less the reference that they are taken against (in
+  // log2; at first a reference that every score raises and against which -Inf gives 0)
+  float nr[2], l[2];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    m[c] = -__builtin_huge_valf();
+    nr[c] = 1e37f;
     l[c] = 0.0f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -909,25 +930,26 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
       for (int e = 0; e < 16; ++e) o[c][d][e] = 0.0f;
   }
   // S^T of the 32 keys at byte `at` of K's ring
-  auto scores = [&](uint32_t at, f32x16 (&s)[2]) {
+  auto scores = [&](uint32_t at, Sv (&s)[2]) __attribute__((always_inline)) {
+    f32x16 acc[2] = {};
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const v8 kf = lds_v8<v8>((kaddr ^ (32 * kk)) + at);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) acc[c] = Mx<BF>::mfma32(kf, qf[c][kk], acc[c]);
+    }
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[c][e] = 0.0f;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      const v8 kf = lds_v8<v8>(kaddr[kk] + at);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) s[c] = Mx<BF>::mfma32(kf, qf[c][kk], s[c]);
-    }
+      for (int e = 0; e < 16; ++e) s[c][e] = acc[c][e];
   };
   // O^T += V^T P^T of the 32 keys at byte `at` of V's ring
-  auto product = [&](uint32_t at, const u32x4 (&pr)[2][2], auto clean) {
+  auto product = [&](uint32_t at, const u32x4 (&pr)[2][2], auto clean) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const uint32_t va = vlane[d] + at + 16 * i * kRowBytes;
+        const uint32_t va = (vaddr ^ (64 * d)) + at + 16 * i * kRowBytes;
         s16x8 x = __builtin_shufflevector(lds_tr(va), lds_tr(va + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7);
         if constexpr (decltype(clean)::value) x = finite_part<BF>(x);
         const v8 vf = __builtin_bit_cast(v8, x);
@@ -935,53 +957,70 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
         for (int c = 0; c < 2; ++c) o[c][d] = Mx<BF>::mfma32(vf, __builtin_bit_cast(v8, pr[c][i]), o[c][d]);
       }
   };
-  auto exponentials = [&](const f32x16 (&s)[2], u32x4 (&pr)[2][2]) {
+  auto exponentials = [&](const Sv (&s)[2], u32x4 (&pr)[2][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const float neg = m[c] == -__builtin_huge_valf() ? 0.0f : Mx<BF>::kShift - m[c] * c1;
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, neg));
-        const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, neg));
+        const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
+        const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, nr[c]));
         const typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
         l[c] = Mx<BF>::add_pair(pair, l[c]);
         pr[c][e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, pair);
       }
     }
   };
-  auto map_scores = [&](f32x16 (&s)[2], int key) {
-    if constexpr (MAPPED) {
+  auto map_scores = [&](Sv (&s)[2], int key) __attribute__((always_inline)) {
+    if constexpr (MAP != 0) {
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          s[c][e] = mapped(sm[c], s[c][e], abs(pos[c] - (key + 8 * (e >> 2) + 4 * half + (e & 3))));
+          s[c][e] = mapped<MAP == 2>(sm, slope[c], s[c][e], pos[c] - 4 * half - (key + 8 * (e >> 2) + (e & 3)));
     }
   };
-  // The maximum of a half's scores: where it is raised, the sums' factor in f (and true).
-  auto raise = [&](const f32x16 (&s)[2], float (&f)[2]) -> bool {
-    float mx[2];
-    bool up = false;
+  // The same of element e, for keys up to the row's own: the bias is linear in the key.
+  auto bias_base = [&](int c, int key) __attribute__((always_inline)) { return slope[c] * (float)(key + 4 * half - pos[c]); };
+  auto map_seen = [&](float s, int c, int e, float base) __attribute__((always_inline)) -> float {
+    const float bias = __builtin_fmaf(slope[c], (float)(8 * (e >> 2) + (e & 3)), base);
+    if constexpr (MAP == 1) return __builtin_fmaf(s, sm.c1, bias);
+    return mapped<true>(sm, 0.0f, s, 0) + bias;
+  };
+  auto map_half = [&](Sv (&s)[2], int key) __attribute__((always_inline)) {
+    if constexpr (MAP != 0) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[c][e] = map_seen(s[c][e], c, e, bias_base(c, key));
+    }
+  };
+  float mx[2];  // the lane's maxima of a half's scores
+  auto maxima = [&](const Sv (&s)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       mx[c] = fmaxf(s[c][0], s[c][1]);
 #pragma unroll
       for (int e = 2; e < 16; e += 2) mx[c] = fmaxf(fmaxf(mx[c], s[c][e]), s[c][e + 1]);
-      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx[c]), __float_as_uint(mx[c]), false, false);
-      mx[c] = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-      up |= (mx[c] - m[c]) * c1 > kSlack;  // -Inf less -Inf is no reason
     }
+  };
+  // Where one exceeds the reference by kSlack: the reference becomes the maximum of the row's
+  // scores, l follows, and f is the factor for O.
+  auto raise = [&](float (&f)[2]) __attribute__((always_inline)) -> bool {
+    bool up = false;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) up |= __builtin_fmaf(mx[c], c1, nr[c]) > kSlack + Mx<BF>::kShift;
     if (!__ballot(up)) return false;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const float mn = fmaxf(m[c], mx[c]);
-      f[c] = mn == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f((m[c] - mn) * c1);
-      m[c] = mn;
+      const float top = fmaxf(mx[c], __shfl_xor(mx[c], 32, kWave));
+      const float to = fminf(nr[c], Mx<BF>::kShift - top * c1);
+      f[c] = __builtin_amdgcn_exp2f(to - nr[c]);
+      nr[c] = to;
       l[c] *= f[c];
     }
     return true;
   };
-  auto rescale = [&](const float (&f)[2]) {
+  auto rescale = [&](const float (&f)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -989,7 +1028,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   };
   // K of block b + 1 and V of block b are in LDS once all but the last 8 loads are done; what
   // this wave has read of K's stage b - 1 and V's b - 2 is read.
-  auto advance = [&](int b) {
+  auto advance = [&](int b) __attribute__((always_inline)) {
     wait_vm<8>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -1002,7 +1041,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   };
 
   // Blocks that some query of the wave does not see whole: a half at a time, without overlap.
-  auto masked_block = [&](int b) {
+  auto masked_block = [&](int b) __attribute__((always_inline)) {
     const int key_b = key0 + b * kManyKeys;
     advance(b);
     if (key_b + kManyKeys > n || absent) {  // rows that are not there: V is cleared, a wave its 16
@@ -1032,7 +1071,8 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
           if (!(k >= lo[c] && k < hi[c] && (e < 8 ? in0 : in1))) sa[c][e] = -__builtin_huge_valf();
         }
       float f[2];
-      if (raise(sa, f)) rescale(f);
+      maxima(sa);
+      if (raise(f)) rescale(f);
       exponentials(sa, pa);
       if (!any_nonfinite<BF, kHalf>(lds0 + kVRing + at)) {
         product(at, pa, std::false_type());
@@ -1062,76 +1102,68 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   // two, in `ka` and `kb`, for the step after, K at `kafter`), and of two exponentials with
   // what belongs to them: a wave alone on its SIMD issues about as long as the two matrix
   // instructions run.
-  float neg_ref[2], above[2], mx[2];  // -maximum, the score that raises it, maxima of `sn` in the lane
-  auto reference = [&]() {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      neg_ref[c] = m[c] == -__builtin_huge_valf() ? 0.0f : Mx<BF>::kShift - m[c] * c1;
-      above[c] = m[c] + kSlack / c1;
-    }
-  };
-  auto k_frag = [&](uint32_t at, int kk) { return lds_v8<v8>(kaddr[kk] + at); };
-  auto v_frag = [&](uint32_t at, int j) {
-    const uint32_t va = vlane[j & 3] + at + 16 * (j >> 2) * kRowBytes;
+  auto k_frag = [&](uint32_t at, int kk) __attribute__((always_inline)) { return lds_v8<v8>((kaddr ^ (32 * kk)) + at); };
+  auto v_frag = [&](uint32_t at, int j) __attribute__((always_inline)) {
+    const uint32_t va = (vaddr ^ (64 * (j & 3))) + at + 16 * (j >> 2) * kRowBytes;
     return join4<v8>(lds_tr(va), lds_tr(va + 8 * kRowBytes));
   };
-  auto half_step = [&](const f32x16 (&s)[2], u32x4 (&pr)[2][2], uint32_t kat, f32x16 (&sn)[2], int key_next, uint32_t vat,
-                       const u32x4 (&pp)[2][2], v8& ka, v8& kb, uint32_t kafter) {
+  auto half_step = [&](const Sv (&s)[2], u32x4 (&pr)[2][2], uint32_t kat, Sv (&sn)[2], int key_next, uint32_t vat,
+                       const u32x4 (&pp)[2][2], v8& ka, v8& kb, uint32_t kafter) __attribute__((always_inline)) {
     v8 fr[18];
+    f32x16 acc[2];
+    float base = 0.0f;
+    asm volatile("" : "+v"(kaddr), "+v"(vaddr));  // (else twelve addresses stay in registers)
     fr[0] = ka;
     fr[1] = kb;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      fr[j + 2] = j < 6 ? k_frag(kat, j + 2) : j < 14 ? v_frag(vat, j - 6) : k_frag(kafter, j - 14);
+    static_for<0, 16>([&](auto piece) __attribute__((always_inline)) {
+      constexpr int j = decltype(piece)::value;
+      if constexpr (j < 6) fr[j + 2] = k_frag(kat, j + 2);
+      else if constexpr (j < 14) fr[j + 2] = v_frag(vat, j - 6);
+      else fr[j + 2] = k_frag(kafter, j - 14);
       const f32x16 zero = {};
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        if (j < 8) sn[c] = Mx<BF>::mfma32(fr[j], qf[c][j], j == 0 ? zero : sn[c]);
-        else o[c][(j - 8) & 3] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[c][(j - 8) >> 2]), o[c][(j - 8) & 3]);
+        if constexpr (j < 8) {
+          acc[c] = Mx<BF>::mfma32(fr[j], qf[c][j], j == 0 ? zero : acc[c]);
+        } else {
+          constexpr int i = (j - 8) >> 2, d = j & 3;
+          o[c][d] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[c][i]), o[c][d]);
+        }
       }
-      const int c = j >> 3, e = 2 * (j & 7);
-      const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, neg_ref[c]));
-      const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, neg_ref[c]));
-      typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
+      constexpr int c = j >> 3, e = 2 * (j & 7);
+      const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
+      const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, nr[c]));
+      const typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
       l[c] = Mx<BF>::add_pair(pair, l[c]);
       // pinned: the compiler would move it to where it is used, behind the branch
       uint32_t word = __builtin_bit_cast(uint32_t, pair);
       asm volatile("" : "+v"(word), "+v"(l[c]));
       pr[c][e >> 3][(e & 7) >> 1] = word;
-      if (j >= 10) {  // the scores are complete: map, and the lane's maxima
+      if constexpr (j >= 10) {  // the scores are complete: map, and the lane's maxima
         constexpr int kFrom[7] = {0, 6, 12, 18, 24, 28, 32};
-#pragma unroll
-        for (int y = 0; y < 32; y += 2) {
-          if (y < kFrom[j - 10] || y >= kFrom[j - 9]) continue;
-          const int cc = y >> 4, ee = y & 15;
-          if constexpr (MAPPED) {
-#pragma unroll
-            for (int z = ee; z < ee + 2; ++z)
-              sn[cc][z] = mapped(sm[cc], sn[cc][z], abs(pos[cc] - (key_next + 8 * (z >> 2) + 4 * half + (z & 3))));
+        static_for<kFrom[j - 10] / 2, kFrom[j - 9] / 2>([&](auto two) __attribute__((always_inline)) {
+          constexpr int cc = decltype(two)::value >> 3, ee = 2 * (decltype(two)::value & 7);
+          if constexpr (MAP == 0) {
+            mx[cc] = ee == 0 ? fmaxf(acc[cc][0], acc[cc][1]) : fmaxf(fmaxf(mx[cc], acc[cc][ee]), acc[cc][ee + 1]);
+          } else {
+            if constexpr (ee == 0) base = bias_base(cc, key_next);
+            const float z0 = map_seen(acc[cc][ee], cc, ee, base), z1 = map_seen(acc[cc][ee + 1], cc, ee + 1, base);
+            sn[cc][ee] = z0;
+            sn[cc][ee + 1] = z1;
+            mx[cc] = ee == 0 ? fmaxf(z0, z1) : fmaxf(fmaxf(mx[cc], z0), z1);
           }
-          mx[cc] = ee == 0 ? fmaxf(sn[cc][0], sn[cc][1]) : fmaxf(fmaxf(mx[cc], sn[cc][ee]), sn[cc][ee + 1]);
           asm volatile("" : "+v"(mx[cc]));
-        }
+        });
       }
       __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (MAP == 0) {
+      sn[0] = acc[0];
+      sn[1] = acc[1];
     }
     ka = fr[16];
     kb = fr[17];
   };
-  // Raises the maximum to that of both halves of the lanes, where one exceeds it by kSlack.
-  auto check = [&](float (&f)[2]) -> bool {
-    if (!__ballot(mx[0] > above[0] || mx[1] > above[1])) return false;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const float mn = fmaxf(m[c], fmaxf(mx[c], __shfl_xor(mx[c], 32, kWave)));
-      f[c] = mn == -__builtin_huge_valf() ? 1.0f : __builtin_amdgcn_exp2f((m[c] - mn) * c1);
-      m[c] = mn;
-      l[c] *= f[c];
-    }
-    reference();
-    return true;
-  };
-
   // Blocks [f0, f1) are seen whole by every query of the wave; f0 at stage 0 of the rings, so
   // that the four copies of the loop know their stages.
   const int f0 = absent ? nb : min((max((lo_max - key0 + kManyKeys - 1) / kManyKeys, 0) + 3) & ~3, nb);
@@ -1143,27 +1175,27 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     const int key = key0 + f0 * kManyKeys;
     advance(f0);
     scores(0, sa);
-    map_scores(sa, key);
-    if (raise(sa, f)) rescale(f);
-    reference();
+    map_half(sa, key);
+    maxima(sa);
+    if (raise(f)) rescale(f);
     scores(kHalf, sb);
     exponentials(sa, pa);
-    map_scores(sb, key + 32);
+    map_half(sb, key + 32);
     // where it is raised, the product that is still to come is in the old scale: O follows after it
-    bool up = raise(sb, f);
-    reference();
+    maxima(sb);
+    bool up = raise(f);
     v8 ka = k_frag(kStage, 0), kb = k_frag(kStage, 1);
     int b = f0;
-    auto block = [&](auto at) {  // second half of block b at stage `at`, first half of block b + 1
+    auto block = [&](auto at) __attribute__((always_inline)) {  // second half of block b at stage `at`, first half of block b + 1
       constexpr uint32_t s0 = decltype(at)::value * kStage, s1 = (decltype(at)::value + 1) % kManyStages * kStage;
       half_step(sb, pb, s1, sa, key0 + (b + 1) * kManyKeys, s0, pa, ka, kb, s1 + kHalf);
       if (up) rescale(f);
-      up = check(f);
+      up = raise(f);
       advance(b + 1);
       constexpr uint32_t s2 = (decltype(at)::value + 2) % kManyStages * kStage;
       half_step(sa, pa, s1 + kHalf, sb, key0 + (b + 1) * kManyKeys + 32, s0 + kHalf, pb, ka, kb, s2);
       if (up) rescale(f);
-      up = check(f);
+      up = raise(f);
       ++b;
       return b + 1 < f1;
     };
@@ -1207,7 +1239,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
         for (int e = 0; e < 16; e += 4)
           *reinterpret_cast<f32x4*>(op + 32 * d + 2 * e) = (f32x4){o[c][d][e], o[c][d][e + 1], o[c][d][e + 2], o[c][d][e + 3]};
       if (half == 0) {
-        p.part_ml[pr * 2] = m[c] * c1;
+        p.part_ml[pr * 2] = Mx<BF>::kShift - nr[c];
         p.part_ml[pr * 2 + 1] = lt;
       }
     }
@@ -1306,10 +1338,9 @@ static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) 
   if (a.run_many) {
     const dim3 grid((unsigned)(a.tiles * a.nsplit * p.c.H));
     const size_t lds = (size_t)kManyStages * kManyStage + plan;
-    if (p.softcap > 0.0f || p.slopes || !(p.sm_scale > 0.0f))
-      hipLaunchKernelGGL((attn_many_kernel<BF, true>), grid, dim3(256), lds, s, p);
-    else
-      hipLaunchKernelGGL((attn_many_kernel<BF, false>), grid, dim3(256), lds, s, p);
+    if (p.softcap > 0.0f) hipLaunchKernelGGL((attn_many_kernel<BF, 2>), grid, dim3(256), lds, s, p);
+    else if (p.slopes || !(p.sm_scale > 0.0f)) hipLaunchKernelGGL((attn_many_kernel<BF, 1>), grid, dim3(256), lds, s, p);
+    else hipLaunchKernelGGL((attn_many_kernel<BF, 0>), grid, dim3(256), lds, s, p);
     if (a.nsplit > 1)
       hipLaunchKernelGGL((attn_many_join_kernel<BF>), dim3((unsigned)(a.tiles * p.c.H), kManyRows / kManyJoin),
                          dim3(256), plan, s, p);
