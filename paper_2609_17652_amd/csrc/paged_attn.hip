@@ -739,12 +739,13 @@ __device__ __forceinline__ void many_plan(const PagedAttnArgs& p, int* before, i
 __device__ __forceinline__ int parts_of(int nb, int nsplit) { return max(min(nsplit, nb / 4), 1); }
 
 struct ManyTile {
-  int s, h, tok0, toks, n, lo, hi;  // tokens of the tile and the union of their ranges
+  int s, h, tok0, toks, total, n;  // tokens of the tile and of the request, new and all
+  int lo, hi, lo_max;              // the union of their ranges, the largest first position
   int64_t a;
 };
 
 // Tile and head of a workgroup index (later tiles, which see more, first).  Every thread of
-// 256; red[8] is LDS.
+// 256; red[12] is LDS.
 __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int* before, int tile, int h, int* red) {
   ManyTile t;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tm = kManyRows / p.G;
@@ -753,23 +754,34 @@ __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int*
   t.h = h;
   t.a = fixed(p.start, t.s);
   t.n = uniform((int)fixed(p.n, t.s));
-  const int total = uniform((int)(fixed(p.start, t.s + 1) - t.a));
+  t.total = uniform((int)(fixed(p.start, t.s + 1) - t.a));
   t.tok0 = (x - uniform(before[t.s])) * tm;
-  t.toks = min(tm, total - t.tok0);
-  int lo = t.n, hi = 0;
-  if (tid < t.toks) token_range(p, t.s, t.a + t.tok0 + tid, t.n - total + t.tok0 + tid, t.n, &lo, &hi);
+  t.toks = min(tm, t.total - t.tok0);
+  if (!p.first && !p.prefix) {
+    t.lo = t.lo_max = 0;
+    t.hi = t.n - t.total + t.tok0 + t.toks;
+    return t;
+  }
+  int lo = t.n, hi = 0, lo_max = 0;
+  if (tid < t.toks) {
+    token_range(p, t.s, t.a + t.tok0 + tid, t.n - t.total + t.tok0 + tid, t.n, &lo, &hi);
+    lo_max = lo;
+  }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     lo = min(lo, __shfl_xor(lo, o, kWave));
     hi = max(hi, __shfl_xor(hi, o, kWave));
+    lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
   }
   if (lane == 0) {
     red[wave] = lo;
     red[4 + wave] = hi;
+    red[8 + wave] = lo_max;
   }
   __syncthreads();
   t.lo = uniform(min(min(red[0], red[1]), min(red[2], red[3]))) & ~(kManyKeys - 1);
   t.hi = uniform(max(max(red[4], red[5]), max(red[6], red[7])));
+  t.lo_max = uniform(max(max(red[8], red[9]), max(red[10], red[11])));
   __syncthreads();
   return t;
 }
@@ -812,21 +824,9 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   const int b0 = (int)((int64_t)all * part / parts), nb = (int)((int64_t)all * (part + 1) / parts) - b0;
   const int key0 = t.lo + b0 * kManyKeys, n = t.n;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))smem;
-  const int total = uniform((int)(fixed(p.start, t.s + 1) - t.a)), rows = t.toks * G;
+  const int rows = t.toks * G;
 
-  // ---- absent pages among the keys: their blocks are masked throughout ----
   bool absent = false;
-  {
-    const int e1 = min(key0 + nb * kManyKeys, n);
-    for (int k = key0 + 16 * tid; k < e1; k += 16 * 256)
-      absent |= (uint32_t)page_of(p.c, t.s, k >> p.c.shift) >= (uint32_t)p.c.P;
-    if (lane == 0) red[wave] = 0;
-    const bool any = __ballot(absent) != 0;
-    if (lane == 0) red[wave] = any;
-    __syncthreads();
-    absent = uniform(red[0] | red[1] | red[2] | red[3]) != 0;
-    if (absent && tid == 0) set_status(p.st, FATHOM_DEV_BAD_PAGE);
-  }
   // whether key k's page is there
   auto there = [&](int k) __attribute__((always_inline)) -> bool {
     return !absent || (uint32_t)page_of(p.c, t.s, min(k, n - 1) >> p.c.shift) < (uint32_t)p.c.P;
@@ -852,7 +852,12 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     return (int64_t)((uint32_t)id < (uint32_t)p.c.P ? id : 0) * p.c.ld_page +
            (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
   };
-  auto stage = [](int b) __attribute__((always_inline)) -> uint32_t { return (uint32_t)(b % kManyStages) * (kManyStage / 2); };
+  // Blocks [f0, ..) have no key before a query's first; f0 is at stage 0 of the rings, so that
+  // the four copies of the loop below know their stages.
+  const int f0 = min(max((t.lo_max - key0 + kManyKeys - 1) / kManyKeys, 0), nb), phase = -f0 & (kManyStages - 1);
+  auto stage = [&](int b) __attribute__((always_inline)) -> uint32_t {
+    return (uint32_t)((b + phase) % kManyStages) * (kManyStage / 2);
+  };
   constexpr uint32_t kVRing = kManyStages * (kManyStage / 2);  // V's stages behind K's
   const uint32_t mine = lds0 + wave * 4096;
   // K runs three blocks ahead of what is in use, V two: a block's V is read half a block
@@ -869,7 +874,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
 
   // ---- the wave's 64 query rows: column tiles of 32 ----
   v8 qf[2][8];
-  int pos[2], lo[2], hi[2], lo_max = 0, hi_min = n;
+  int pos[2], lo[2], hi[2], hi_min = n;
   float slope[2];
   const ScoreMap sm = score_map(p);
 #pragma unroll
@@ -884,23 +889,34 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     for (int kk = 0; kk < 8; ++kk) qf[c][kk] = __builtin_bit_cast(v8, z);
     if (r < rows) {
       const int64_t row = t.a + t.tok0 + tok;
-      pos[c] = n - total + t.tok0 + tok;
+      pos[c] = n - t.total + t.tok0 + tok;
       token_range(p, t.s, row, pos[c], n, &lo[c], &hi[c]);
       if (p.slopes) slope[c] = p.slopes[h * G + g] * kLog2e;
       const uint16_t* qp = p.q + row * p.ldq_tok + (int64_t)(h * G + g) * p.ldq_head + 8 * half;
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) qf[c][kk] = *reinterpret_cast<const v8*>(qp + 16 * kk);
-      lo_max = max(lo_max, lo[c]);
       hi_min = min(hi_min, MAP != 0 ? min(hi[c], pos[c] + 1) : hi[c]);  // (map_seen)
     }
   }
+  if (!p.prefix) {  // the wave's first token
+    hi_min = wave * 64 < rows ? n - t.total + t.tok0 + wave * 64 / G + 1 : n;
+  } else {
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) {
-    lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
-    hi_min = min(hi_min, __shfl_xor(hi_min, o, kWave));
+    for (int o = 16; o >= 1; o >>= 1) hi_min = min(hi_min, __shfl_xor(hi_min, o, kWave));
+    hi_min = uniform(hi_min);
   }
-  lo_max = uniform(lo_max);
-  hi_min = uniform(hi_min);
+  // ---- absent pages among the keys: their blocks are masked throughout ----
+  {
+    const int e1 = min(key0 + nb * kManyKeys, n);
+    for (int k = key0 + 16 * tid; k < e1; k += 16 * 256)
+      absent |= (uint32_t)page_of(p.c, t.s, k >> p.c.shift) >= (uint32_t)p.c.P;
+    if (lane == 0) red[wave] = 0;
+    const bool any = __ballot(absent) != 0;
+    if (lane == 0) red[wave] = any;
+    __syncthreads();
+    absent = uniform(red[0] | red[1] | red[2] | red[3]) != 0;
+    if (absent && tid == 0) set_status(p.st, FATHOM_DEV_BAD_PAGE);
+  }
   const float c1 = MAP != 0 ? 1.0f : sm.c1;
 
   // LDS places of a lane's part of K fragments (of key lr, channels 8 half ..: chunk
@@ -1115,33 +1131,13 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     asm volatile("" : "+v"(kaddr), "+v"(vaddr));  // (else twelve addresses stay in registers)
     fr[0] = ka;
     fr[1] = kb;
-    static_for<0, 16>([&](auto piece) __attribute__((always_inline)) {
-      constexpr int j = decltype(piece)::value;
-      if constexpr (j < 6) fr[j + 2] = k_frag(kat, j + 2);
-      else if constexpr (j < 14) fr[j + 2] = v_frag(vat, j - 6);
-      else fr[j + 2] = k_frag(kafter, j - 14);
-      const f32x16 zero = {};
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        if constexpr (j < 8) {
-          acc[c] = Mx<BF>::mfma32(fr[j], qf[c][j], j == 0 ? zero : acc[c]);
-        } else {
-          constexpr int i = (j - 8) >> 2, d = j & 3;
-          o[c][d] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[c][i]), o[c][d]);
-        }
-      }
-      constexpr int c = j >> 3, e = 2 * (j & 7);
-      const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
-      const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, nr[c]));
-      const typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
-      l[c] = Mx<BF>::add_pair(pair, l[c]);
-      // pinned: the compiler would move it to where it is used, behind the branch
-      uint32_t word = __builtin_bit_cast(uint32_t, pair);
-      asm volatile("" : "+v"(word), "+v"(l[c]));
-      pr[c][e >> 3][(e & 7) >> 1] = word;
-      if constexpr (j >= 10) {  // the scores are complete: map, and the lane's maxima
-        constexpr int kFrom[7] = {0, 6, 12, 18, 24, 28, 32};
-        static_for<kFrom[j - 10] / 2, kFrom[j - 9] / 2>([&](auto two) __attribute__((always_inline)) {
+    // once the scores are complete, from the 20th of 32 matrix instructions on: map them, and
+    // the lane's maxima, a pair or two at a time
+    auto last_max = [&](auto place) __attribute__((always_inline)) {
+      constexpr int at = decltype(place)::value - 20;
+      if constexpr (at >= 0) {
+        constexpr int first = at < 8 ? at : 8 + 2 * (at - 8), last = at < 8 ? at + 1 : first + 2;
+        static_for<first, last>([&](auto two) __attribute__((always_inline)) {
           constexpr int cc = decltype(two)::value >> 3, ee = 2 * (decltype(two)::value & 7);
           if constexpr (MAP == 0) {
             mx[cc] = ee == 0 ? fmaxf(acc[cc][0], acc[cc][1]) : fmaxf(fmaxf(mx[cc], acc[cc][ee]), acc[cc][ee + 1]);
@@ -1155,6 +1151,29 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
           asm volatile("" : "+v"(mx[cc]));
         });
       }
+    };
+    static_for<0, 16>([&](auto piece) __attribute__((always_inline)) {
+      constexpr int j = decltype(piece)::value;
+      if constexpr (j < 6) fr[j + 2] = k_frag(kat, j + 2);
+      else if constexpr (j < 14) fr[j + 2] = v_frag(vat, j - 6);
+      else fr[j + 2] = k_frag(kafter, j - 14);
+      constexpr int c = j >> 3, e = 2 * (j & 7), i = (j - 8) >> 2, d = j & 3;
+      const f32x16 zero = {};
+      if constexpr (j < 8) acc[0] = Mx<BF>::mfma32(fr[j], qf[0][j], j == 0 ? zero : acc[0]);
+      else o[0][d] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[0][i]), o[0][d]);
+      const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
+      last_max(std::integral_constant<int, 2 * j>());
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (j < 8) acc[1] = Mx<BF>::mfma32(fr[j], qf[1][j], j == 0 ? zero : acc[1]);
+      else o[1][d] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[1][i]), o[1][d]);
+      const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, nr[c]));
+      const typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
+      l[c] = Mx<BF>::add_pair(pair, l[c]);
+      // pinned: the compiler would move it to where it is used, behind the branch
+      uint32_t word = __builtin_bit_cast(uint32_t, pair);
+      asm volatile("" : "+v"(word), "+v"(l[c]));
+      pr[c][e >> 3][(e & 7) >> 1] = word;
+      last_max(std::integral_constant<int, 2 * j + 1>());
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (MAP == 0) {
@@ -1164,10 +1183,8 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     ka = fr[16];
     kb = fr[17];
   };
-  // Blocks [f0, f1) are seen whole by every query of the wave; f0 at stage 0 of the rings, so
-  // that the four copies of the loop know their stages.
-  const int f0 = absent ? nb : min((max((lo_max - key0 + kManyKeys - 1) / kManyKeys, 0) + 3) & ~3, nb);
-  const int f1 = max(f0, min((hi_min - key0) / kManyKeys, nb));
+  // Blocks [f0, f1) are seen whole by every query of the wave.
+  const int f1 = absent ? f0 : max(f0, min((hi_min - key0) / kManyKeys, nb));
   for (int b = 0; b < f0; ++b) masked_block(b);
   if (f0 < f1) {
     constexpr uint32_t kStage = kManyStage / 2;
@@ -1331,7 +1348,7 @@ size_t paged_attn_ws_bytes(int64_t T, int S, int H, int G, int64_t max_new) {
 
 template <bool BF>
 static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) {
-  const size_t plan = (size_t)(p.S + 1 + 8) * sizeof(int);
+  const size_t plan = (size_t)(p.S + 1 + 12) * sizeof(int);
   p.tiles = (int)a.tiles;
   p.nsplit = a.nsplit;
   p.few = a.few;
