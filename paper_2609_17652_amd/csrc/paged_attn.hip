@@ -161,6 +161,10 @@ struct Mx<false> {
     const v2 one = {(_Float16)1.0f, (_Float16)1.0f};
     return __builtin_amdgcn_fdot2(a, one, sum, false);
   }
+  static __device__ __forceinline__ float add_zeros(v2 a, float sum) {
+    const v2 zero = {(_Float16)0.0f, (_Float16)0.0f};
+    return __builtin_amdgcn_fdot2(a, zero, sum, false);
+  }
 };
 template <>
 struct Mx<true> {
@@ -178,6 +182,10 @@ struct Mx<true> {
   static __device__ __forceinline__ float add_pair(v2 a, float sum) {
     const v2 one = {(__bf16)1.0f, (__bf16)1.0f};
     return __builtin_amdgcn_fdot2_f32_bf16(a, one, sum, false);
+  }
+  static __device__ __forceinline__ float add_zeros(v2 a, float sum) {
+    const v2 zero = {(__bf16)0.0f, (__bf16)0.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(a, zero, sum, false);
   }
 };
 
@@ -204,19 +212,18 @@ __device__ __forceinline__ V8 join4(s16x4 a, s16x4 b) {
 }
 
 // Whether BYTES (a multiple of 1024) of V at `at` hold a value that is not finite; uniform.
+// (Zero times such a value is no zero: a sum of products with zeros shows it.)
 template <bool BF, int BYTES>
 __device__ __forceinline__ bool any_nonfinite(uint32_t at) {
-  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-  u16x2 top = {0, 0};
   const uint32_t mine = at + 16 * (threadIdx.x & 63);
+  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < BYTES; i += 1024) {
     const u32x4 w = *LDS_AT(const u32x4, mine + i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[e] & 0x7FFF7FFFu));
+    for (int e = 0; e < 4; ++e) sum[e] = Mx<BF>::add_zeros(__builtin_bit_cast(typename Mx<BF>::v2, (uint32_t)w[e]), sum[e]);
   }
-  return __ballot(top[0] >= Mx<BF>::kInf || top[1] >= Mx<BF>::kInf) != 0;
+  return __ballot((sum[0] + sum[1]) + (sum[2] + sum[3]) != 0.0f) != 0;  // NaN
 }
 
 // Such values leave the product, and are added (as they are: Inf and NaN do what the sum
@@ -740,12 +747,12 @@ __device__ __forceinline__ int parts_of(int nb, int nsplit) { return max(min(nsp
 
 struct ManyTile {
   int s, h, tok0, toks, total, n;  // tokens of the tile and of the request, new and all
-  int lo, hi, lo_max;              // the union of their ranges, the largest first position
+  int lo, hi;                      // the union of their ranges
   int64_t a;
 };
 
 // Tile and head of a workgroup index (later tiles, which see more, first).  Every thread of
-// 256; red[12] is LDS.
+// 256; red[8] is LDS.
 __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int* before, int tile, int h, int* red) {
   ManyTile t;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tm = kManyRows / p.G;
@@ -758,30 +765,24 @@ __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int*
   t.tok0 = (x - uniform(before[t.s])) * tm;
   t.toks = min(tm, t.total - t.tok0);
   if (!p.first && !p.prefix) {
-    t.lo = t.lo_max = 0;
+    t.lo = 0;
     t.hi = t.n - t.total + t.tok0 + t.toks;
     return t;
   }
-  int lo = t.n, hi = 0, lo_max = 0;
-  if (tid < t.toks) {
-    token_range(p, t.s, t.a + t.tok0 + tid, t.n - t.total + t.tok0 + tid, t.n, &lo, &hi);
-    lo_max = lo;
-  }
+  int lo = t.n, hi = 0;
+  if (tid < t.toks) token_range(p, t.s, t.a + t.tok0 + tid, t.n - t.total + t.tok0 + tid, t.n, &lo, &hi);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     lo = min(lo, __shfl_xor(lo, o, kWave));
     hi = max(hi, __shfl_xor(hi, o, kWave));
-    lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
   }
   if (lane == 0) {
     red[wave] = lo;
     red[4 + wave] = hi;
-    red[8 + wave] = lo_max;
   }
   __syncthreads();
   t.lo = uniform(min(min(red[0], red[1]), min(red[2], red[3]))) & ~(kManyKeys - 1);
   t.hi = uniform(max(max(red[4], red[5]), max(red[6], red[7])));
-  t.lo_max = uniform(max(max(red[8], red[9]), max(red[10], red[11])));
   __syncthreads();
   return t;
 }
@@ -852,11 +853,8 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     return (int64_t)((uint32_t)id < (uint32_t)p.c.P ? id : 0) * p.c.ld_page +
            (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
   };
-  // Blocks [f0, ..) have no key before a query's first; f0 is at stage 0 of the rings, so that
-  // the four copies of the loop below know their stages.
-  const int f0 = min(max((t.lo_max - key0 + kManyKeys - 1) / kManyKeys, 0), nb), phase = -f0 & (kManyStages - 1);
-  auto stage = [&](int b) __attribute__((always_inline)) -> uint32_t {
-    return (uint32_t)((b + phase) % kManyStages) * (kManyStage / 2);
+  auto stage = [](int b) __attribute__((always_inline)) -> uint32_t {
+    return (uint32_t)(b % kManyStages) * (kManyStage / 2);
   };
   constexpr uint32_t kVRing = kManyStages * (kManyStage / 2);  // V's stages behind K's
   const uint32_t mine = lds0 + wave * 4096;
@@ -874,7 +872,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
 
   // ---- the wave's 64 query rows: column tiles of 32 ----
   v8 qf[2][8];
-  int pos[2], lo[2], hi[2], hi_min = n;
+  int pos[2], lo[2], hi[2], lo_max = 0, hi_min = n;
   float slope[2];
   const ScoreMap sm = score_map(p);
 #pragma unroll
@@ -895,16 +893,21 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
       const uint16_t* qp = p.q + row * p.ldq_tok + (int64_t)(h * G + g) * p.ldq_head + 8 * half;
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) qf[c][kk] = *reinterpret_cast<const v8*>(qp + 16 * kk);
+      lo_max = max(lo_max, lo[c]);
       hi_min = min(hi_min, MAP != 0 ? min(hi[c], pos[c] + 1) : hi[c]);  // (map_seen)
     }
   }
-  if (!p.prefix) {  // the wave's first token
+  if (!p.prefix && !p.first) {  // the wave's first token
     hi_min = wave * 64 < rows ? n - t.total + t.tok0 + wave * 64 / G + 1 : n;
   } else {
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) hi_min = min(hi_min, __shfl_xor(hi_min, o, kWave));
-    hi_min = uniform(hi_min);
+    for (int o = 16; o >= 1; o >>= 1) {
+      lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
+      hi_min = min(hi_min, __shfl_xor(hi_min, o, kWave));
+    }
   }
+  lo_max = uniform(lo_max);
+  hi_min = uniform(hi_min);
   // ---- absent pages among the keys: their blocks are masked throughout ----
   {
     const int e1 = min(key0 + nb * kManyKeys, n);
@@ -945,12 +948,17 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[c][d][e] = 0.0f;
   }
+  auto k_frag = [&](uint32_t at, int kk) __attribute__((always_inline)) { return lds_v8<v8>((kaddr ^ (32 * kk)) + at); };
+  auto v_frag = [&](uint32_t at, int j) __attribute__((always_inline)) {
+    const uint32_t va = (vaddr ^ (64 * (j & 3))) + at + 16 * (j >> 2) * kRowBytes;
+    return join4<v8>(lds_tr(va), lds_tr(va + 8 * kRowBytes));
+  };
   // S^T of the 32 keys at byte `at` of K's ring
   auto scores = [&](uint32_t at, Sv (&s)[2]) __attribute__((always_inline)) {
     f32x16 acc[2] = {};
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) {
-      const v8 kf = lds_v8<v8>((kaddr ^ (32 * kk)) + at);
+      const v8 kf = k_frag(at, kk);
 #pragma unroll
       for (int c = 0; c < 2; ++c) acc[c] = Mx<BF>::mfma32(kf, qf[c][kk], acc[c]);
     }
@@ -960,15 +968,12 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
       for (int e = 0; e < 16; ++e) s[c][e] = acc[c][e];
   };
   // O^T += V^T P^T of the 32 keys at byte `at` of V's ring
-  auto product = [&](uint32_t at, const u32x4 (&pr)[2][2], auto clean) __attribute__((always_inline)) {
+  auto product = [&](uint32_t at, const u32x4 (&pr)[2][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const uint32_t va = (vaddr ^ (64 * d)) + at + 16 * i * kRowBytes;
-        s16x8 x = __builtin_shufflevector(lds_tr(va), lds_tr(va + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7);
-        if constexpr (decltype(clean)::value) x = finite_part<BF>(x);
-        const v8 vf = __builtin_bit_cast(v8, x);
+        const v8 vf = v_frag(at, 4 * i + d);
 #pragma unroll
         for (int c = 0; c < 2; ++c) o[c][d] = Mx<BF>::mfma32(vf, __builtin_bit_cast(v8, pr[c][i]), o[c][d]);
       }
@@ -1056,10 +1061,11 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     from = from_next;
   };
 
-  // Blocks that some query of the wave does not see whole: a half at a time, without overlap.
+  // A block (`advance`d to) that some query of the wave does not see whole: a half at a time,
+  // without overlap.  Kept short: a workgroup meets two or three such blocks, and code that
+  // is not in the instruction cache costs more than it does.
   auto masked_block = [&](int b) __attribute__((always_inline)) {
     const int key_b = key0 + b * kManyKeys;
-    advance(b);
     if (key_b + kManyKeys > n || absent) {  // rows that are not there: V is cleared, a wave its 16
       const bool in = there(key_b + 16 * wave);
 #pragma unroll
@@ -1077,38 +1083,55 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
       const int key = key_b + 32 * hf;
       const uint32_t at = stage(b) + hf * kHalf;
       scores(at, sa);
-      map_scores(sa, key);
-      const bool in0 = there(key), in1 = there(key + 16);
+      if (MAP != 0 && !p.prefix) map_half(sa, key);  // (what it gives for keys behind the row's own is masked)
+      else map_scores(sa, key);
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < 2; ++c) {
+        const uint32_t from = lo[c] - key - 4 * half, count = max(hi[c] - lo[c], 0);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int k = key + 8 * (e >> 2) + 4 * half + (e & 3);
-          if (!(k >= lo[c] && k < hi[c] && (e < 8 ? in0 : in1))) sa[c][e] = -__builtin_huge_valf();
-        }
+        for (int e = 0; e < 16; ++e)
+          if ((uint32_t)(8 * (e >> 2) + (e & 3)) - from >= count) sa[c][e] = -__builtin_huge_valf();
+      }
+      if (absent) {
+        const bool in0 = there(key), in1 = there(key + 16);
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(e < 8 ? in0 : in1)) sa[c][e] = -__builtin_huge_valf();
+      }
       float f[2];
       maxima(sa);
       if (raise(f)) rescale(f);
       exponentials(sa, pa);
-      if (!any_nonfinite<BF, kHalf>(lds0 + kVRing + at)) {
-        product(at, pa, std::false_type());
-        continue;
-      }
+      const bool clean = any_nonfinite<BF, kHalf>(lds0 + kVRing + at);
+      if (clean) {
 #pragma unroll 1
-      for (int row = 0; row < 32; ++row) {
-        const int k = key + row;
-        const bool in = there(k);
+        for (int row = 0; row < 32; ++row) {
+          const int k = key + row;
+          const bool in = there(k);
+          const bool sees[2] = {in && k >= lo[0] && k < hi[0], in && k >= lo[1] && k < hi[1]};
 #pragma unroll
-        for (int y = 0; y < 16; ++y) {  // channels 8 y + 4 half ..
-          const s16x4 x = *LDS_AT(const s16x4, lds0 + kVRing + at + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
+          for (int y = 0; y < 16; ++y) {  // channels 8 y + 4 half ..
+            const s16x4 x = *LDS_AT(const s16x4, lds0 + kVRing + at + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 4; ++e) {
+              const float add = nonfinite_part<BF>(x[e]);
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-              if (in && k >= lo[c] && k < hi[c]) o[c][y >> 2][4 * (y & 3) + e] += nonfinite_part<BF>(x[e]);
+              for (int c = 0; c < 2; ++c) o[c][y >> 2][4 * (y & 3) + e] += sees[c] ? add : 0.0f;
+            }
+          }
         }
       }
-      product(at, pa, std::true_type());
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          v8 vf = v_frag(at, 4 * i + d);
+          if (clean) vf = __builtin_bit_cast(v8, finite_part<BF>(__builtin_bit_cast(s16x8, vf)));
+#pragma unroll
+          for (int c = 0; c < 2; ++c) o[c][d] = Mx<BF>::mfma32(vf, __builtin_bit_cast(v8, pa[c][i]), o[c][d]);
+        }
     }
   };
 
@@ -1118,11 +1141,6 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   // two, in `ka` and `kb`, for the step after, K at `kafter`), and of two exponentials with
   // what belongs to them: a wave alone on its SIMD issues about as long as the two matrix
   // instructions run.
-  auto k_frag = [&](uint32_t at, int kk) __attribute__((always_inline)) { return lds_v8<v8>((kaddr ^ (32 * kk)) + at); };
-  auto v_frag = [&](uint32_t at, int j) __attribute__((always_inline)) {
-    const uint32_t va = (vaddr ^ (64 * (j & 3))) + at + 16 * (j >> 2) * kRowBytes;
-    return join4<v8>(lds_tr(va), lds_tr(va + 8 * kRowBytes));
-  };
   auto half_step = [&](const Sv (&s)[2], u32x4 (&pr)[2][2], uint32_t kat, Sv (&sn)[2], int key_next, uint32_t vat,
                        const u32x4 (&pp)[2][2], v8& ka, v8& kb, uint32_t kafter) __attribute__((always_inline)) {
     v8 fr[18];
@@ -1184,48 +1202,51 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     kb = fr[17];
   };
   // Blocks [f0, f1) are seen whole by every query of the wave.
-  const int f1 = absent ? f0 : max(f0, min((hi_min - key0) / kManyKeys, nb));
-  for (int b = 0; b < f0; ++b) masked_block(b);
+  const int f0 = absent ? nb : min(max((lo_max - key0 + kManyKeys - 1) / kManyKeys, 0), nb);
+  const int f1 = max(f0, min((hi_min - key0) / kManyKeys, nb));
+#pragma unroll 1
+  for (int b = 0; b < f0; ++b) {
+    advance(b);
+    masked_block(b);
+  }
   if (f0 < f1) {
-    constexpr uint32_t kStage = kManyStage / 2;
+    int b = f0;
+    advance(b);
     float f[2];
-    const int key = key0 + f0 * kManyKeys;
-    advance(f0);
-    scores(0, sa);
-    map_half(sa, key);
+    scores(stage(b), sa);
+    map_half(sa, key0 + b * kManyKeys);
     maxima(sa);
     if (raise(f)) rescale(f);
-    scores(kHalf, sb);
+    scores(stage(b) + kHalf, sb);
     exponentials(sa, pa);
-    map_half(sb, key + 32);
+    map_half(sb, key0 + b * kManyKeys + 32);
     // where it is raised, the product that is still to come is in the old scale: O follows after it
     maxima(sb);
     bool up = raise(f);
-    v8 ka = k_frag(kStage, 0), kb = k_frag(kStage, 1);
-    int b = f0;
-    auto block = [&](auto at) __attribute__((always_inline)) {  // second half of block b at stage `at`, first half of block b + 1
-      constexpr uint32_t s0 = decltype(at)::value * kStage, s1 = (decltype(at)::value + 1) % kManyStages * kStage;
-      half_step(sb, pb, s1, sa, key0 + (b + 1) * kManyKeys, s0, pa, ka, kb, s1 + kHalf);
+    v8 ka = k_frag(stage(b + 1), 0), kb = k_frag(stage(b + 1), 1);
+    // the second half of block b, the first half of block b + 1
+#pragma unroll 1
+    for (; b + 1 < f1; ++b) {
+      const uint32_t s0 = stage(b), s1 = stage(b + 1), s2 = stage(b + 2);
+      const int key = key0 + (b + 1) * kManyKeys;
+      half_step(sb, pb, s1, sa, key, s0, pa, ka, kb, s1 + kHalf);
       if (up) rescale(f);
       up = raise(f);
       advance(b + 1);
-      constexpr uint32_t s2 = (decltype(at)::value + 2) % kManyStages * kStage;
-      half_step(sa, pa, s1 + kHalf, sb, key0 + (b + 1) * kManyKeys + 32, s0 + kHalf, pb, ka, kb, s2);
+      half_step(sa, pa, s1 + kHalf, sb, key + 32, s0 + kHalf, pb, ka, kb, s2);
       if (up) rescale(f);
       up = raise(f);
-      ++b;
-      return b + 1 < f1;
-    };
-    if (b + 1 < f1)
-      while (block(std::integral_constant<int, 0>()) && block(std::integral_constant<int, 1>()) &&
-             block(std::integral_constant<int, 2>()) && block(std::integral_constant<int, 3>())) {
-      }
-    product(stage(f1 - 1), pa, std::false_type());
+    }
+    product(stage(b), pa);
     if (up) rescale(f);
     exponentials(sb, pb);
-    product(stage(f1 - 1) + kHalf, pb, std::false_type());
+    product(stage(b) + kHalf, pb);
   }
-  for (int b = f1; b < nb; ++b) masked_block(b);
+#pragma unroll 1
+  for (int b = f1; b < nb; ++b) {
+    advance(b);
+    masked_block(b);
+  }
 
   // ---- the output, or a part of it ----
   wait_vm<0>();
