@@ -394,39 +394,53 @@ def fathom_klt_rotate_q(q, V, out=None, stream=None):
 
 
 # ---------------------------------------------------------------- paged cache
+# A call of a decode step runs for 3 to 16 us on the GPU, so the host's share is kept small: addresses go to the library
+# as integers, and a tensor's device is asked for once, as a number.
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _a(t):
+    return None if t is None else t.data_ptr()
+
+
+def _here(stream, ts):
+    """The raw stream, after a check that the tensors are on the current device: the launch goes to it."""
+    if not ts[0].is_cuda:
+        raise ValueError("fathom calls take device tensors")
+    dev = _get_device()
+    for t in ts:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("paged calls take tensors of the current device")
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
 def _paged_dt(t: torch.Tensor) -> int:
-    return FATHOM_BF16 if t.dtype == torch.bfloat16 else _dt(t)
+    return FATHOM_BF16 if t.dtype is torch.bfloat16 else _dt(t)
 
 
 def _pages(K, V):
     """fathom_pages of pools K and V [P][H][page][D] (any strides with channel stride 1; V None: keys only)."""
-    if K.dim() != 4 or K.stride(3) != 1 or K.dtype not in (torch.float16, torch.bfloat16):
+    shape, st, dt = K.shape, K.stride(), K.dtype
+    if len(shape) != 4 or st[3] != 1 or not (dt is torch.float16 or dt is torch.bfloat16):
         raise ValueError("pages are fp16 or bf16 [P][H][page][D] with channel stride 1")
-    if V is not None and (V.shape != K.shape or V.stride() != K.stride() or V.dtype != K.dtype):
+    if V is not None and (V.shape != shape or V.stride() != st or V.dtype is not dt):
         raise ValueError("K and V pages need the same shape, strides and type")
-    P, H, page, _ = K.shape
-    return _Pages(K.data_ptr(), None if V is None else V.data_ptr(), _paged_dt(K), H, page, P, K.stride(0), K.stride(1),
-                  K.stride(2))
+    return _Pages(K.data_ptr(), None if V is None else V.data_ptr(), FATHOM_BF16 if dt is torch.bfloat16 else FATHOM_F16,
+                  shape[1], shape[2], shape[0], st[0], st[1], st[2])
 
 
 def _table(table):
-    if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+    shape = table.shape
+    if table.dtype is not torch.int32 or len(shape) != 2 or not table.is_contiguous():
         raise ValueError("table is contiguous int32 [S][pages]")
-    return table.shape[1]
+    return shape
 
 
-def _here(*ts):
-    """Device tensors of the current device: the launch goes to its stream."""
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in ts:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise ValueError("paged calls take tensors of the current device")
-
-
-def _int64(S, **ts):
-    for name, t in ts.items():
-        if t is not None and (t.dtype != torch.int64 or t.numel() != S or not t.is_contiguous()):
-            raise ValueError(f"{name} is contiguous int64 of {S} elements")
+def _int64(name, t, n):
+    if t.dtype is not torch.int64 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} is contiguous int64 of {n} elements")
 
 
 def fathom_paged_map(n_old, n, page, table, ring, state, T, H=1, slots=None, start=None, n_now=None, n_unit=None,
@@ -435,85 +449,90 @@ def fathom_paged_map(n_old, n, page, table, ring, state, T, H=1, slots=None, sta
     (ring [P] i32, state = (head, count)) into table [S][pages] i32 or returning them -> (slots [T], start [S + 1],
     n_now [S], n_unit [S*H], state_out [2]).  table and ring are updated; a request that cannot be served keeps its
     length (dev_status)."""
-    _here(n_old, n, table, ring, state, slots, start, n_now, n_unit, state_out, dev_status)
-    S, T, dev = table.shape[0], int(T), n.device
-    ld = _table(table)
-    i64 = dict(dtype=torch.int64, device=dev)
+    S, ld = _table(table)
+    T, H = int(T), int(H)
+    i64 = dict(dtype=torch.int64, device=table.device)
     slots = torch.empty((T,), **i64) if slots is None else slots
     start = torch.empty((S + 1,), **i64) if start is None else start
     n_now = torch.empty((S,), **i64) if n_now is None else n_now
     n_unit = torch.empty((S * H,), **i64) if n_unit is None else n_unit
     state_out = torch.empty((2,), **i64) if state_out is None else state_out
-    _int64(S, n_old=n_old, n=n, n_now=n_now)
-    _int64(2, state=state, state_out=state_out)
-    _int64(T, slots=slots)
-    _int64(S + 1, start=start)
-    _int64(S * H, n_unit=n_unit)
-    if ring.dtype != torch.int32 or not ring.is_contiguous():
+    st = _here(stream, (table, n_old, n, ring, state, slots, start, n_now, n_unit, state_out, dev_status))
+    _int64("n_old", n_old, S)
+    _int64("n", n, S)
+    _int64("n_now", n_now, S)
+    _int64("state", state, 2)
+    _int64("state_out", state_out, 2)
+    _int64("slots", slots, T)
+    _int64("start", start, S + 1)
+    _int64("n_unit", n_unit, S * H)
+    if ring.dtype is not torch.int32 or not ring.is_contiguous():
         raise ValueError("ring is contiguous int32")
-    _check(lib().fathom_paged_map(_p(n_old), _p(n), S, int(H), int(page), _p(table), ld, _p(ring), ring.numel(),
-                                  _p(state), _p(slots), T, _p(start), _p(n_now), _p(n_unit), _p(state_out),
-                                  _p(dev_status), _stream(stream)), "fathom_paged_map")
+    _check(lib().fathom_paged_map(_a(n_old), _a(n), S, H, int(page), _a(table), ld, _a(ring), ring.numel(), _a(state),
+                                  _a(slots), T, _a(start), _a(n_now), _a(n_unit), _a(state_out), _a(dev_status), st),
+           "fathom_paged_map")
     return slots, start, n_now, n_unit, state_out
 
 
 def fathom_paged_write(K, V, slots, Kpages, Vpages, dev_status=None, stream=None):
     """New rows K, V [T][H][D] (the pages' type, or fp32: rounded) to their slots [T] in the pages [P][H][page][D];
     negative slots are skipped."""
-    _here(K, V, slots, Kpages, Vpages, dev_status)
+    st = _here(stream, (K, V, slots, Kpages, Vpages, dev_status))
     pg = _pages(Kpages, Vpages)
     T, H, D = K.shape
-    if V.shape != K.shape or V.dtype != K.dtype or H != pg.H or D != Kpages.shape[3]:
+    if V.shape != K.shape or V.dtype is not K.dtype or H != pg.H or D != Kpages.shape[3]:
         raise ValueError("K and V are [T][H][D] of one type, with the pages' H and D")
-    if K.stride(2) != 1 or V.stride(2) != 1:
+    ks, vs = K.stride(), V.stride()
+    if ks[2] != 1 or vs[2] != 1:
         raise ValueError("channel stride must be 1")
-    _int64(T, slots=slots)
-    _check(lib().fathom_paged_write(_p(K), _p(V), _paged_dt(K), K.stride(0), K.stride(1), V.stride(0), V.stride(1),
-                                    _p(slots), T, D, C.byref(pg), _p(dev_status), _stream(stream)),
-           "fathom_paged_write")
+    _int64("slots", slots, T)
+    _check(lib().fathom_paged_write(_a(K), _a(V), _paged_dt(K), ks[0], ks[1], vs[0], vs[1], _a(slots), T, D, C.byref(pg),
+                                    _a(dev_status), st), "fathom_paged_write")
     return Kpages, Vpages
 
 
 def fathom_paged_pack(Kpages, table, n, planes, scales, n_old=None, max_new=0, dev_status=None, stream=None):
     """fathom_pack (n_old None) or fathom_pack_append over keys in pages: units s*H + h of planes [S*H][D][4][nb_cap] and
     scales [S*H][D][nb_cap]; n and n_old [S] are per request."""
-    _here(Kpages, table, n, planes, scales, n_old, dev_status)
+    st = _here(stream, (Kpages, table, n, planes, scales, n_old, dev_status))
     pg = _pages(Kpages, None)
-    S = table.shape[0]
-    ld = _table(table)
-    _int64(S, n=n, n_old=n_old)
-    U, D, _, nb_cap = planes.shape
-    if U != S * pg.H or tuple(scales.shape) != (U, D, nb_cap) or not planes.is_contiguous() or not scales.is_contiguous():
-        raise ValueError("planes and scales are contiguous [S*H][D][4][nb_cap] and [S*H][D][nb_cap]")
-    _check(lib().fathom_paged_pack(C.byref(pg), _p(table), ld, _p(n_old), _p(n), int(max_new), S, D, nb_cap, _p(planes),
-                                   _p(scales), _p(dev_status), _stream(stream)), "fathom_paged_pack")
+    S, ld = _table(table)
+    _int64("n", n, S)
+    if n_old is not None:
+        _int64("n_old", n_old, S)
+    U, D, four, nb_cap = planes.shape
+    if U != S * pg.H or D != Kpages.shape[3] or four != 4 or scales.shape != (U, D, nb_cap) or \
+            planes.element_size() != 8 or scales.element_size() != 2 or \
+            not planes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("planes and scales are contiguous [S*H][D][4][nb_cap] of 64 and [S*H][D][nb_cap] of 16 bits")
+    _check(lib().fathom_paged_pack(C.byref(pg), _a(table), ld, _a(n_old), _a(n), int(max_new), S, D, nb_cap, _a(planes),
+                                   _a(scales), _a(dev_status), st), "fathom_paged_pack")
     return planes, scales
 
 
 def fathom_paged_sparse_attn(q, Kpages, Vpages, table, n, idx, n_sink=0, n_local=0, sm_scale=None, out=None,
                              dev_status=None, stream=None, ws=None):
     """fathom_sparse_attn over rows in pages: q [S*H][G][D], idx [S*H][G][k], n [S] per request -> out [S*H][G][D] fp32."""
-    _here(q, Kpages, Vpages, table, n, idx, out, ws, dev_status)
+    st = _here(stream, (q, Kpages, Vpages, table, n, idx, out, ws, dev_status))
     pg = _pages(Kpages, Vpages)
     U, G, D = q.shape
-    S = table.shape[0]
-    ld = _table(table)
-    _int64(S, n=n)
-    if U != S * pg.H or not q.is_contiguous():
+    S, ld = _table(table)
+    _int64("n", n, S)
+    if U != S * pg.H or D != Kpages.shape[3] or not q.is_contiguous():
         raise ValueError("q is contiguous [S*H][G][D]")
-    if idx is not None and (idx.dtype != torch.int32 or not idx.is_contiguous() or tuple(idx.shape[:2]) != (U, G)):
+    if idx is not None and (idx.dtype is not torch.int32 or not idx.is_contiguous() or idx.shape[:2] != (U, G)):
         raise ValueError("idx is contiguous int32 [S*H][G][k]")
     k = 0 if idx is None else idx.shape[-1]
     sm_scale = 1.0 / (D ** 0.5) if sm_scale is None else sm_scale
     if out is None:
         out = torch.empty((U, G, D), dtype=torch.float32, device=q.device)
-    if out.dtype != torch.float32 or out.shape != q.shape or not out.is_contiguous():
+    elif out.dtype is not torch.float32 or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("out is contiguous fp32 [S*H][G][D]")
-    ws = _ws(fathom_sparse_attn_workspace_size(U, G, k, n_sink, n_local), ws, q.device)
-    _check(lib().fathom_paged_sparse_attn(_p(q), _paged_dt(q), C.byref(pg), _p(table), ld, _p(n), S, G, D, _p(idx), k,
-                                          int(n_sink), int(n_local), C.c_float(sm_scale), _p(out), _p(ws),
-                                          ws.numel() * ws.element_size(), _p(dev_status), _stream(stream)),
-           "fathom_paged_sparse_attn")
+    if ws is None:
+        ws = _ws(fathom_sparse_attn_workspace_size(U, G, k, n_sink, n_local), ws, q.device)
+    _check(lib().fathom_paged_sparse_attn(_a(q), _paged_dt(q), C.byref(pg), _a(table), ld, _a(n), S, G, D, _a(idx), k,
+                                          int(n_sink), int(n_local), sm_scale, _a(out), _a(ws),
+                                          ws.numel() * ws.element_size(), _a(dev_status), st), "fathom_paged_sparse_attn")
     return out
 
 
@@ -527,27 +546,29 @@ def fathom_paged_attn(q, Kpages, Vpages, table, start, n, max_new, sm_scale=None
     n[s] tokens) over the paged cache -> out [T][H*G][D] of the pages' type.  softcap: scores capped by
     softcap * tanh(z / softcap); slopes [H*G] fp32: bias -slope * distance; prefix [S]: leading positions that every token
     sees; first [T]: the first position that a token sees.  max_new bounds start[s + 1] - start[s]."""
-    _here(q, Kpages, Vpages, table, start, n, slopes, prefix, first, out, ws, dev_status)
+    st = _here(stream, (q, Kpages, Vpages, table, start, n, slopes, prefix, first, out, ws, dev_status))
     pg = _pages(Kpages, Vpages)
     T, HG, D = q.shape
-    S = table.shape[0]
-    ld = _table(table)
-    _int64(S, n=n, prefix=prefix)
-    _int64(S + 1, start=start)
-    _int64(T, first=first)
-    if q.dtype != Kpages.dtype or q.stride(2) != 1 or HG % pg.H:
+    S, ld = _table(table)
+    _int64("n", n, S)
+    _int64("start", start, S + 1)
+    if prefix is not None:
+        _int64("prefix", prefix, S)
+    if first is not None:
+        _int64("first", first, T)
+    H, qs = pg.H, q.stride()
+    if q.dtype is not Kpages.dtype or qs[2] != 1 or HG % H or D != Kpages.shape[3]:
         raise ValueError("q is [T][H*G][D] of the pages' type with channel stride 1")
-    if slopes is not None and (slopes.dtype != torch.float32 or slopes.numel() != HG or not slopes.is_contiguous()):
+    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.numel() != HG or not slopes.is_contiguous()):
         raise ValueError("slopes is contiguous fp32 [H*G]")
-    G = HG // pg.H
     sm_scale = 1.0 / (D ** 0.5) if sm_scale is None else sm_scale
     if out is None:
         out = torch.empty((T, HG, D), dtype=q.dtype, device=q.device)
-    if out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous():
+    elif out.dtype is not q.dtype or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("out is contiguous [T][H*G][D] of the pages' type")
-    ws = _ws(fathom_paged_attn_workspace_size(T, S, pg.H, G, max_new), ws, q.device)
-    _check(lib().fathom_paged_attn(_p(q), q.stride(0), q.stride(1), C.byref(pg), _p(table), ld, _p(start), _p(n), S, T,
-                                   int(max_new), G, D, C.c_float(sm_scale), C.c_float(softcap), _p(slopes), _p(prefix),
-                                   _p(first), _p(out), _p(ws), ws.numel() * ws.element_size(), _p(dev_status),
-                                   _stream(stream)), "fathom_paged_attn")
+    if ws is None:
+        ws = _ws(fathom_paged_attn_workspace_size(T, S, H, HG // H, max_new), ws, q.device)
+    _check(lib().fathom_paged_attn(_a(q), qs[0], qs[1], C.byref(pg), _a(table), ld, _a(start), _a(n), S, T, int(max_new),
+                                   HG // H, D, sm_scale, softcap, _a(slopes), _a(prefix), _a(first), _a(out), _a(ws),
+                                   ws.numel() * ws.element_size(), _a(dev_status), st), "fathom_paged_attn")
     return out

@@ -20,9 +20,11 @@
 
 namespace fathom {
 
+// Threads of a workgroup and requests of a thread: up to 256 requests of a call 256 and 1
+// (its 4 waves meet sooner), up to the limit 1024 and 4.
 constexpr int kMapThreads = 1024;
-constexpr int kMapPer = kMaxSeqs / kMapThreads;  // requests per thread
-static_assert(kMapPer * kMapThreads == kMaxSeqs, "requests divide over the threads");
+constexpr int kMapFew = 256;
+static_assert(kMaxSeqs % kMapThreads == 0, "requests divide over the threads");
 
 struct MapArgs {
   const int64_t *n_old, *n;
@@ -39,7 +41,8 @@ struct MapArgs {
 };
 
 // Inclusive sums of three values over the workgroup (each thread's own sum given).
-__device__ __forceinline__ void block_scan3(int64_t (&v)[3], int64_t (&part)[3][kMapThreads / kWave]) {
+template <int THREADS>
+__device__ __forceinline__ void block_scan3(int64_t (&v)[3], int64_t (&part)[3][THREADS / kWave]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
@@ -54,7 +57,8 @@ __device__ __forceinline__ void block_scan3(int64_t (&v)[3], int64_t (&part)[3][
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     int64_t before = 0;
-    for (int w = 0; w < wave; ++w) before += part[i][w];
+#pragma unroll
+    for (int w = 0; w < THREADS / kWave; ++w) before += w < wave ? part[i][w] : 0;
     v[i] += before;
   }
 }
@@ -77,10 +81,11 @@ __device__ __forceinline__ int last_at_most(const int32_t* a, int count, int32_t
 __device__ __forceinline__ int32_t clip31(int64_t x) { return (int32_t)(x < 0x7fffffff ? x : 0x7fffffff); }
 
 // FILL: slots, table and ring.  FINISH: start, lengths and state, after every read.
-template <bool FILL, bool FINISH>
-__global__ __launch_bounds__(kMapThreads) void paged_map_kernel(MapArgs a) {
+template <int THREADS, bool FILL, bool FINISH>
+__global__ __launch_bounds__(THREADS) void paged_map_kernel(MapArgs a) {
   extern __shared__ int32_t sm[];
-  __shared__ int64_t part[3][kMapThreads / kWave];
+  constexpr int kPer = THREADS == kMapFew ? kMapFew / THREADS : kMaxSeqs / THREADS;
+  __shared__ int64_t part[3][THREADS / kWave];
   __shared__ int64_t tot[4];  // rows, pages returned; pages taken by those served
   const int S = a.S, tid = threadIdx.x;
   int32_t* s_start = sm;        // [S] first new row
@@ -97,16 +102,16 @@ __global__ __launch_bounds__(kMapThreads) void paged_map_kernel(MapArgs a) {
     count = 0;
   }
   if (tid == 0) tot[2] = 0;
-  int64_t no[kMapPer], nn[kMapPer], sum[3] = {0, 0, 0};
+  int64_t no[kPer], nn[kPer], sum[3] = {0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < kMapPer; ++i) {
-    const int s = tid * kMapPer + i;
+  for (int i = 0; i < kPer; ++i) {
+    const int s = tid * kPer + i;
     no[i] = s < S ? a.n_old[s] : 0;
     nn[i] = s < S ? a.n[s] : 0;
   }
-  int64_t add[kMapPer][3];
+  int64_t add[kPer][3];
 #pragma unroll
-  for (int i = 0; i < kMapPer; ++i) {
+  for (int i = 0; i < kPer; ++i) {
     const bool ok = no[i] >= 0 && no[i] <= cap && nn[i] >= 0 && nn[i] <= cap;
     const int64_t before = (no[i] + rnd) >> a.shift, after = (nn[i] + rnd) >> a.shift;
     add[i][0] = ok && nn[i] > no[i] ? nn[i] - no[i] : 0;
@@ -116,17 +121,17 @@ __global__ __launch_bounds__(kMapThreads) void paged_map_kernel(MapArgs a) {
     for (int x = 0; x < 3; ++x) sum[x] += add[i][x];
   }
   int64_t inc[3] = {sum[0], sum[1], sum[2]};
-  block_scan3(inc, part);
-  if (tid == kMapThreads - 1) {
+  block_scan3<THREADS>(inc, part);
+  if (tid == THREADS - 1) {
     tot[0] = inc[0];
     tot[1] = inc[2];
   }
   int64_t at[3] = {inc[0] - sum[0], inc[1] - sum[1], inc[2] - sum[2]}, mine = 0;
-  int64_t first[kMapPer];
-  bool served[kMapPer];
+  int64_t first[kPer];
+  bool served[kPer];
 #pragma unroll
-  for (int i = 0; i < kMapPer; ++i) {
-    const int s = tid * kMapPer + i;
+  for (int i = 0; i < kPer; ++i) {
+    const int s = tid * kPer + i;
     const bool ok_old = no[i] >= 0 && no[i] <= cap, ok = ok_old && nn[i] >= 0 && nn[i] <= cap;
     first[i] = at[0];
     const bool fits = at[0] + add[i][0] <= a.T, pages = add[i][1] == 0 || at[1] + add[i][1] <= count;
@@ -156,7 +161,8 @@ __global__ __launch_bounds__(kMapThreads) void paged_map_kernel(MapArgs a) {
     back = 0;
   }
   if constexpr (FILL) {
-    const int64_t gt = (int64_t)blockIdx.x * kMapThreads + tid, step = (int64_t)gridDim.x * kMapThreads;
+    const int64_t gt = (int64_t)blockIdx.x * THREADS + tid, step = (int64_t)gridDim.x * THREADS;
+#pragma unroll 4
     for (int64_t t = gt; t < a.T; t += step) {
       int64_t slot = -1;
       if (t < rows) {
@@ -179,6 +185,7 @@ __global__ __launch_bounds__(kMapThreads) void paged_map_kernel(MapArgs a) {
       }
       a.slots[t] = slot;
     }
+#pragma unroll 2
     for (int64_t j = gt; j < taken; j += step) {
       const int s = last_at_most(s_taken, S, (int32_t)j);
       int64_t r = head + j;
@@ -188,6 +195,7 @@ __global__ __launch_bounds__(kMapThreads) void paged_map_kernel(MapArgs a) {
       const int64_t before = ((int64_t)s_old[s] + rnd) >> a.shift;
       a.table[(int64_t)s * a.ld_table + before + (j - s_taken[s])] = id;
     }
+#pragma unroll 4
     for (int64_t j = gt; j < back; j += step) {
       const int s = last_at_most(s_back, S, (int32_t)j);
       int64_t r = head + count + j;
@@ -199,8 +207,8 @@ __global__ __launch_bounds__(kMapThreads) void paged_map_kernel(MapArgs a) {
   }
   if constexpr (FINISH) {
 #pragma unroll
-    for (int i = 0; i < kMapPer; ++i) {
-      const int s = tid * kMapPer + i;
+    for (int i = 0; i < kPer; ++i) {
+      const int s = tid * kPer + i;
       if (s >= S) break;
       const int64_t now = served[i] ? nn[i] : no[i];
       a.start[s] = first[i];
@@ -225,14 +233,18 @@ fathom_status launch_paged_map(const int64_t* n_old, const int64_t* n, int S, in
   const MapArgs a = {n_old, n,     S, H,     shift, table, ld_table, ring, P,
                      state, slots, T, start, n_now, n_unit, state_out, st};
   const size_t lds = (size_t)5 * S * sizeof(int32_t);
-  const int64_t items = T + (int64_t)S * ld_table;  // an upper bound on slots and moved pages
-  if (items <= 32 * kMapThreads) {
-    hipLaunchKernelGGL((paged_map_kernel<true, true>), dim3(1), dim3(kMapThreads), lds, s, a);
+  // A step that moves few tokens is one launch of one workgroup.  (Pages taken are bounded by
+  // the new tokens; pages that come back are not, but a workgroup moves 1000 in about a
+  // microsecond.)
+  if (T <= 8 * kMapFew && S <= kMapFew) {
+    hipLaunchKernelGGL((paged_map_kernel<kMapFew, true, true>), dim3(1), dim3(kMapFew), lds, s, a);
+  } else if (T <= 8 * kMapThreads) {
+    hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, true>), dim3(1), dim3(kMapThreads), lds, s, a);
   } else {
-    const int64_t wgs = items / (8 * kMapThreads) + 1;
-    hipLaunchKernelGGL((paged_map_kernel<true, false>), dim3((unsigned)(wgs < 256 ? wgs : 256)), dim3(kMapThreads), lds,
-                       s, a);
-    hipLaunchKernelGGL((paged_map_kernel<false, true>), dim3(1), dim3(kMapThreads), lds, s, a);
+    const int64_t wgs = T / (4 * kMapThreads) + 1;
+    hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, false>), dim3((unsigned)(wgs < 256 ? wgs : 256)),
+                       dim3(kMapThreads), lds, s, a);
+    hipLaunchKernelGGL((paged_map_kernel<kMapThreads, false, true>), dim3(1), dim3(kMapThreads), lds, s, a);
   }
   FATHOM_LAUNCH_CHECK();
   return FATHOM_OK;

@@ -324,9 +324,17 @@ __device__ __forceinline__ int request_of(const int* before, int S, int x) {
   return lo;
 }
 
+// a / b of non-negative values (a 64-bit division takes some 150 instructions)
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
+}
+
 // Share of worker w: blocks [share(w), share(w + 1)) of W.
-__device__ __forceinline__ int64_t share(int64_t w, int64_t W) { return w * W / kFewWorkers; }
-__device__ __forceinline__ int worker_of(int64_t g, int64_t W) { return (int)(((g + 1) * kFewWorkers - 1) / W); }
+__device__ __forceinline__ int64_t share(int64_t w, int64_t W) { return (int64_t)((uint64_t)(w * W) / kFewWorkers); }
+__device__ __forceinline__ int worker_of(int64_t g, int64_t W) {
+  return (int)quotient((g + 1) * kFewWorkers - 1, W);
+}
 
 // A wave's place in the blocks of all requests and heads.
 struct Place {
@@ -376,11 +384,12 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
   };
   auto place = [&](int64_t g) {
     Place x;
-    x.s = uniform(request_of(before, S, (int)(g / H)));
-    x.nb = uniform(before[x.s + 1] - before[x.s]);
-    const int64_t rem = g - (int64_t)before[x.s] * H;
-    x.h = uniform((int)(rem / x.nb));
-    x.b = uniform((int)(rem % x.nb));
+    x.s = uniform(request_of(before, S, (int)quotient(g, H)));
+    const int first = uniform(before[x.s]);
+    x.nb = uniform(before[x.s + 1]) - first;
+    const int64_t rem = g - (int64_t)first * H;
+    x.h = uniform((int)quotient(rem, x.nb));
+    x.b = uniform((int)(rem - (int64_t)x.h * x.nb));
     x.lo = lowest(x.s);
     x.n = uniform((int)fixed(p.n, x.s));
     return x;
@@ -626,7 +635,8 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
 #pragma unroll
         for (int c = 0; c < 8; ++c) *reinterpret_cast<f32x4*>(op + 16 * c) = o[t][c];
         if (quad == 0) {
-          p.part_ml[(pr + r) * 2] = m[t];
+          // (a sum without a maximum is NaN, of NaN scores, and must not be taken for an empty part)
+          p.part_ml[(pr + r) * 2] = m[t] == -__builtin_huge_valf() && lt != 0.0f ? 0.0f : m[t];
           p.part_ml[(pr + r) * 2 + 1] = lt;
         }
       }
@@ -638,77 +648,81 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
   if (flags && lane == 0) set_status(p.st, flags);
 }
 
-// Joins the parts of one query row: out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c
-// over `count` parts, part c's row at row_of(c) (negative: none).  256 threads: 8
-// groups of 32 take every eighth part, 4 channels a thread.
-template <bool BF, class RowOf>
-__device__ __forceinline__ void join_row(const PagedAttnArgs& p, int count, RowOf row_of, uint16_t* out) {
-  __shared__ float red[4], sum_l[8];
-  __shared__ f32x4 acc[8][32];
-  const int tid = threadIdx.x, x = tid & 31, g = tid >> 5;
-  float M = -__builtin_huge_valf();
-  for (int c = tid; c < count; c += 256) {
-    const int64_t r = row_of(c);
-    if (r >= 0) M = fmaxf(M, p.part_ml[2 * r]);
-  }
-  M = wave_max(M);
-  if ((tid & 63) == 0) red[tid >> 6] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  float l = 0.0f;
-  for (int c = g; c < count; c += 8) {
-    const int64_t r = row_of(c);
-    if (r < 0) continue;
-    const float m = p.part_ml[2 * r];
-    if (m == -__builtin_huge_valf()) continue;
-    const float w = __builtin_amdgcn_exp2f(m - M);
-    l += w * p.part_ml[2 * r + 1];
-    o += w * *reinterpret_cast<const f32x4*>(p.part_o + r * kD + 4 * x);
-  }
-  acc[g][x] = o;
-  if (x == 0) sum_l[g] = l;
-  __syncthreads();
-  if (tid < 32) {
-    float den = 0.0f;
-    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      den += sum_l[i];
-      s += acc[i][tid];
-    }
-    typename Mx<BF>::t y[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(den == 0.0f ? 0.0f : s[e] / den);
-    *reinterpret_cast<u32x2*>(out + 4 * tid) = *reinterpret_cast<u32x2*>(y);
-  }
-}
-
 // The requests of attn_few_kernel whose blocks went to more than one wave: a workgroup a
-// query row.  Block counts are recomputed from the lengths.
+// query row, out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over the row's parts, in a
+// fixed order.  Block counts are recomputed from the lengths.  A trip to memory for the
+// lengths, one for every part's (m, l), a thread a part, and one for eight parts' sums at a
+// time, 32 threads and 4 channels a thread each (one part after another: 14 us for 128
+// parts, where this takes 5).
+constexpr int kJoinGroups = 8, kJoinBatch = 8;
 template <bool BF>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ float weight[kFewWorkers], red_m[4], red_l[4];
+  __shared__ f32x4 acc[kJoinGroups][32];
   int* before = reinterpret_cast<int*>(smem);
+  const int s = blockIdx.x, h = blockIdx.y / R, r = blockIdx.y % R, H = p.c.H, G = p.G;
+  const int64_t a = fixed(p.start, s);
+  if (r >= (fixed(p.start, s + 1) - a) * G) return;
   uint32_t flags = 0;
   few_plan(p, before, before + p.S + 1, flags);
-  const int s = blockIdx.x, h = blockIdx.y / R, r = blockIdx.y % R, H = p.c.H, G = p.G;
-  const int nb = before[s + 1] - before[s];
+  const int nb = uniform(before[s + 1] - before[s]);
   if (nb == 0) return;
-  const int64_t a = p.start[s];
-  if (r >= (int)(p.start[s + 1] - a) * G) return;
-  const int64_t W = (int64_t)before[p.S] * H, g0 = (int64_t)before[s] * H + (int64_t)h * nb;
-  const int w0 = worker_of(g0, W), w1 = worker_of(g0 + nb - 1, W);
-  if (w0 == w1) return;
+  const int64_t W = (int64_t)uniform(before[p.S]) * H, g0 = (int64_t)uniform(before[s]) * H + (int64_t)h * nb;
+  const int w0 = worker_of(g0, W), count = worker_of(g0 + nb - 1, W) - w0 + 1;
+  if (count == 1) return;
+  const int tid = threadIdx.x, x = tid & 31, g = tid >> 5;
+  // a part is its wave's first piece, but for a wave that begins in an earlier request or head
+  const int64_t row0 = (int64_t)w0 * 2 * R + r, step = 2 * R;
+  const int64_t late = share(w0, W) < g0 ? R : 0;
+  float M = -__builtin_huge_valf(), l = 0.0f;
+  for (int c = tid; c < count; c += 256) {
+    float m = -__builtin_huge_valf();
+    if (share(w0 + c, W) < share(w0 + c + 1, W)) m = p.part_ml[2 * (row0 + c * step + (c == 0 ? late : 0))];
+    weight[c] = m;
+    M = fmaxf(M, m);
+  }
+  M = wave_max(M);
+  if ((tid & 63) == 0) red_m[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+  for (int c = tid; c < count; c += 256) {
+    const float m = weight[c];
+    const float w = m == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(m - M);
+    weight[c] = w;
+    if (m != -__builtin_huge_valf()) l += w * p.part_ml[2 * (row0 + c * step + (c == 0 ? late : 0)) + 1];
+  }
+  l = wave_sum(l);
+  if ((tid & 63) == 0) red_l[tid >> 6] = l;
+  __syncthreads();
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int c0 = g; c0 < count; c0 += kJoinGroups * kJoinBatch) {
+    f32x4 v[kJoinBatch];
+    float w[kJoinBatch];
+#pragma unroll
+    for (int i = 0; i < kJoinBatch; ++i) {
+      const int c = c0 + i * kJoinGroups;
+      w[i] = c < count ? weight[c] : 0.0f;
+      v[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+      if (w[i] != 0.0f)  // a part without weight may not be there
+        v[i] = *reinterpret_cast<const f32x4*>(p.part_o + (row0 + c * step + (c == 0 ? late : 0)) * kD + 4 * x);
+    }
+#pragma unroll
+    for (int i = 0; i < kJoinBatch; ++i) o += w[i] * v[i];
+  }
+  acc[g][x] = o;
+  __syncthreads();
+  if (tid >= 32) return;
+  const float den = (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
+  f32x4 sum = acc[0][tid];
+#pragma unroll
+  for (int i = 1; i < kJoinGroups; ++i) sum += acc[i][tid];
   const int tok = r / G;
-  join_row<BF>(
-      p, w1 - w0 + 1,
-      [&](int c) -> int64_t {
-        const int64_t b = share(w0 + c, W);
-        if (b == share(w0 + c + 1, W)) return -1;  // a wave without blocks
-        return ((int64_t)(w0 + c) * 2 + (b < g0 ? 1 : 0)) * R + r;
-      },
-      p.out + ((a + tok) * H * G + h * G + (r - tok * G)) * kD);
+  typename Mx<BF>::t y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(den == 0.0f ? 0.0f : sum[e] / den);
+  *reinterpret_cast<u32x2*>(p.out + ((a + tok) * H * G + h * G + (r - tok * G)) * kD + 4 * tid) =
+      *reinterpret_cast<u32x2*>(y);
 }
 
 // ---------------------------------------------------------------- many query rows
