@@ -10,8 +10,8 @@
 // and written behind its end, the table's read and written entries are disjoint,
 // so nothing waits for anything.  A small call is one workgroup and one launch;
 // a large one spreads slots and pages over workgroups that each recompute the
-// sums (16 bytes a request from L2), and a second launch of one workgroup writes
-// what the first one still reads (state, lengths: the caller's may be in place).
+// sums (16 bytes a request from L2); the first of them writes lengths and state, or, where
+// the caller's are in place and the others still read them, a second launch does.
 //
 // Write.  A copy of rows: 16 lanes take a row's 256 bytes of output, the row's
 // slot gives the page.  Bound by bytes where they are many and by one trip to
@@ -206,21 +206,28 @@ __global__ __launch_bounds__(THREADS) void paged_map_kernel(MapArgs a) {
     }
   }
   if constexpr (FINISH) {
+    if (blockIdx.x == 0) {
+      __syncthreads();  // s_back is done with: it takes the lengths, for stores in order
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int s = tid * kPer + i;
-      if (s >= S) break;
-      const int64_t now = served[i] ? nn[i] : no[i];
-      a.start[s] = first[i];
-      a.n_now[s] = now;
-      if (a.n_unit)
-        for (int h = 0; h < a.H; ++h) a.n_unit[(int64_t)s * a.H + h] = now;
-    }
-    if (tid == 0) {
-      a.start[S] = rows;
-      const int64_t h1 = head + taken;
-      a.state_out[0] = bad_state ? head : h1 >= a.P ? h1 - a.P : h1;
-      a.state_out[1] = bad_state ? a.state[1] : count - taken + back;
+      for (int i = 0; i < kPer; ++i) {
+        const int s = tid * kPer + i;
+        if (s >= S) break;
+        const int64_t now = served[i] ? nn[i] : no[i];
+        a.start[s] = first[i];
+        a.n_now[s] = now;
+        s_back[s] = (int32_t)now;
+      }
+      if (tid == 0) {
+        a.start[S] = rows;
+        const int64_t h1 = head + taken;
+        const int64_t c0 = bad_state ? a.state[1] : count - taken + back;
+        a.state_out[0] = bad_state ? head : h1 >= a.P ? h1 - a.P : h1;
+        a.state_out[1] = c0;
+      }
+      if (a.n_unit) {
+        __syncthreads();
+        for (int u = tid; u < S * a.H; u += THREADS) a.n_unit[u] = s_back[(uint32_t)u / (uint32_t)a.H];
+      }
     }
   }
   if (flags) set_status(a.st, flags);
@@ -241,10 +248,15 @@ fathom_status launch_paged_map(const int64_t* n_old, const int64_t* n, int S, in
   } else if (T <= 8 * kMapThreads) {
     hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, true>), dim3(1), dim3(kMapThreads), lds, s, a);
   } else {
-    const int64_t wgs = T / (4 * kMapThreads) + 1;
-    hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, false>), dim3((unsigned)(wgs < 256 ? wgs : 256)),
-                       dim3(kMapThreads), lds, s, a);
-    hipLaunchKernelGGL((paged_map_kernel<kMapThreads, false, true>), dim3(1), dim3(kMapThreads), lds, s, a);
+    // a slot a thread, over two workgroups a CU at most
+    const int64_t wgs = T / kMapThreads + 1;
+    const dim3 grid((unsigned)(wgs < 512 ? wgs : 512));
+    if (n_now != n_old && n_now != n && state_out != state) {
+      hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, true>), grid, dim3(kMapThreads), lds, s, a);
+    } else {
+      hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, false>), grid, dim3(kMapThreads), lds, s, a);
+      hipLaunchKernelGGL((paged_map_kernel<kMapThreads, false, true>), dim3(1), dim3(kMapThreads), lds, s, a);
+    }
   }
   FATHOM_LAUNCH_CHECK();
   return FATHOM_OK;
