@@ -762,11 +762,12 @@ __device__ __forceinline__ int parts_of(int nb, int nsplit) { return max(min(nsp
 struct ManyTile {
   int s, h, tok0, toks, total, n;  // tokens of the tile and of the request, new and all
   int lo, hi;                      // the union of their ranges
+  int lo_max, hi_min;              // and what all of them see (up to the first token's own position)
   int64_t a;
 };
 
 // Tile and head of a workgroup index (later tiles, which see more, first).  Every thread of
-// 256; red[8] is LDS.
+// 256; red[12] is LDS.
 __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int* before, int tile, int h, int* red) {
   ManyTile t;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tm = kManyRows / p.G;
@@ -779,24 +780,32 @@ __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int*
   t.tok0 = (x - uniform(before[t.s])) * tm;
   t.toks = min(tm, t.total - t.tok0);
   if (!p.first && !p.prefix) {
-    t.lo = 0;
+    t.lo = t.lo_max = 0;
+    t.hi_min = t.n - t.total + t.tok0 + 1;
     t.hi = t.n - t.total + t.tok0 + t.toks;
     return t;
   }
-  int lo = t.n, hi = 0;
-  if (tid < t.toks) token_range(p, t.s, t.a + t.tok0 + tid, t.n - t.total + t.tok0 + tid, t.n, &lo, &hi);
+  int lo = t.n, hi = 0, lo_max = 0;
+  if (tid < t.toks) {
+    token_range(p, t.s, t.a + t.tok0 + tid, t.n - t.total + t.tok0 + tid, t.n, &lo, &hi);
+    lo_max = lo;
+  }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     lo = min(lo, __shfl_xor(lo, o, kWave));
     hi = max(hi, __shfl_xor(hi, o, kWave));
+    lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
   }
   if (lane == 0) {
     red[wave] = lo;
     red[4 + wave] = hi;
+    red[8 + wave] = lo_max;
   }
   __syncthreads();
   t.lo = uniform(min(min(red[0], red[1]), min(red[2], red[3]))) & ~(kManyKeys - 1);
   t.hi = uniform(max(max(red[4], red[5]), max(red[6], red[7])));
+  t.lo_max = uniform(max(max(red[8], red[9]), max(red[10], red[11])));
+  t.hi_min = t.n - t.total + t.tok0 + 1;
   __syncthreads();
   return t;
 }
@@ -1005,16 +1014,8 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
       }
     }
   };
-  auto map_scores = [&](Sv (&s)[2], int key) __attribute__((always_inline)) {
-    if constexpr (MAP != 0) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[c][e] = mapped<MAP == 2>(sm, slope[c], s[c][e], pos[c] - 4 * half - (key + 8 * (e >> 2) + (e & 3)));
-    }
-  };
-  // The same of element e, for keys up to the row's own: the bias is linear in the key.
+  // The mapped score of element e of a half, with a bias linear in the key: it is the bias for
+  // keys up to the row's own (mask_half has the others).
   auto bias_base = [&](int c, int key) __attribute__((always_inline)) { return slope[c] * (float)(key + 4 * half - pos[c]); };
   auto map_seen = [&](float s, int c, int e, float base) __attribute__((always_inline)) -> float {
     const float bias = __builtin_fmaf(slope[c], (float)(8 * (e >> 2) + (e & 3)), base);
@@ -1049,7 +1050,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     for (int c = 0; c < 2; ++c) {
       const float top = fmaxf(mx[c], __shfl_xor(mx[c], 32, kWave));
       const float to = fminf(nr[c], Mx<BF>::kShift - top * c1);
-      f[c] = __builtin_amdgcn_exp2f(to - nr[c]);
+      f[c] = fmaxf(__builtin_amdgcn_exp2f(to - nr[c]), 0x1p-126f);  // not 0: O may hold an infinity
       nr[c] = to;
       l[c] *= f[c];
     }
@@ -1075,78 +1076,82 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     from = from_next;
   };
 
-  // A block (`advance`d to) that some query of the wave does not see whole: a half at a time,
-  // without overlap.  Kept short: a workgroup meets two or three such blocks, and code that
-  // is not in the instruction cache costs more than it does.
-  auto masked_block = [&](int b) __attribute__((always_inline)) {
-    const int key_b = key0 + b * kManyKeys;
-    if (key_b + kManyKeys > n || absent) {  // rows that are not there: V is cleared, a wave its 16
-      const bool in = there(key_b + 16 * wave);
+  // What the rows of the wave do not see of the half at `key` takes no part; `mx` again.
+  auto mask_half = [&](Sv (&s)[2], int key) __attribute__((always_inline)) {
+    if (key >= lo_max && key + 32 <= hi_min && !absent) return;
+    if (MAP != 0 && p.prefix) {  // keys behind the row's own: slope * distance was added, not taken off
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const int row = 16 * wave + 4 * y + (lane >> 4);
-        if (key_b + row >= n || !in)
-          *LDS_AT(u32x4, lds0 + kVRing + stage(b) + row * kRowBytes + 16 * (lane & 15)) = (u32x4){0u, 0u, 0u, 0u};
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-    }
-#pragma unroll 1
-    for (int hf = 0; hf < 2; ++hf) {
-      const int key = key_b + 32 * hf;
-      const uint32_t at = stage(b) + hf * kHalf;
-      scores(at, sa);
-      if (MAP != 0 && !p.prefix) map_half(sa, key);  // (what it gives for keys behind the row's own is masked)
-      else map_scores(sa, key);
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const uint32_t from = lo[c] - key - 4 * half, count = max(hi[c] - lo[c], 0);
+      for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if ((uint32_t)(8 * (e >> 2) + (e & 3)) - from >= count) sa[c][e] = -__builtin_huge_valf();
-      }
-      if (absent) {
-        const bool in0 = there(key), in1 = there(key + 16);
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!(e < 8 ? in0 : in1)) sa[c][e] = -__builtin_huge_valf();
-      }
-      float f[2];
-      maxima(sa);
-      if (raise(f)) rescale(f);
-      exponentials(sa, pa);
-      const bool clean = any_nonfinite<BF, kHalf>(lds0 + kVRing + at);
-      if (clean) {
-#pragma unroll 1
-        for (int row = 0; row < 32; ++row) {
-          const int k = key + row;
-          const bool in = there(k);
-          const bool sees[2] = {in && k >= lo[0] && k < hi[0], in && k >= lo[1] && k < hi[1]};
-#pragma unroll
-          for (int y = 0; y < 16; ++y) {  // channels 8 y + 4 half ..
-            const s16x4 x = *LDS_AT(const s16x4, lds0 + kVRing + at + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float add = nonfinite_part<BF>(x[e]);
-#pragma unroll
-              for (int c = 0; c < 2; ++c) o[c][y >> 2][4 * (y & 3) + e] += sees[c] ? add : 0.0f;
-            }
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          v8 vf = v_frag(at, 4 * i + d);
-          if (clean) vf = __builtin_bit_cast(v8, finite_part<BF>(__builtin_bit_cast(s16x8, vf)));
-#pragma unroll
-          for (int c = 0; c < 2; ++c) o[c][d] = Mx<BF>::mfma32(vf, __builtin_bit_cast(v8, pa[c][i]), o[c][d]);
-        }
+          s[c][e] = __builtin_fmaf(-2.0f * slope[c], (float)max(key + 8 * (e >> 2) + 4 * half + (e & 3) - pos[c], 0), s[c][e]);
     }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint32_t from = lo[c] - key - 4 * half, count = max(hi[c] - lo[c], 0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if ((uint32_t)(8 * (e >> 2) + (e & 3)) - from >= count) s[c][e] = -__builtin_huge_valf();
+    }
+    if (absent) {
+      const bool in0 = there(key), in1 = there(key + 16);
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(e < 8 ? in0 : in1)) s[c][e] = -__builtin_huge_valf();
+    }
+    maxima(s);
+  };
+  // A block that not every query of the workgroup sees whole: V's rows that are not there are
+  // cleared, and of values that are not finite the product takes none: they go to O of the
+  // queries that see them before the block's V is cleared of them.
+  auto prepare = [&](int b) __attribute__((always_inline)) {
+    const int key_b = key0 + b * kManyKeys;
+    if (key_b >= t.lo_max && key_b + kManyKeys <= t.hi_min && !absent) return;
+    const uint32_t v0 = lds0 + kVRing + stage(b), rows16 = v0 + wave * 4096;
+    const bool in = there(key_b + 16 * wave);
+    if (key_b + 16 * wave + 16 > n || !in) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const int row = 4 * y + (lane >> 4);
+        if (key_b + 16 * wave + row >= n || !in)
+          *LDS_AT(u32x4, rows16 + row * kRowBytes + 16 * (lane & 15)) = (u32x4){0u, 0u, 0u, 0u};
+      }
+    }
+    const bool bad = any_nonfinite<BF, 4096>(rows16);
+    if (lane == 0) red[wave] = bad;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (!uniform(red[0] | red[1] | red[2] | red[3])) return;
+#pragma unroll 1
+    for (int row = 0; row < kManyKeys; ++row) {
+      const int k = key_b + row;
+      const bool has = there(k);
+      const bool sees[2] = {has && k >= lo[0] && k < hi[0], has && k >= lo[1] && k < hi[1]};
+#pragma unroll
+      for (int y = 0; y < 16; ++y) {  // channels 8 y + 4 half ..
+        const s16x4 x = *LDS_AT(const s16x4, v0 + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float add = nonfinite_part<BF>(x[e]);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) o[c][y >> 2][4 * (y & 3) + e] += sees[c] ? add : 0.0f;
+        }
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const uint32_t mine = rows16 + y * 1024 + 16 * lane;
+      *LDS_AT(s16x8, mine) = finite_part<BF>(*LDS_AT(const s16x8, mine));
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
 
   // A half step: the exponentials of `s` to P, the scores of the next half (K at byte `kat`) to
@@ -1215,51 +1220,44 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     ka = fr[16];
     kb = fr[17];
   };
-  // Blocks [f0, f1) are seen whole by every query of the wave.
-  const int f0 = absent ? nb : min(max((lo_max - key0 + kManyKeys - 1) / kManyKeys, 0), nb);
-  const int f1 = max(f0, min((hi_min - key0) / kManyKeys, nb));
-#pragma unroll 1
-  for (int b = 0; b < f0; ++b) {
-    advance(b);
-    masked_block(b);
-  }
-  if (f0 < f1) {
-    int b = f0;
-    advance(b);
+  if (nb > 0) {
     float f[2];
-    scores(stage(b), sa);
-    map_half(sa, key0 + b * kManyKeys);
+    int b = 0;
+    advance(0);
+    prepare(0);
+    scores(stage(0), sa);
+    map_half(sa, key0);
     maxima(sa);
-    if (raise(f)) rescale(f);
-    scores(stage(b) + kHalf, sb);
+    mask_half(sa, key0);
+    raise(f);  // (O is 0, or infinite)
+    scores(stage(0) + kHalf, sb);
     exponentials(sa, pa);
-    map_half(sb, key0 + b * kManyKeys + 32);
+    map_half(sb, key0 + 32);
     // where it is raised, the product that is still to come is in the old scale: O follows after it
     maxima(sb);
+    mask_half(sb, key0 + 32);
     bool up = raise(f);
-    v8 ka = k_frag(stage(b + 1), 0), kb = k_frag(stage(b + 1), 1);
+    v8 ka = k_frag(stage(1), 0), kb = k_frag(stage(1), 1);
     // the second half of block b, the first half of block b + 1
 #pragma unroll 1
-    for (; b + 1 < f1; ++b) {
+    for (; b + 1 < nb; ++b) {
       const uint32_t s0 = stage(b), s1 = stage(b + 1), s2 = stage(b + 2);
       const int key = key0 + (b + 1) * kManyKeys;
       half_step(sb, pb, s1, sa, key, s0, pa, ka, kb, s1 + kHalf);
       if (up) rescale(f);
+      mask_half(sa, key);
       up = raise(f);
       advance(b + 1);
+      prepare(b + 1);
       half_step(sa, pa, s1 + kHalf, sb, key + 32, s0 + kHalf, pb, ka, kb, s2);
       if (up) rescale(f);
+      mask_half(sb, key + 32);
       up = raise(f);
     }
     product(stage(b), pa);
     if (up) rescale(f);
     exponentials(sb, pb);
     product(stage(b) + kHalf, pb);
-  }
-#pragma unroll 1
-  for (int b = f1; b < nb; ++b) {
-    advance(b);
-    masked_block(b);
   }
 
   // ---- the output, or a part of it ----
