@@ -53,10 +53,11 @@ constexpr int kFewKeys = 32;      // keys a step of a wave
 constexpr int kFewWaves = 4;
 constexpr int kFewWorkers = 1024; // waves: one workgroup of 128 KB of LDS on each of 256 CUs
 constexpr int kFewStage = 2 * kFewKeys * kRowBytes;
-constexpr int kManyRows = 256;    // query rows of a workgroup, 64 a wave
-constexpr int kManyKeys = 64;
-constexpr int kManyStage = 2 * kManyKeys * kRowBytes;
-constexpr int kManyStages = 4;
+// attn_many_kernel<CT>: column tiles of 32 query rows that a wave holds, 1 or 2
+constexpr int kManyKeys = 64;     // keys are divided among workgroups by these
+constexpr int kManyStages = 4;    // blocks of 32 CT keys in each of the rings of K and V
+constexpr int many_rows(int ct) { return 128 * ct; }  // query rows of a workgroup
+constexpr int many_lds(int ct) { return 2 * kManyStages * 32 * ct * kRowBytes; }
 constexpr int kNone = -(1 << 30);
 
 struct PagedAttnArgs {
@@ -116,18 +117,32 @@ __device__ __forceinline__ void token_range(const PagedAttnArgs& p, int s, int64
 }
 
 // ---------------------------------------------------------------- tools
-// 16 rows, four of 64 lanes x 16 bytes at a time: rows 4y .. 4y + 3 from base + 1024 y + off[y]
-// (a lane's) to LDS at `lds` + 1024 y + 16 lane; an instruction's offset counts on both sides.
-// The wait is the caller's (vmcnt); no register is written.
-__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, const uint32_t (&off)[4]) {
-  asm volatile(
-      "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, %5\n\t"
-      "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-      "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-      "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds),
-      "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base)
-      : "memory");
+// Rows, four of 64 lanes x 16 bytes at a time, 2 or 4 times: rows 4y .. 4y + 3 from base +
+// 1024 y + off[y] (a lane's) to LDS at `lds` + 1024 y + 16 lane; an instruction's offset counts
+// on both sides.  The wait is the caller's (vmcnt); no register is written.
+template <int N>
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* from, const uint32_t (&off)[N]) {
+  const uint64_t at = reinterpret_cast<uint64_t>(from);
+  const uint64_t base = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32) |
+                        (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+  lds = __builtin_amdgcn_readfirstlane((int)lds);
+  if constexpr (N == 4) {
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %5\n\t"
+        "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds),
+        "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base)
+        : "memory");
+  } else {
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %3\n\t"
+        "global_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds),
+        "v"(off[0]), "v"(off[1]), "s"(base)
+        : "memory");
+  }
 }
 
 template <int N>
@@ -726,11 +741,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
 }
 
 // ---------------------------------------------------------------- many query rows
-// Row tiles of the requests with more than `few` query rows: before[s] those of the
+// Row tiles, of tm tokens, of the requests with more than `few` query rows: before[s] those of the
 // requests before s.
-__device__ __forceinline__ void many_plan(const PagedAttnArgs& p, int* before, int* part, uint32_t& flags) {
+__device__ __forceinline__ void many_plan(const PagedAttnArgs& p, int tm, int* before, int* part, uint32_t& flags) {
   const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (p.S + nt - 1) / nt, tm = kManyRows / p.G;
+  const int per = (p.S + nt - 1) / nt;
   int sum = 0;
   for (int i = 0; i < per; ++i) {
     const int s = tid * per + i;
@@ -768,9 +783,10 @@ struct ManyTile {
 
 // Tile and head of a workgroup index (later tiles, which see more, first).  Every thread of
 // 256; red[12] is LDS.
-__device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, const int* before, int tile, int h, int* red) {
+__device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, int tm, const int* before, int tile, int h,
+                                              int* red) {
   ManyTile t;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tm = kManyRows / p.G;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int x = before[p.S] - 1 - tile;
   t.s = uniform(request_of(before, p.S, x));
   t.h = h;
@@ -828,25 +844,28 @@ struct Scores16 {
 
 // MAP: 0 the scaled score, 1 with a bias (and for scales below 0), 2 capped.
 
-template <bool BF, int MAP>
-__global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
+template <bool BF, int MAP, int CT>
+__global__ __launch_bounds__(256, CT == 1 ? 2 : 1) void attn_many_kernel(PagedAttnArgs p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef typename Mx<BF>::v8 v8;
   typedef typename Mx<BF>::t vt;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5, lr = lane & 31;
-  int* before = reinterpret_cast<int*>(smem + kManyStages * kManyStage);
+  int* before = reinterpret_cast<int*>(smem + many_lds(CT));
   int* red = before + p.S + 1;
   uint32_t flags = 0;
-  many_plan(p, before, red, flags);
+  many_plan(p, many_rows(CT) / p.G, before, red, flags);
   if (flags && blockIdx.x == 0) set_status(p.st, flags);
   const int H = p.c.H, G = p.G;
   const int bid = blockIdx.x, h = bid % H, part = (bid / H) % p.nsplit, tile = bid / H / p.nsplit;
   if (tile >= before[p.S]) return;
-  const ManyTile t = many_tile(p, before, tile, h, red);
+  const ManyTile t = many_tile(p, many_rows(CT) / G, before, tile, h, red);
   const int all = max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 0), parts = parts_of(all, p.nsplit);
   if (part >= parts) return;
-  const int b0 = (int)((int64_t)all * part / parts), nb = (int)((int64_t)all * (part + 1) / parts) - b0;
-  const int key0 = t.lo + b0 * kManyKeys, n = t.n;
+  const int from64 = (int)((int64_t)all * part / parts), count64 = (int)((int64_t)all * (part + 1) / parts) - from64;
+  // blocks of 32 CT keys, halves of 32 (CT 1: a block is a half; their number is even)
+  constexpr int kKeys = 32 * CT;
+  constexpr uint32_t kHalf = 32 * kRowBytes;
+  const int nb = count64 * (kManyKeys / kKeys), key0 = t.lo + from64 * kManyKeys, n = t.n;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))smem;
   const int rows = t.toks * G;
 
@@ -856,51 +875,53 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     return !absent || (uint32_t)page_of(p.c, t.s, min(k, n - 1) >> p.c.shift) < (uint32_t)p.c.P;
   };
 
-  // ---- loads: wave w takes keys 16w .. 16w + 15 of a block ----
+  // ---- loads: wave w takes keys 8 CT w .. 8 CT (w + 1) - 1 of a block ----
   const uint32_t row_step = (uint32_t)p.c.ld_tok * 2;
-  uint32_t koff[4], voff[4];
+  uint32_t koff[2 * CT], voff[2 * CT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = 4 * i + (lane >> 4);
-    koff[i] = row * row_step + 16 * k_chunk(row, lane & 15) - 1024 * i;  // 4 rows are 1024 bytes at least
-    voff[i] = row * row_step + 16 * v_chunk(row, lane & 15) - 1024 * i;
+  for (int i = 0; i < 2 * CT; ++i) {
+    const int row = 4 * i + (lane >> 4), at = 8 * CT * wave + row;
+    koff[i] = row * row_step + 16 * k_chunk(at, lane & 15) - 1024 * i;  // 4 rows are 1024 bytes at least
+    voff[i] = row * row_step + 16 * v_chunk(at, lane & 15) - 1024 * i;
   }
   // Where the wave's keys of block b begin in a pool; page 0 where there is none.
   const uint16_t *Kh = p.c.K + (int64_t)h * p.c.ld_head, *Vh = p.c.V + (int64_t)h * p.c.ld_head;
   auto page = [&](int b) __attribute__((always_inline)) -> int {
-    const int k = key0 + b * kManyKeys + 16 * wave;
+    const int k = key0 + b * kKeys + 8 * CT * wave;
     return b < nb && k < n ? page_uniform(p.c, t.s, k >> p.c.shift) : 0;
   };
   auto place = [&](int b, int id) __attribute__((always_inline)) -> int64_t {
-    const int k = key0 + b * kManyKeys + 16 * wave;
+    const int k = key0 + b * kKeys + 8 * CT * wave;
     return (int64_t)((uint32_t)id < (uint32_t)p.c.P ? id : 0) * p.c.ld_page +
            (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
   };
-  auto stage = [](int b) __attribute__((always_inline)) -> uint32_t {
-    return (uint32_t)(b % kManyStages) * (kManyStage / 2);
-  };
-  constexpr uint32_t kVRing = kManyStages * (kManyStage / 2);  // V's stages behind K's
-  const uint32_t mine = lds0 + wave * 4096;
-  // K runs three blocks ahead of what is in use, V two: a block's V is read half a block
-  // after its K.  Blocks behind the last are loaded from page 0 and not used, so that the
-  // number of loads in flight is always the same.
-  int64_t from = place(0, page(0)), from_next = place(1, page(1));
-  load_to_lds(mine + stage(0), Kh + from, koff);
-  load_to_lds(mine + stage(1), Kh + from_next, koff);
-  load_to_lds(mine + kVRing + stage(0), Vh + from, voff);
-  from = place(2, page(2));
-  load_to_lds(mine + stage(2), Kh + from, koff);
-  load_to_lds(mine + kVRing + stage(1), Vh + from_next, voff);
-  int id_next = page(3);
+  auto stage = [](int b) __attribute__((always_inline)) -> uint32_t { return (uint32_t)(b % kManyStages) * CT * kHalf; };
+  constexpr uint32_t kVRing = many_lds(CT) / 2;  // V's stages behind K's
+  const uint32_t mine = lds0 + wave * (2048 * CT);
+  // `advance(b)` issues K of block b + kAhead and V of block b + 2, in stages that are read by
+  // then (with two halves a block, K of block b is still in use).  Blocks behind the last are
+  // loaded from page 0 and not used, so that the number of loads in flight is always the same.
+  constexpr int kAhead = CT == 1 ? 4 : 3;
+  int64_t from[kAhead];  // places of blocks b + 2 .. b + kAhead + 1, before advance(b)
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) from[i] = place(i, page(i));
+#pragma unroll
+  for (int i = 0; i < kAhead - 1; ++i) load_to_lds(mine + stage(i), Kh + from[i], koff);
+  load_to_lds(mine + kVRing + stage(0), Vh + from[0], voff);
+  load_to_lds(mine + stage(kAhead - 1), Kh + from[kAhead - 1], koff);
+  load_to_lds(mine + kVRing + stage(1), Vh + from[1], voff);
+#pragma unroll
+  for (int i = 0; i + 2 < kAhead; ++i) from[i] = from[i + 2];
+  int id_next = page(kAhead);
 
-  // ---- the wave's 64 query rows: column tiles of 32 ----
-  v8 qf[2][8];
-  int pos[2], lo[2], hi[2], lo_max = 0, hi_min = n;
-  float slope[2];
+  // ---- the wave's query rows: column tiles of 32 ----
+  v8 qf[CT][8];
+  int pos[CT], lo[CT], hi[CT], lo_max = 0, hi_min = n;
+  float slope[CT];
   const ScoreMap sm = score_map(p);
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int r = wave * 64 + c * 32 + lr, tok = r / G, g = r - tok * G;
+  for (int c = 0; c < CT; ++c) {
+    const int r = (wave * CT + c) * 32 + lr, tok = r / G, g = r - tok * G;
     pos[c] = 0;
     lo[c] = 0;
     hi[c] = n;
@@ -921,7 +942,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     }
   }
   if (!p.prefix && !p.first) {  // the wave's first token
-    hi_min = wave * 64 < rows ? n - t.total + t.tok0 + wave * 64 / G + 1 : n;
+    hi_min = wave * CT * 32 < rows ? n - t.total + t.tok0 + wave * CT * 32 / G + 1 : n;
   } else {
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) {
@@ -933,7 +954,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   hi_min = uniform(hi_min);
   // ---- absent pages among the keys: their blocks are masked throughout ----
   {
-    const int e1 = min(key0 + nb * kManyKeys, n);
+    const int e1 = min(key0 + nb * kKeys, n);
     for (int k = key0 + 16 * tid; k < e1; k += 16 * 256)
       absent |= (uint32_t)page_of(p.c, t.s, k >> p.c.shift) >= (uint32_t)p.c.P;
     if (lane == 0) red[wave] = 0;
@@ -953,17 +974,16 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     const int r0 = 4 * half + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     vaddr = lds0 + kVRing + r0 * kRowBytes + 16 * v_chunk(r0, ch) + 8 * (lane & 1);
   }
-  constexpr uint32_t kHalf = 32 * kRowBytes;
 
   typedef std::conditional_t<MAP == 0, f32x16, Scores16> Sv;
-  f32x16 o[2][4];
-  Sv sa[2], sb[2];
-  u32x4 pa[2][2], pb[2][2];
+  f32x16 o[CT][4];
+  Sv sa[CT], sb[CT];
+  u32x4 pa[CT][2], pb[CT][2];
   // l: sums of the probabilities; nr: kShift less the reference that they are taken against (in
   // log2; at first a reference that every score raises and against which -Inf gives 0)
-  float nr[2], l[2];
+  float nr[CT], l[CT];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
+  for (int c = 0; c < CT; ++c) {
     nr[c] = 1e37f;
     l[c] = 0.0f;
 #pragma unroll
@@ -977,33 +997,33 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     return join4<v8>(lds_tr(va), lds_tr(va + 8 * kRowBytes));
   };
   // S^T of the 32 keys at byte `at` of K's ring
-  auto scores = [&](uint32_t at, Sv (&s)[2]) __attribute__((always_inline)) {
-    f32x16 acc[2] = {};
+  auto scores = [&](uint32_t at, Sv (&s)[CT]) __attribute__((always_inline)) {
+    f32x16 acc[CT] = {};
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) {
       const v8 kf = k_frag(at, kk);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) acc[c] = Mx<BF>::mfma32(kf, qf[c][kk], acc[c]);
+      for (int c = 0; c < CT; ++c) acc[c] = Mx<BF>::mfma32(kf, qf[c][kk], acc[c]);
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < CT; ++c)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[c][e] = acc[c][e];
   };
   // O^T += V^T P^T of the 32 keys at byte `at` of V's ring
-  auto product = [&](uint32_t at, const u32x4 (&pr)[2][2]) __attribute__((always_inline)) {
+  auto product = [&](uint32_t at, const u32x4 (&pr)[CT][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         const v8 vf = v_frag(at, 4 * i + d);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) o[c][d] = Mx<BF>::mfma32(vf, __builtin_bit_cast(v8, pr[c][i]), o[c][d]);
+        for (int c = 0; c < CT; ++c) o[c][d] = Mx<BF>::mfma32(vf, __builtin_bit_cast(v8, pr[c][i]), o[c][d]);
       }
   };
-  auto exponentials = [&](const Sv (&s)[2], u32x4 (&pr)[2][2]) __attribute__((always_inline)) {
+  auto exponentials = [&](const Sv (&s)[CT], u32x4 (&pr)[CT][2]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < CT; ++c) {
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
         const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
@@ -1022,18 +1042,18 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     if constexpr (MAP == 1) return __builtin_fmaf(s, sm.c1, bias);
     return mapped<true>(sm, 0.0f, s, 0) + bias;
   };
-  auto map_half = [&](Sv (&s)[2], int key) __attribute__((always_inline)) {
+  auto map_half = [&](Sv (&s)[CT], int key) __attribute__((always_inline)) {
     if constexpr (MAP != 0) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[c][e] = map_seen(s[c][e], c, e, bias_base(c, key));
     }
   };
-  float mx[2];  // the lane's maxima of a half's scores
-  auto maxima = [&](const Sv (&s)[2]) __attribute__((always_inline)) {
+  float mx[CT];  // the lane's maxima of a half's scores
+  auto maxima = [&](const Sv (&s)[CT]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < CT; ++c) {
       mx[c] = fmaxf(s[c][0], s[c][1]);
 #pragma unroll
       for (int e = 2; e < 16; e += 2) mx[c] = fmaxf(fmaxf(mx[c], s[c][e]), s[c][e + 1]);
@@ -1041,13 +1061,13 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   };
   // Where one exceeds the reference by kSlack: the reference becomes the maximum of the row's
   // scores, l follows, and f is the factor for O.
-  auto raise = [&](float (&f)[2]) __attribute__((always_inline)) -> bool {
+  auto raise = [&](float (&f)[CT]) __attribute__((always_inline)) -> bool {
     bool up = false;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) up |= __builtin_fmaf(mx[c], c1, nr[c]) > kSlack + Mx<BF>::kShift;
+    for (int c = 0; c < CT; ++c) up |= __builtin_fmaf(mx[c], c1, nr[c]) > kSlack + Mx<BF>::kShift;
     if (!__ballot(up)) return false;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < CT; ++c) {
       const float top = fmaxf(mx[c], __shfl_xor(mx[c], 32, kWave));
       const float to = fminf(nr[c], Mx<BF>::kShift - top * c1);
       f[c] = fmaxf(__builtin_amdgcn_exp2f(to - nr[c]), 0x1p-126f);  // not 0: O may hold an infinity
@@ -1056,38 +1076,38 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     }
     return true;
   };
-  auto rescale = [&](const float (&f)[2]) __attribute__((always_inline)) {
+  auto rescale = [&](const float (&f)[CT]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < CT; ++c)
 #pragma unroll
       for (int d = 0; d < 4; ++d) o[c][d] *= f[c];
   };
-  // K of block b + 1 and V of block b are in LDS once all but the last 8 loads are done; what
-  // this wave has read of K's stage b - 1 and V's b - 2 is read.
+  // Block b is begun: its V, its K and the K that is read up to the next call are in LDS once
+  // all but what the last call issued is; what this wave has read of the stages is read.
   auto advance = [&](int b) __attribute__((always_inline)) {
-    wait_vm<8>();
+    wait_vm<4 * CT>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    from_next = place(b + 3, id_next);
-    id_next = page(b + 4);
-    load_to_lds(mine + stage(b + 3), Kh + from_next, koff);
-    load_to_lds(mine + kVRing + stage(b + 2), Vh + from, voff);
-    from = from_next;
+    from[kAhead - 2] = place(b + kAhead, id_next);
+    id_next = page(b + kAhead + 1);
+    load_to_lds(mine + stage(b + kAhead), Kh + from[kAhead - 2], koff);
+    load_to_lds(mine + kVRing + stage(b + 2), Vh + from[0], voff);
+#pragma unroll
+    for (int i = 0; i + 1 < kAhead - 1; ++i) from[i] = from[i + 1];
   };
-
   // What the rows of the wave do not see of the half at `key` takes no part; `mx` again.
-  auto mask_half = [&](Sv (&s)[2], int key) __attribute__((always_inline)) {
+  auto mask_half = [&](Sv (&s)[CT], int key) __attribute__((always_inline)) {
     if (key >= lo_max && key + 32 <= hi_min && !absent) return;
     if (MAP != 0 && p.prefix) {  // keys behind the row's own: slope * distance was added, not taken off
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           s[c][e] = __builtin_fmaf(-2.0f * slope[c], (float)max(key + 8 * (e >> 2) + 4 * half + (e & 3) - pos[c], 0), s[c][e]);
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < CT; ++c) {
       const uint32_t from = lo[c] - key - 4 * half, count = max(hi[c] - lo[c], 0);
 #pragma unroll
       for (int e = 0; e < 16; ++e)
@@ -1096,7 +1116,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     if (absent) {
       const bool in0 = there(key), in1 = there(key + 16);
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (!(e < 8 ? in0 : in1)) s[c][e] = -__builtin_huge_valf();
@@ -1107,29 +1127,32 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   // cleared, and of values that are not finite the product takes none: they go to O of the
   // queries that see them before the block's V is cleared of them.
   auto prepare = [&](int b) __attribute__((always_inline)) {
-    const int key_b = key0 + b * kManyKeys;
-    if (key_b >= t.lo_max && key_b + kManyKeys <= t.hi_min && !absent) return;
-    const uint32_t v0 = lds0 + kVRing + stage(b), rows16 = v0 + wave * 4096;
-    const bool in = there(key_b + 16 * wave);
-    if (key_b + 16 * wave + 16 > n || !in) {
+    const int key_b = key0 + b * kKeys;
+    if (key_b >= t.lo_max && key_b + kKeys <= t.hi_min && !absent) return;
+    const uint32_t v0 = lds0 + kVRing + stage(b), own = v0 + wave * (2048 * CT);
+    const int key_w = key_b + 8 * CT * wave;
+    const bool in = there(key_w);
+    if (key_w + 8 * CT > n || !in) {
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
+      for (int y = 0; y < 2 * CT; ++y) {
         const int row = 4 * y + (lane >> 4);
-        if (key_b + 16 * wave + row >= n || !in)
-          *LDS_AT(u32x4, rows16 + row * kRowBytes + 16 * (lane & 15)) = (u32x4){0u, 0u, 0u, 0u};
+        if (key_w + row >= n || !in)
+          *LDS_AT(u32x4, own + row * kRowBytes + 16 * (lane & 15)) = (u32x4){0u, 0u, 0u, 0u};
       }
     }
-    const bool bad = any_nonfinite<BF, 4096>(rows16);
+    const bool bad = any_nonfinite<BF, 2048 * CT>(own);
     if (lane == 0) red[wave] = bad;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (!uniform(red[0] | red[1] | red[2] | red[3])) return;
 #pragma unroll 1
-    for (int row = 0; row < kManyKeys; ++row) {
+    for (int row = 0; row < kKeys; ++row) {
       const int k = key_b + row;
       const bool has = there(k);
-      const bool sees[2] = {has && k >= lo[0] && k < hi[0], has && k >= lo[1] && k < hi[1]};
+      bool sees[CT];
+#pragma unroll
+      for (int c = 0; c < CT; ++c) sees[c] = has && k >= lo[c] && k < hi[c];
 #pragma unroll
       for (int y = 0; y < 16; ++y) {  // channels 8 y + 4 half ..
         const s16x4 x = *LDS_AT(const s16x4, v0 + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
@@ -1137,7 +1160,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
         for (int e = 0; e < 4; ++e) {
           const float add = nonfinite_part<BF>(x[e]);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) o[c][y >> 2][4 * (y & 3) + e] += sees[c] ? add : 0.0f;
+          for (int c = 0; c < CT; ++c) o[c][y >> 2][4 * (y & 3) + e] += sees[c] ? add : 0.0f;
         }
       }
     }
@@ -1145,9 +1168,9 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const uint32_t mine = rows16 + y * 1024 + 16 * lane;
-      *LDS_AT(s16x8, mine) = finite_part<BF>(*LDS_AT(const s16x8, mine));
+    for (int y = 0; y < 2 * CT; ++y) {
+      const uint32_t at = own + y * 1024 + 16 * lane;
+      *LDS_AT(s16x8, at) = finite_part<BF>(*LDS_AT(const s16x8, at));
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -1160,20 +1183,20 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
   // two, in `ka` and `kb`, for the step after, K at `kafter`), and of two exponentials with
   // what belongs to them: a wave alone on its SIMD issues about as long as the two matrix
   // instructions run.
-  auto half_step = [&](const Sv (&s)[2], u32x4 (&pr)[2][2], uint32_t kat, Sv (&sn)[2], int key_next, uint32_t vat,
-                       const u32x4 (&pp)[2][2], v8& ka, v8& kb, uint32_t kafter) __attribute__((always_inline)) {
+  auto half_step = [&](const Sv (&s)[CT], u32x4 (&pr)[CT][2], uint32_t kat, Sv (&sn)[CT], int key_next, uint32_t vat,
+                       const u32x4 (&pp)[CT][2], v8& ka, v8& kb, uint32_t kafter) __attribute__((always_inline)) {
     v8 fr[18];
-    f32x16 acc[2];
+    f32x16 acc[CT];
     float base = 0.0f;
     asm volatile("" : "+v"(kaddr), "+v"(vaddr));  // (else twelve addresses stay in registers)
     fr[0] = ka;
     fr[1] = kb;
-    // once the scores are complete, from the 20th of 32 matrix instructions on: map them, and
-    // the lane's maxima, a pair or two at a time
+    // once the scores are complete, from five eighths of the matrix instructions on: map them,
+    // and the lane's maxima, a pair or two at a time
     auto last_max = [&](auto place) __attribute__((always_inline)) {
-      constexpr int at = decltype(place)::value - 20;
+      constexpr int at = decltype(place)::value - 10 * CT, one = 4 * CT;
       if constexpr (at >= 0) {
-        constexpr int first = at < 8 ? at : 8 + 2 * (at - 8), last = at < 8 ? at + 1 : first + 2;
+        constexpr int first = at < one ? at : one + 2 * (at - one), last = at < one ? at + 1 : first + 2;
         static_for<first, last>([&](auto two) __attribute__((always_inline)) {
           constexpr int cc = decltype(two)::value >> 3, ee = 2 * (decltype(two)::value & 7);
           if constexpr (MAP == 0) {
@@ -1189,82 +1212,114 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
         });
       }
     };
+    float even = 0.0f;
     static_for<0, 16>([&](auto piece) __attribute__((always_inline)) {
       constexpr int j = decltype(piece)::value;
       if constexpr (j < 6) fr[j + 2] = k_frag(kat, j + 2);
       else if constexpr (j < 14) fr[j + 2] = v_frag(vat, j - 6);
       else fr[j + 2] = k_frag(kafter, j - 14);
-      constexpr int c = j >> 3, e = 2 * (j & 7), i = (j - 8) >> 2, d = j & 3;
-      const f32x16 zero = {};
-      if constexpr (j < 8) acc[0] = Mx<BF>::mfma32(fr[j], qf[0][j], j == 0 ? zero : acc[0]);
-      else o[0][d] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[0][i]), o[0][d]);
-      const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
-      last_max(std::integral_constant<int, 2 * j>());
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (j < 8) acc[1] = Mx<BF>::mfma32(fr[j], qf[1][j], j == 0 ? zero : acc[1]);
-      else o[1][d] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[1][i]), o[1][d]);
-      const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, nr[c]));
-      const typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
-      l[c] = Mx<BF>::add_pair(pair, l[c]);
-      // pinned: the compiler would move it to where it is used, behind the branch
-      uint32_t word = __builtin_bit_cast(uint32_t, pair);
-      asm volatile("" : "+v"(word), "+v"(l[c]));
-      pr[c][e >> 3][(e & 7) >> 1] = word;
-      last_max(std::integral_constant<int, 2 * j + 1>());
-      __builtin_amdgcn_sched_barrier(0);
+      static_for<0, CT>([&](auto tile) __attribute__((always_inline)) {
+        constexpr int ct = decltype(tile)::value, at = CT * j + ct;  // matrix instruction; element of s
+        constexpr int c = at >> 4, e = at & 15;
+        const f32x16 zero = {};
+        if constexpr (j < 8) {
+          acc[ct] = Mx<BF>::mfma32(fr[j], qf[ct][j], j == 0 ? zero : acc[ct]);
+        } else {
+          constexpr int i = (j - 8) >> 2, d = j & 3;
+          o[ct][d] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[ct][i]), o[ct][d]);
+        }
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
+        if constexpr (e % 2 == 0) {
+          even = x;
+        } else {
+          const typename Mx<BF>::v2 pair = {(vt)even, (vt)x};
+          l[c] = Mx<BF>::add_pair(pair, l[c]);
+          // pinned: the compiler would move it to where it is used, behind the branch
+          uint32_t word = __builtin_bit_cast(uint32_t, pair);
+          asm volatile("" : "+v"(word), "+v"(l[c]));
+          pr[c][e >> 3][(e & 7) >> 1] = word;
+        }
+        last_max(std::integral_constant<int, at>());
+        __builtin_amdgcn_sched_barrier(0);
+      });
     });
     if constexpr (MAP == 0) {
-      sn[0] = acc[0];
-      sn[1] = acc[1];
+#pragma unroll
+      for (int c = 0; c < CT; ++c) sn[c] = acc[c];
     }
     ka = fr[16];
     kb = fr[17];
   };
   if (nb > 0) {
-    float f[2];
+    float f[CT];
     int b = 0;
+    if constexpr (CT == 1) {  // K of block 4 takes the stage of block 0's
+      wait_vm<4>();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      scores(stage(0), sa);
+    }
     advance(0);
     prepare(0);
-    scores(stage(0), sa);
+    if constexpr (CT == 2) scores(stage(0), sa);
     map_half(sa, key0);
     maxima(sa);
     mask_half(sa, key0);
     raise(f);  // (O is 0, or infinite)
-    scores(stage(0) + kHalf, sb);
+    scores(CT == 1 ? stage(1) : stage(0) + kHalf, sb);
     exponentials(sa, pa);
     map_half(sb, key0 + 32);
-    // where it is raised, the product that is still to come is in the old scale: O follows after it
     maxima(sb);
     mask_half(sb, key0 + 32);
+    // where it is raised, the product that is still to come is in the old scale: O follows after it
     bool up = raise(f);
-    v8 ka = k_frag(stage(1), 0), kb = k_frag(stage(1), 1);
-    // the second half of block b, the first half of block b + 1
+    v8 ka = k_frag(stage(3 - CT), 0), kb = k_frag(stage(3 - CT), 1);
+    if constexpr (CT == 1) {
 #pragma unroll 1
-    for (; b + 1 < nb; ++b) {
-      const uint32_t s0 = stage(b), s1 = stage(b + 1), s2 = stage(b + 2);
-      const int key = key0 + (b + 1) * kManyKeys;
-      half_step(sb, pb, s1, sa, key, s0, pa, ka, kb, s1 + kHalf);
-      if (up) rescale(f);
-      mask_half(sa, key);
-      up = raise(f);
-      advance(b + 1);
-      prepare(b + 1);
-      half_step(sa, pa, s1 + kHalf, sb, key + 32, s0 + kHalf, pb, ka, kb, s2);
-      if (up) rescale(f);
-      mask_half(sb, key + 32);
-      up = raise(f);
+      for (b = 1; b + 1 < nb; b += 2) {  // halves b and b + 1
+        advance(b);
+        prepare(b);
+        half_step(sb, pb, stage(b + 1), sa, key0 + 32 * (b + 1), stage(b - 1), pa, ka, kb, stage(b + 2));
+        if (up) rescale(f);
+        mask_half(sa, key0 + 32 * (b + 1));
+        up = raise(f);
+        advance(b + 1);
+        prepare(b + 1);
+        half_step(sa, pa, stage(b + 2), sb, key0 + 32 * (b + 2), stage(b), pb, ka, kb, stage(b + 3));
+        if (up) rescale(f);
+        mask_half(sb, key0 + 32 * (b + 2));
+        up = raise(f);
+      }
+      advance(b);
+      prepare(b);
+    } else {
+#pragma unroll 1
+      for (; b + 1 < nb; ++b) {  // the second half of block b, the first half of block b + 1
+        const uint32_t s0 = stage(b), s1 = stage(b + 1), s2 = stage(b + 2);
+        const int key = key0 + (b + 1) * kKeys;
+        half_step(sb, pb, s1, sa, key, s0, pa, ka, kb, s1 + kHalf);
+        if (up) rescale(f);
+        mask_half(sa, key);
+        up = raise(f);
+        advance(b + 1);
+        prepare(b + 1);
+        half_step(sa, pa, s1 + kHalf, sb, key + 32, s0 + kHalf, pb, ka, kb, s2);
+        if (up) rescale(f);
+        mask_half(sb, key + 32);
+        up = raise(f);
+      }
     }
-    product(stage(b), pa);
+    product(CT == 1 ? stage(b - 1) : stage(b), pa);
     if (up) rescale(f);
     exponentials(sb, pb);
-    product(stage(b) + kHalf, pb);
+    product(CT == 1 ? stage(b) : stage(b) + kHalf, pb);
   }
 
   // ---- the output, or a part of it ----
   wait_vm<0>();
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int r = wave * 64 + c * 32 + lr;
+  for (int c = 0; c < CT; ++c) {
+    const int r = (wave * CT + c) * 32 + lr;
     float lt = l[c] + __shfl_xor(l[c], 32, kWave);
     if (r >= rows) continue;
     if (parts == 1) {
@@ -1281,7 +1336,7 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
           *reinterpret_cast<u32x2*>(op + 32 * d + 2 * e) = *reinterpret_cast<u32x2*>(y);
         }
     } else {
-      const int64_t pr = (((int64_t)tile * H + h) * p.nsplit + part) * kManyRows + r;
+      const int64_t pr = (((int64_t)tile * H + h) * p.nsplit + part) * many_rows(CT) + r;
       float* op = p.part_o + pr * kD + 4 * half;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -1299,18 +1354,18 @@ __global__ __launch_bounds__(256, 1) void attn_many_kernel(PagedAttnArgs p) {
 // The tiles whose keys were split, a workgroup 16 query rows.
 constexpr int kManyJoin = 16;
 template <bool BF>
-__global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
+__global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p, int tile_rows) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   int* before = reinterpret_cast<int*>(smem);
   int* red = before + p.S + 1;
   uint32_t flags = 0;
-  many_plan(p, before, red, flags);
+  many_plan(p, tile_rows / p.G, before, red, flags);
   const int H = p.c.H, G = p.G, tile = blockIdx.x / H, h = blockIdx.x % H;
   if (tile >= before[p.S]) return;
-  const ManyTile t = many_tile(p, before, tile, h, red);
+  const ManyTile t = many_tile(p, tile_rows / G, before, tile, h, red);
   const int parts = parts_of(max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 0), p.nsplit), rows = t.toks * G;
   if (parts == 1) return;
-  const int64_t base = ((int64_t)tile * H + h) * p.nsplit * kManyRows;
+  const int64_t base = ((int64_t)tile * H + h) * p.nsplit * tile_rows;
   // 8 rows at a time, 32 threads and 4 channels a thread each
   const int x = threadIdx.x & 31;
 #pragma unroll
@@ -1318,11 +1373,11 @@ __global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
     const int r = blockIdx.y * kManyJoin + i + (threadIdx.x >> 5);
     if (r >= rows) return;
     float M = -__builtin_huge_valf();
-    for (int c = 0; c < parts; ++c) M = fmaxf(M, p.part_ml[2 * (base + (int64_t)c * kManyRows + r)]);
+    for (int c = 0; c < parts; ++c) M = fmaxf(M, p.part_ml[2 * (base + (int64_t)c * tile_rows + r)]);
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     float l = 0.0f;
     for (int c = 0; c < parts; ++c) {
-      const int64_t pr = base + (int64_t)c * kManyRows + r;
+      const int64_t pr = base + (int64_t)c * tile_rows + r;
       const float m = p.part_ml[2 * pr];
       if (m == -__builtin_huge_valf()) continue;
       const float w = __builtin_amdgcn_exp2f(m - M);
@@ -1343,7 +1398,7 @@ struct PagedAttnPlan {
   int few, R;         // rows up to which a request goes to attn_few_kernel; the rows it is built for
   bool run_few, run_many;
   int64_t tiles;      // bound on attn_many_kernel's row tiles
-  int nsplit;
+  int nsplit, ct;     // parts of a tile's keys at most; column tiles of a wave
   int64_t part_rows;  // rows of partial results
 };
 
@@ -1355,7 +1410,8 @@ static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) 
   a.run_many = most > kFewRows;
   // one request whose rows are all there are is known to be large; more may be of either kind
   a.run_few = !a.run_many || S > 1 || T <= kFewRows / G;
-  const int tm = kManyRows / G;
+  a.ct = getenv("FCT") ? atoi(getenv("FCT")) : 2;
+  const int tm = many_rows(a.ct) / G;
   a.nsplit = 1;
   if (a.run_many) {
     const int64_t large = T / (kFewRows / G + 1) < S ? T / (kFewRows / G + 1) : S;  // requests that can be large
@@ -1369,14 +1425,23 @@ static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) 
     }
   }
   const int64_t few_rows = a.run_few ? (int64_t)kFewWorkers * 2 * a.R : 0;
-  const int64_t many_rows = a.run_many && a.nsplit > 1 ? a.tiles * H * a.nsplit * kManyRows : 0;
-  a.part_rows = few_rows > many_rows ? few_rows : many_rows;
+  const int64_t many_part = a.run_many && a.nsplit > 1 ? a.tiles * H * a.nsplit * many_rows(a.ct) : 0;
+  a.part_rows = few_rows > many_part ? few_rows : many_part;
   return a;
 }
 
 size_t paged_attn_ws_bytes(int64_t T, int S, int H, int G, int64_t max_new) {
   const PagedAttnPlan a = attn_plan(T, S, H, G, max_new);
   return (size_t)a.part_rows * (kD + 2) * sizeof(float) + 1024;
+}
+
+template <bool BF, int CT>
+static void launch_many(const PagedAttnArgs& p, const PagedAttnPlan& a, size_t plan, hipStream_t s) {
+  const dim3 grid((unsigned)(a.tiles * a.nsplit * p.c.H)), threads(256);
+  const size_t lds = many_lds(CT) + plan;
+  if (p.softcap > 0.0f) hipLaunchKernelGGL((attn_many_kernel<BF, 2, CT>), grid, threads, lds, s, p);
+  else if (p.slopes || !(p.sm_scale > 0.0f)) hipLaunchKernelGGL((attn_many_kernel<BF, 1, CT>), grid, threads, lds, s, p);
+  else hipLaunchKernelGGL((attn_many_kernel<BF, 0, CT>), grid, threads, lds, s, p);
 }
 
 template <bool BF>
@@ -1386,14 +1451,12 @@ static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) 
   p.nsplit = a.nsplit;
   p.few = a.few;
   if (a.run_many) {
-    const dim3 grid((unsigned)(a.tiles * a.nsplit * p.c.H));
-    const size_t lds = (size_t)kManyStages * kManyStage + plan;
-    if (p.softcap > 0.0f) hipLaunchKernelGGL((attn_many_kernel<BF, 2>), grid, dim3(256), lds, s, p);
-    else if (p.slopes || !(p.sm_scale > 0.0f)) hipLaunchKernelGGL((attn_many_kernel<BF, 1>), grid, dim3(256), lds, s, p);
-    else hipLaunchKernelGGL((attn_many_kernel<BF, 0>), grid, dim3(256), lds, s, p);
+    if (a.ct == 1) launch_many<BF, 1>(p, a, plan, s);
+    else launch_many<BF, 2>(p, a, plan, s);
     if (a.nsplit > 1)
-      hipLaunchKernelGGL((attn_many_join_kernel<BF>), dim3((unsigned)(a.tiles * p.c.H), kManyRows / kManyJoin),
-                         dim3(256), plan, s, p);
+      hipLaunchKernelGGL((attn_many_join_kernel<BF>),
+                         dim3((unsigned)(a.tiles * p.c.H), (unsigned)(many_rows(a.ct) / kManyJoin)), dim3(256), plan, s,
+                         p, many_rows(a.ct));
   }
   if (a.run_few) {
     const dim3 grid(kFewWorkers / kFewWaves), threads(kFewWaves * kWave);
