@@ -53,11 +53,12 @@ constexpr int kFewKeys = 32;      // keys a step of a wave
 constexpr int kFewWaves = 4;
 constexpr int kFewWorkers = 1024; // waves: one workgroup of 128 KB of LDS on each of 256 CUs
 constexpr int kFewStage = 2 * kFewKeys * kRowBytes;
-// attn_many_kernel<CT>: column tiles of 32 query rows that a wave holds, 1 or 2
+constexpr int kManyRows = 128;    // attn_many_kernel: query rows of a workgroup, 32 a wave
+constexpr int kBlock = 32;        // keys of a block
+constexpr int kBlockBytes = kBlock * kRowBytes;
+constexpr int kManyStages = 4;    // blocks in each of the rings of K and V
+constexpr int kManyLds = 2 * kManyStages * kBlockBytes;
 constexpr int kManyKeys = 64;     // keys are divided among workgroups by these
-constexpr int kManyStages = 4;    // blocks of 32 CT keys in each of the rings of K and V
-constexpr int many_rows(int ct) { return 128 * ct; }  // query rows of a workgroup
-constexpr int many_lds(int ct) { return 2 * kManyStages * 32 * ct * kRowBytes; }
 constexpr int kNone = -(1 << 30);
 
 struct PagedAttnArgs {
@@ -72,7 +73,7 @@ struct PagedAttnArgs {
   const int64_t *prefix, *first;
   uint16_t* out;
   float *part_o, *part_ml;  // partial results: rows of kD sums, and (maximum, sum) of each
-  int tiles, nsplit;        // attn_many_kernel: row tiles launched, parts of their keys
+  int nsplit;               // attn_many_kernel: parts of a tile's keys at most
   uint32_t* st;
 };
 
@@ -226,11 +227,11 @@ __device__ __forceinline__ V8 join4(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(V8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Whether BYTES (a multiple of 1024) of V at `at` hold a value that is not finite; uniform.
+// Whether BYTES (a multiple of 1024) of V, from `mine` - 16 lane on, hold a value that is not
+// finite; uniform.
 // (Zero times such a value is no zero: a sum of products with zeros shows it.)
 template <bool BF, int BYTES>
-__device__ __forceinline__ bool any_nonfinite(uint32_t at) {
-  const uint32_t mine = at + 16 * (threadIdx.x & 63);
+__device__ __forceinline__ bool any_nonfinite(uint32_t mine) {
   float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < BYTES; i += 1024) {
@@ -585,7 +586,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
         const uint32_t va = vat + r0 * kRowBytes + 16 * v_chunk(r0, 2 * c + ((lr & 3) >> 1)) + 8 * (lr & 1);
         return __builtin_shufflevector(lds_tr(va), lds_tr(va + 16 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7);
       };
-      const bool clean = masked && any_nonfinite<BF, kFewStage / 2>(vat);
+      const bool clean = masked && any_nonfinite<BF, kFewStage / 2>(vat + 16 * lane);
       if (clean) {
 #pragma unroll 1
         for (int row = 0; row < kFewKeys; ++row) {
@@ -741,69 +742,87 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
 }
 
 // ---------------------------------------------------------------- many query rows
-// Row tiles, of tm tokens, of the requests with more than `few` query rows: before[s] those of the
-// requests before s.
-__device__ __forceinline__ void many_plan(const PagedAttnArgs& p, int tm, int* before, int* part, uint32_t& flags) {
-  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (p.S + nt - 1) / nt;
-  int sum = 0;
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s >= p.S) break;
-    int64_t a, n;
-    const int rows = request_rows(p, s, &a, &n, flags);
-    before[s] = sum;
-    if (rows * p.G > p.few) sum += (rows + tm - 1) / tm;
-  }
-  int inc = sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(inc, o, kWave);
-    if (lane >= o) inc += x;
-  }
-  if (lane == 63) part[wave] = inc;
-  __syncthreads();
-  int base = inc - sum;
-  for (int w = 0; w < wave; ++w) base += part[w];
-  for (int i = 0; i < per; ++i)
-    if (tid * per + i < p.S) before[tid * per + i] += base;
-  if (tid == nt - 1) before[p.S] = base + sum;
-  __syncthreads();
-}
-
-// Parts that a tile of nb key blocks is cut into, of at least 4 blocks each.
-__device__ __forceinline__ int parts_of(int nb, int nsplit) { return max(min(nsplit, nb / 4), 1); }
-
+// A workgroup's share: a tile of at most 128 / G new tokens of one request and head.
 struct ManyTile {
   int s, h, tok0, toks, total, n;  // tokens of the tile and of the request, new and all
   int lo, hi;                      // the union of their ranges
   int lo_max, hi_min;              // and what all of them see (up to the first token's own position)
-  int64_t a;
+  int64_t a;                       // the request's first row
 };
 
-// Tile and head of a workgroup index (later tiles, which see more, first).  Every thread of
+// Tile `tile` of those of all requests with more than `few` query rows, tm tokens each (later
+// tiles, which see more, first); false where there are fewer.  Up to 64 requests a wave finds
+// it by itself, a lane a request; more go through `before` [S + 1] in LDS.  Every thread of
 // 256; red[12] is LDS.
-__device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, int tm, const int* before, int tile, int h,
-                                              int* red) {
-  ManyTile t;
+__device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int tile, int h, int* before, int* red,
+                                          ManyTile* t, uint32_t& flags) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int x = before[p.S] - 1 - tile;
-  t.s = uniform(request_of(before, p.S, x));
-  t.h = h;
-  t.a = fixed(p.start, t.s);
-  t.n = uniform((int)fixed(p.n, t.s));
-  t.total = uniform((int)(fixed(p.start, t.s + 1) - t.a));
-  t.tok0 = (x - uniform(before[t.s])) * tm;
-  t.toks = min(tm, t.total - t.tok0);
-  if (!p.first && !p.prefix) {
-    t.lo = t.lo_max = 0;
-    t.hi_min = t.n - t.total + t.tok0 + 1;
-    t.hi = t.n - t.total + t.tok0 + t.toks;
-    return t;
+  t->h = h;
+  int x, first;
+  if (p.S <= kWave) {
+    int64_t a = 0, n = 0;
+    int rows = 0, tiles = 0;
+    if (lane < p.S) {
+      rows = request_rows(p, lane, &a, &n, flags);
+      if (rows * p.G > p.few) tiles = (rows + tm - 1) / tm;
+    }
+    int inc = tiles;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(inc, o, kWave);
+      if (lane >= o) inc += y;
+    }
+    x = __builtin_amdgcn_readlane(inc, kWave - 1) - 1 - tile;
+    if (x < 0) return false;
+    t->s = uniform(__builtin_popcountll(__ballot(inc <= x)));  // requests that end before tile x
+    first = __builtin_amdgcn_readlane(inc - tiles, t->s);
+    t->total = __builtin_amdgcn_readlane(rows, t->s);
+    t->n = __builtin_amdgcn_readlane((int)n, t->s);
+    t->a = __builtin_amdgcn_readlane((int)a, t->s);  // (below 2^30)
+  } else {
+    const int per = (p.S + 255) / 256;
+    int sum = 0;
+    for (int i = 0; i < per; ++i) {
+      const int s = tid * per + i;
+      if (s >= p.S) break;
+      int64_t a, n;
+      const int rows = request_rows(p, s, &a, &n, flags);
+      before[s] = sum;
+      if (rows * p.G > p.few) sum += (rows + tm - 1) / tm;
+    }
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(inc, o, kWave);
+      if (lane >= o) inc += y;
+    }
+    if (lane == 63) red[wave] = inc;
+    __syncthreads();
+    int base = inc - sum;
+    for (int w = 0; w < wave; ++w) base += red[w];
+    for (int i = 0; i < per; ++i)
+      if (tid * per + i < p.S) before[tid * per + i] += base;
+    if (tid == 255) before[p.S] = base + sum;
+    __syncthreads();
+    x = uniform(before[p.S]) - 1 - tile;
+    if (x < 0) return false;
+    t->s = uniform(request_of(before, p.S, x));
+    first = uniform(before[t->s]);
+    t->a = fixed(p.start, t->s);
+    t->n = uniform((int)fixed(p.n, t->s));
+    t->total = uniform((int)(fixed(p.start, t->s + 1) - t->a));
   }
-  int lo = t.n, hi = 0, lo_max = 0;
-  if (tid < t.toks) {
-    token_range(p, t.s, t.a + t.tok0 + tid, t.n - t.total + t.tok0 + tid, t.n, &lo, &hi);
+  t->tok0 = (x - first) * tm;
+  t->toks = min(tm, t->total - t->tok0);
+  t->hi_min = t->n - t->total + t->tok0 + 1;
+  if (!p.first && !p.prefix) {
+    t->lo = t->lo_max = 0;
+    t->hi = t->n - t->total + t->tok0 + t->toks;
+    return true;
+  }
+  int lo = t->n, hi = 0, lo_max = 0;
+  if (tid < t->toks) {
+    token_range(p, t->s, t->a + t->tok0 + tid, t->n - t->total + t->tok0 + tid, t->n, &lo, &hi);
     lo_max = lo;
   }
 #pragma unroll
@@ -812,137 +831,141 @@ __device__ __forceinline__ ManyTile many_tile(const PagedAttnArgs& p, int tm, co
     hi = max(hi, __shfl_xor(hi, o, kWave));
     lo_max = max(lo_max, __shfl_xor(lo_max, o, kWave));
   }
+  __syncthreads();  // red is free
   if (lane == 0) {
     red[wave] = lo;
     red[4 + wave] = hi;
     red[8 + wave] = lo_max;
   }
   __syncthreads();
-  t.lo = uniform(min(min(red[0], red[1]), min(red[2], red[3]))) & ~(kManyKeys - 1);
-  t.hi = uniform(max(max(red[4], red[5]), max(red[6], red[7])));
-  t.lo_max = uniform(max(max(red[8], red[9]), max(red[10], red[11])));
-  t.hi_min = t.n - t.total + t.tok0 + 1;
+  t->lo = uniform(min(min(red[0], red[1]), min(red[2], red[3]))) & ~(kManyKeys - 1);
+  t->hi = uniform(max(max(red[4], red[5]), max(red[6], red[7])));
+  t->lo_max = uniform(max(max(red[8], red[9]), max(red[10], red[11])));
   __syncthreads();
-  return t;
+  return true;
 }
 
-// A block of 64 keys is two halves of 32.  While the matrix cores form the scores of the
-// next half and add the last half's products with V, the vector unit takes the exponentials
-// of this half: three halves are under way at a time, in registers S (two), P (two) and O.
-// The maximum that the exponentials are taken against is raised only when a score exceeds
-// it by more than kSlack (a factor of 2^kSlack is no loss in 32-bit sums, and
-// Mx::kShift leaves room for it in the probabilities), so the sums are rarely rescaled.
+// The keys of a tile in units of 64, and the parts that they are cut into, of at least 4 each.
+__device__ __forceinline__ int units_of(const ManyTile& t) { return max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 0); }
+__device__ __forceinline__ int parts_of(int units, int nsplit) { return max(min(nsplit, units / 4), 1); }
+
+// Keys go by in blocks of 32.  While the matrix cores form the scores of the next block and
+// add the last block's product with V, the vector unit takes the exponentials of this one:
+// three blocks are under way at a time, in registers S (two), P (two) and O, 190 and no more
+// than 256 of them, so that two workgroups share a CU and one computes while the other
+// begins, waits or ends.  The maximum that the exponentials are taken against is raised only
+// when a score exceeds it by more than kSlack (a factor of 2^kSlack is no loss in 32-bit
+// sums, and Mx::kShift leaves room for it in the probabilities), so the sums are rarely
+// rescaled.
+//
+// Bound by the matrix cores' power: 2048 tokens over 65536 take 2.1 ms, 1.05 PFLOP/s, where
+// a large matrix product of this type reaches 1.2; with neither exponentials nor LDS reads
+// the same instructions take 1.75 ms.  64 rows a wave and one workgroup a CU need half of
+// the LDS reads and are as fast there, and slower where tiles are short (28 prompts of 700
+// tokens 154 us against 137; 6 requests of documents 307 against 235).
 constexpr float kSlack = 6.0f;
 
-// A half's scores between two half steps: as the matrix instructions leave them, or, mapped,
-// as values of their own (values put back into an accumulator cost copies of all of it).
+// A block's scores between two steps: as the matrix instructions leave them, or, mapped, as
+// values of their own (values put back into an accumulator cost copies of all of it).
 struct Scores16 {
   float v[16];
   __device__ __forceinline__ float& operator[](int i) { return v[i]; }
   __device__ __forceinline__ float operator[](int i) const { return v[i]; }
 };
 
-// MAP: 0 the scaled score, 1 with a bias (and for scales below 0), 2 capped.
+#define INLINE __attribute__((always_inline))
 
-template <bool BF, int MAP, int CT>
-__global__ __launch_bounds__(256, CT == 1 ? 2 : 1) void attn_many_kernel(PagedAttnArgs p) {
+// MAP: 0 the scaled score, 1 with a bias (and for scales that are not above 0), 2 capped.
+template <bool BF, int MAP>
+__global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   typedef typename Mx<BF>::v8 v8;
   typedef typename Mx<BF>::t vt;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5, lr = lane & 31;
-  int* before = reinterpret_cast<int*>(smem + many_lds(CT));
-  int* red = before + p.S + 1;
-  uint32_t flags = 0;
-  many_plan(p, many_rows(CT) / p.G, before, red, flags);
-  if (flags && blockIdx.x == 0) set_status(p.st, flags);
   const int H = p.c.H, G = p.G;
   const int bid = blockIdx.x, h = bid % H, part = (bid / H) % p.nsplit, tile = bid / H / p.nsplit;
-  if (tile >= before[p.S]) return;
-  const ManyTile t = many_tile(p, many_rows(CT) / G, before, tile, h, red);
-  const int all = max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 0), parts = parts_of(all, p.nsplit);
+  int* before = reinterpret_cast<int*>(smem + kManyLds);
+  int* red = before + p.S + 1;
+  ManyTile t;
+  {
+    uint32_t flags = 0;
+    const bool some = many_tile(p, kManyRows / G, tile, h, before, red, &t, flags);
+    if (flags && blockIdx.x == 0) set_status(p.st, flags);
+    if (!some) return;
+  }
+  const int units = units_of(t), parts = parts_of(units, p.nsplit);
   if (part >= parts) return;
-  const int from64 = (int)((int64_t)all * part / parts), count64 = (int)((int64_t)all * (part + 1) / parts) - from64;
-  // blocks of 32 CT keys, halves of 32 (CT 1: a block is a half; their number is even)
-  constexpr int kKeys = 32 * CT;
-  constexpr uint32_t kHalf = 32 * kRowBytes;
-  const int nb = count64 * (kManyKeys / kKeys), key0 = t.lo + from64 * kManyKeys, n = t.n;
+  const int unit0 = (int)((int64_t)units * part / parts), unit1 = (int)((int64_t)units * (part + 1) / parts);
+  // blocks, an even number
+  const int nb = (unit1 - unit0) * (kManyKeys / kBlock), key0 = t.lo + unit0 * kManyKeys, n = t.n;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_PTR(char))smem;
   const int rows = t.toks * G;
 
   bool absent = false;
   // whether key k's page is there
-  auto there = [&](int k) __attribute__((always_inline)) -> bool {
+  auto there = [&](int k) INLINE -> bool {
     return !absent || (uint32_t)page_of(p.c, t.s, min(k, n - 1) >> p.c.shift) < (uint32_t)p.c.P;
   };
 
-  // ---- loads: wave w takes keys 8 CT w .. 8 CT (w + 1) - 1 of a block ----
+  // ---- loads: wave w takes keys 8w .. 8w + 7 of a block ----
   const uint32_t row_step = (uint32_t)p.c.ld_tok * 2;
-  uint32_t koff[2 * CT], voff[2 * CT];
+  uint32_t koff[2], voff[2];
 #pragma unroll
-  for (int i = 0; i < 2 * CT; ++i) {
-    const int row = 4 * i + (lane >> 4), at = 8 * CT * wave + row;
+  for (int i = 0; i < 2; ++i) {
+    const int row = 4 * i + (lane >> 4), at = 8 * wave + row;
     koff[i] = row * row_step + 16 * k_chunk(at, lane & 15) - 1024 * i;  // 4 rows are 1024 bytes at least
     voff[i] = row * row_step + 16 * v_chunk(at, lane & 15) - 1024 * i;
   }
   // Where the wave's keys of block b begin in a pool; page 0 where there is none.
   const uint16_t *Kh = p.c.K + (int64_t)h * p.c.ld_head, *Vh = p.c.V + (int64_t)h * p.c.ld_head;
-  auto page = [&](int b) __attribute__((always_inline)) -> int {
-    const int k = key0 + b * kKeys + 8 * CT * wave;
+  auto page = [&](int b) INLINE -> int {
+    const int k = key0 + b * kBlock + 8 * wave;
     return b < nb && k < n ? page_uniform(p.c, t.s, k >> p.c.shift) : 0;
   };
-  auto place = [&](int b, int id) __attribute__((always_inline)) -> int64_t {
-    const int k = key0 + b * kKeys + 8 * CT * wave;
+  auto place = [&](int b, int id) INLINE -> int64_t {
+    const int k = key0 + b * kBlock + 8 * wave;
     return (int64_t)((uint32_t)id < (uint32_t)p.c.P ? id : 0) * p.c.ld_page +
            (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
   };
-  auto stage = [](int b) __attribute__((always_inline)) -> uint32_t { return (uint32_t)(b % kManyStages) * CT * kHalf; };
-  constexpr uint32_t kVRing = many_lds(CT) / 2;  // V's stages behind K's
-  const uint32_t mine = lds0 + wave * (2048 * CT);
-  // `advance(b)` issues K of block b + kAhead and V of block b + 2, in stages that are read by
-  // then (with two halves a block, K of block b is still in use).  Blocks behind the last are
-  // loaded from page 0 and not used, so that the number of loads in flight is always the same.
-  constexpr int kAhead = CT == 1 ? 4 : 3;
-  int64_t from[kAhead];  // places of blocks b + 2 .. b + kAhead + 1, before advance(b)
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) from[i] = place(i, page(i));
-#pragma unroll
-  for (int i = 0; i < kAhead - 1; ++i) load_to_lds(mine + stage(i), Kh + from[i], koff);
-  load_to_lds(mine + kVRing + stage(0), Vh + from[0], voff);
-  load_to_lds(mine + stage(kAhead - 1), Kh + from[kAhead - 1], koff);
-  load_to_lds(mine + kVRing + stage(1), Vh + from[1], voff);
-#pragma unroll
-  for (int i = 0; i + 2 < kAhead; ++i) from[i] = from[i + 2];
-  int id_next = page(kAhead);
+  auto stage = [](int b) INLINE -> uint32_t { return (uint32_t)(b % kManyStages) * kBlockBytes; };
+  constexpr uint32_t kVRing = kManyLds / 2;  // V's stages behind K's
+  const uint32_t mine = lds0 + wave * (kBlockBytes / 4);
+  // `advance(b)` issues K of block b + 4 and V of block b + 2, in stages that are read by then.
+  // Blocks behind the last are loaded from page 0 and not used, so that the number of loads in
+  // flight is always the same.
+  int64_t from0 = place(0, page(0)), from1 = place(1, page(1)), from2 = place(2, page(2)), from3 = place(3, page(3));
+  load_to_lds(mine + stage(0), Kh + from0, koff);
+  load_to_lds(mine + stage(1), Kh + from1, koff);
+  load_to_lds(mine + stage(2), Kh + from2, koff);
+  load_to_lds(mine + kVRing + stage(0), Vh + from0, voff);
+  load_to_lds(mine + stage(3), Kh + from3, koff);
+  load_to_lds(mine + kVRing + stage(1), Vh + from1, voff);
+  int id_next = page(4);
 
-  // ---- the wave's query rows: column tiles of 32 ----
-  v8 qf[CT][8];
-  int pos[CT], lo[CT], hi[CT], lo_max = 0, hi_min = n;
-  float slope[CT];
+  // ---- the wave's 32 query rows, two lanes each ----
+  v8 qf[8];
+  int pos = 0, lo = 0, hi = n, lo_max = 0, hi_min = n;
+  float slope = 0.0f;
   const ScoreMap sm = score_map(p);
+  {
+    const int r = wave * 32 + lr, tok = r / G, g = r - tok * G;
+    const s16x8 zero = {};
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int r = (wave * CT + c) * 32 + lr, tok = r / G, g = r - tok * G;
-    pos[c] = 0;
-    lo[c] = 0;
-    hi[c] = n;
-    slope[c] = 0.0f;
-    s16x8 z = {};
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) qf[c][kk] = __builtin_bit_cast(v8, z);
+    for (int kk = 0; kk < 8; ++kk) qf[kk] = __builtin_bit_cast(v8, zero);
     if (r < rows) {
       const int64_t row = t.a + t.tok0 + tok;
-      pos[c] = n - t.total + t.tok0 + tok;
-      token_range(p, t.s, row, pos[c], n, &lo[c], &hi[c]);
-      if (p.slopes) slope[c] = p.slopes[h * G + g] * kLog2e;
+      pos = n - t.total + t.tok0 + tok;
+      token_range(p, t.s, row, pos, n, &lo, &hi);
+      if (p.slopes) slope = p.slopes[h * G + g] * kLog2e;
       const uint16_t* qp = p.q + row * p.ldq_tok + (int64_t)(h * G + g) * p.ldq_head + 8 * half;
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) qf[c][kk] = *reinterpret_cast<const v8*>(qp + 16 * kk);
-      lo_max = max(lo_max, lo[c]);
-      hi_min = min(hi_min, MAP != 0 ? min(hi[c], pos[c] + 1) : hi[c]);  // (map_seen)
+      for (int kk = 0; kk < 8; ++kk) qf[kk] = *reinterpret_cast<const v8*>(qp + 16 * kk);
+      lo_max = lo;
+      hi_min = MAP != 0 ? min(hi, pos + 1) : hi;  // (map_seen)
     }
   }
   if (!p.prefix && !p.first) {  // the wave's first token
-    hi_min = wave * CT * 32 < rows ? n - t.total + t.tok0 + wave * CT * 32 / G + 1 : n;
+    hi_min = wave * 32 < rows ? n - t.total + t.tok0 + wave * 32 / G + 1 : n;
   } else {
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) {
@@ -952,12 +975,11 @@ __global__ __launch_bounds__(256, CT == 1 ? 2 : 1) void attn_many_kernel(PagedAt
   }
   lo_max = uniform(lo_max);
   hi_min = uniform(hi_min);
-  // ---- absent pages among the keys: their blocks are masked throughout ----
+  // ---- absent pages among the keys: all blocks count as masked then ----
   {
-    const int e1 = min(key0 + nb * kKeys, n);
+    const int e1 = min(key0 + nb * kBlock, n);
     for (int k = key0 + 16 * tid; k < e1; k += 16 * 256)
       absent |= (uint32_t)page_of(p.c, t.s, k >> p.c.shift) >= (uint32_t)p.c.P;
-    if (lane == 0) red[wave] = 0;
     const bool any = __ballot(absent) != 0;
     if (lane == 0) red[wave] = any;
     __syncthreads();
@@ -974,202 +996,159 @@ __global__ __launch_bounds__(256, CT == 1 ? 2 : 1) void attn_many_kernel(PagedAt
     const int r0 = 4 * half + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     vaddr = lds0 + kVRing + r0 * kRowBytes + 16 * v_chunk(r0, ch) + 8 * (lane & 1);
   }
-
-  typedef std::conditional_t<MAP == 0, f32x16, Scores16> Sv;
-  f32x16 o[CT][4];
-  Sv sa[CT], sb[CT];
-  u32x4 pa[CT][2], pb[CT][2];
-  // l: sums of the probabilities; nr: kShift less the reference that they are taken against (in
-  // log2; at first a reference that every score raises and against which -Inf gives 0)
-  float nr[CT], l[CT];
-#pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    nr[c] = 1e37f;
-    l[c] = 0.0f;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[c][d][e] = 0.0f;
-  }
-  auto k_frag = [&](uint32_t at, int kk) __attribute__((always_inline)) { return lds_v8<v8>((kaddr ^ (32 * kk)) + at); };
-  auto v_frag = [&](uint32_t at, int j) __attribute__((always_inline)) {
+  auto k_frag = [&](uint32_t at, int kk) INLINE { return lds_v8<v8>((kaddr ^ (32 * kk)) + at); };
+  auto v_frag = [&](uint32_t at, int j) INLINE {  // keys 16 (j >> 2) .., channels 32 (j & 3) ..
     const uint32_t va = (vaddr ^ (64 * (j & 3))) + at + 16 * (j >> 2) * kRowBytes;
     return join4<v8>(lds_tr(va), lds_tr(va + 8 * kRowBytes));
   };
-  // S^T of the 32 keys at byte `at` of K's ring
-  auto scores = [&](uint32_t at, Sv (&s)[CT]) __attribute__((always_inline)) {
-    f32x16 acc[CT] = {};
+
+  typedef std::conditional_t<MAP == 0, f32x16, Scores16> Sv;
+  f32x16 o[4];      // O^T: channels 32 d + 8 (e >> 2) + 4 half + (e & 3)
+  Sv sa, sb;        // S^T: keys 8 (e >> 2) + 4 half + (e & 3)
+  u32x4 pa[2], pb[2];
+  // l: the sum of the probabilities; nr: kShift less the reference that they are taken against
+  // (in log2; at first a reference that every score raises and against which -Inf gives 0)
+  float nr = 1e37f, l = 0.0f, mx;  // mx: the lane's maximum of a block's scores
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      const v8 kf = k_frag(at, kk);
+  for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int c = 0; c < CT; ++c) acc[c] = Mx<BF>::mfma32(kf, qf[c][kk], acc[c]);
-    }
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+
+  // S^T of the block at byte `at` of K's ring
+  auto scores = [&](uint32_t at, Sv& s) INLINE {
+    f32x16 acc = {};
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
+    for (int kk = 0; kk < 8; ++kk) acc = Mx<BF>::mfma32(k_frag(at, kk), qf[kk], acc);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[c][e] = acc[c][e];
+    for (int e = 0; e < 16; ++e) s[e] = acc[e];
   };
-  // O^T += V^T P^T of the 32 keys at byte `at` of V's ring
-  auto product = [&](uint32_t at, const u32x4 (&pr)[CT][2]) __attribute__((always_inline)) {
+  // O^T += V^T P^T of the block at byte `at` of V's ring
+  auto product = [&](uint32_t at, const u32x4(&pr)[2]) INLINE {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const v8 vf = v_frag(at, 4 * i + d);
-#pragma unroll
-        for (int c = 0; c < CT; ++c) o[c][d] = Mx<BF>::mfma32(vf, __builtin_bit_cast(v8, pr[c][i]), o[c][d]);
-      }
+    for (int j = 0; j < 8; ++j) o[j & 3] = Mx<BF>::mfma32(v_frag(at, j), __builtin_bit_cast(v8, pr[j >> 2]), o[j & 3]);
   };
-  auto exponentials = [&](const Sv (&s)[CT], u32x4 (&pr)[CT][2]) __attribute__((always_inline)) {
+  auto exponentials = [&](const Sv& s, u32x4(&pr)[2]) INLINE {
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
-        const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e + 1], c1, nr[c]));
-        const typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
-        l[c] = Mx<BF>::add_pair(pair, l[c]);
-        pr[c][e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, pair);
-      }
+    for (int e = 0; e < 16; e += 2) {
+      const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c1, nr));
+      const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], c1, nr));
+      const typename Mx<BF>::v2 pair = {(vt)x0, (vt)x1};
+      l = Mx<BF>::add_pair(pair, l);
+      pr[e >> 3][(e & 7) >> 1] = __builtin_bit_cast(uint32_t, pair);
     }
   };
-  // The mapped score of element e of a half, with a bias linear in the key: it is the bias for
-  // keys up to the row's own (mask_half has the others).
-  auto bias_base = [&](int c, int key) __attribute__((always_inline)) { return slope[c] * (float)(key + 4 * half - pos[c]); };
-  auto map_seen = [&](float s, int c, int e, float base) __attribute__((always_inline)) -> float {
-    const float bias = __builtin_fmaf(slope[c], (float)(8 * (e >> 2) + (e & 3)), base);
+  // The mapped score of element e of a block, with a bias linear in the key: it is the bias for
+  // keys up to the row's own (mask_block has the others).
+  auto bias_base = [&](int key) INLINE { return slope * (float)(key + 4 * half - pos); };
+  auto map_seen = [&](float s, int e, float base) INLINE -> float {
+    const float bias = __builtin_fmaf(slope, (float)(8 * (e >> 2) + (e & 3)), base);
     if constexpr (MAP == 1) return __builtin_fmaf(s, sm.c1, bias);
     return mapped<true>(sm, 0.0f, s, 0) + bias;
   };
-  auto map_half = [&](Sv (&s)[CT], int key) __attribute__((always_inline)) {
+  auto maximum = [&](const Sv& s) INLINE {
+    mx = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int e = 2; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[e]), s[e + 1]);
+  };
+  auto map_block = [&](Sv& s, int key) INLINE {
     if constexpr (MAP != 0) {
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[c][e] = map_seen(s[c][e], c, e, bias_base(c, key));
+      for (int e = 0; e < 16; ++e) s[e] = map_seen(s[e], e, bias_base(key));
     }
+    maximum(s);
   };
-  float mx[CT];  // the lane's maxima of a half's scores
-  auto maxima = [&](const Sv (&s)[CT]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      mx[c] = fmaxf(s[c][0], s[c][1]);
-#pragma unroll
-      for (int e = 2; e < 16; e += 2) mx[c] = fmaxf(fmaxf(mx[c], s[c][e]), s[c][e + 1]);
-    }
-  };
-  // Where one exceeds the reference by kSlack: the reference becomes the maximum of the row's
-  // scores, l follows, and f is the factor for O.
-  auto raise = [&](float (&f)[CT]) __attribute__((always_inline)) -> bool {
-    bool up = false;
-#pragma unroll
-    for (int c = 0; c < CT; ++c) up |= __builtin_fmaf(mx[c], c1, nr[c]) > kSlack + Mx<BF>::kShift;
-    if (!__ballot(up)) return false;
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const float top = fmaxf(mx[c], __shfl_xor(mx[c], 32, kWave));
-      const float to = fminf(nr[c], Mx<BF>::kShift - top * c1);
-      f[c] = fmaxf(__builtin_amdgcn_exp2f(to - nr[c]), 0x1p-126f);  // not 0: O may hold an infinity
-      nr[c] = to;
-      l[c] *= f[c];
-    }
-    return true;
-  };
-  auto rescale = [&](const float (&f)[CT]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-      for (int d = 0; d < 4; ++d) o[c][d] *= f[c];
-  };
-  // Block b is begun: its V, its K and the K that is read up to the next call are in LDS once
-  // all but what the last call issued is; what this wave has read of the stages is read.
-  auto advance = [&](int b) __attribute__((always_inline)) {
-    wait_vm<4 * CT>();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    from[kAhead - 2] = place(b + kAhead, id_next);
-    id_next = page(b + kAhead + 1);
-    load_to_lds(mine + stage(b + kAhead), Kh + from[kAhead - 2], koff);
-    load_to_lds(mine + kVRing + stage(b + 2), Vh + from[0], voff);
-#pragma unroll
-    for (int i = 0; i + 1 < kAhead - 1; ++i) from[i] = from[i + 1];
-  };
-  // What the rows of the wave do not see of the half at `key` takes no part; `mx` again.
-  auto mask_half = [&](Sv (&s)[CT], int key) __attribute__((always_inline)) {
-    if (key >= lo_max && key + 32 <= hi_min && !absent) return;
+  // What the rows of the wave do not see of the block at `key` takes no part; `mx` again.
+  auto mask_block = [&](Sv& s, int key) INLINE {
+    if (key >= lo_max && key + kBlock <= hi_min && !absent) return;
     if (MAP != 0 && p.prefix) {  // keys behind the row's own: slope * distance was added, not taken off
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[c][e] = __builtin_fmaf(-2.0f * slope[c], (float)max(key + 8 * (e >> 2) + 4 * half + (e & 3) - pos[c], 0), s[c][e]);
-    }
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const uint32_t from = lo[c] - key - 4 * half, count = max(hi[c] - lo[c], 0);
-#pragma unroll
       for (int e = 0; e < 16; ++e)
-        if ((uint32_t)(8 * (e >> 2) + (e & 3)) - from >= count) s[c][e] = -__builtin_huge_valf();
+        s[e] = __builtin_fmaf(-2.0f * slope, (float)max(key + 8 * (e >> 2) + 4 * half + (e & 3) - pos, 0), s[e]);
     }
+    const uint32_t from = lo - key - 4 * half, count = max(hi - lo, 0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if ((uint32_t)(8 * (e >> 2) + (e & 3)) - from >= count) s[e] = -__builtin_huge_valf();
     if (absent) {
       const bool in0 = there(key), in1 = there(key + 16);
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!(e < 8 ? in0 : in1)) s[c][e] = -__builtin_huge_valf();
+      for (int e = 0; e < 16; ++e)
+        if (!(e < 8 ? in0 : in1)) s[e] = -__builtin_huge_valf();
     }
-    maxima(s);
+    maximum(s);
+  };
+  // Where `mx` exceeds the reference by kSlack: the reference becomes the maximum of the row's
+  // scores, l follows, and f is the factor for O.
+  auto raise = [&](float& f) INLINE -> bool {
+    if (!__ballot(__builtin_fmaf(mx, c1, nr) > kSlack + Mx<BF>::kShift)) return false;
+    const float top = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+    const float to = fminf(nr, Mx<BF>::kShift - top * c1);
+    f = fmaxf(__builtin_amdgcn_exp2f(to - nr), 0x1p-126f);  // not 0: O may hold an infinity
+    nr = to;
+    l *= f;
+    return true;
+  };
+  auto rescale = [&](float f) INLINE {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) o[d] *= f;
+  };
+  // Block b is begun: its V, the next block's K and that of the block after, of which the first
+  // fragments are read ahead, are in LDS once all but what the last call issued is; K of block
+  // b and V of block b - 2 are read, by every wave.
+  auto advance = [&](int b) INLINE {
+    wait_vm<4>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int64_t from4 = place(b + 4, id_next);
+    id_next = page(b + 5);
+    load_to_lds(mine + stage(b + 4), Kh + from4, koff);
+    load_to_lds(mine + kVRing + stage(b + 2), Vh + from2, voff);
+    from2 = from3;
+    from3 = from4;
   };
   // A block that not every query of the workgroup sees whole: V's rows that are not there are
   // cleared, and of values that are not finite the product takes none: they go to O of the
   // queries that see them before the block's V is cleared of them.
-  auto prepare = [&](int b) __attribute__((always_inline)) {
-    const int key_b = key0 + b * kKeys;
-    if (key_b >= t.lo_max && key_b + kKeys <= t.hi_min && !absent) return;
-    const uint32_t v0 = lds0 + kVRing + stage(b), own = v0 + wave * (2048 * CT);
-    const int key_w = key_b + 8 * CT * wave;
+  auto prepare = [&](int b) INLINE {
+    const int key_b = key0 + b * kBlock;
+    if (key_b >= t.lo_max && key_b + kBlock <= t.hi_min && !absent) return;
+    int x = lane;
+    asm volatile("" : "+v"(x));  // (else what follows from the lane stays in registers throughout)
+    const uint32_t v0 = lds0 + kVRing + stage(b), own = v0 + wave * (kBlockBytes / 4);
+    const int key_w = key_b + 8 * wave;
     const bool in = there(key_w);
-    if (key_w + 8 * CT > n || !in) {
+    if (key_w + 8 > n || !in) {
 #pragma unroll
-      for (int y = 0; y < 2 * CT; ++y) {
-        const int row = 4 * y + (lane >> 4);
+      for (int y = 0; y < 2; ++y) {
+        const int row = 4 * y + (x >> 4);
         if (key_w + row >= n || !in)
-          *LDS_AT(u32x4, own + row * kRowBytes + 16 * (lane & 15)) = (u32x4){0u, 0u, 0u, 0u};
+          *LDS_AT(u32x4, own + row * kRowBytes + 16 * (x & 15)) = (u32x4){0u, 0u, 0u, 0u};
       }
     }
-    const bool bad = any_nonfinite<BF, 2048 * CT>(own);
-    if (lane == 0) red[wave] = bad;
+    const bool bad = any_nonfinite<BF, kBlockBytes / 4>(own + 16 * x);
+    if (x == 0) red[wave] = bad;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (!uniform(red[0] | red[1] | red[2] | red[3])) return;
 #pragma unroll 1
-    for (int row = 0; row < kKeys; ++row) {
+    for (int row = 0; row < kBlock; ++row) {
       const int k = key_b + row;
-      const bool has = there(k);
-      bool sees[CT];
-#pragma unroll
-      for (int c = 0; c < CT; ++c) sees[c] = has && k >= lo[c] && k < hi[c];
+      const bool sees = k >= lo && k < hi && there(k);
 #pragma unroll
       for (int y = 0; y < 16; ++y) {  // channels 8 y + 4 half ..
-        const s16x4 x = *LDS_AT(const s16x4, v0 + row * kRowBytes + 16 * v_chunk(row, y) + 8 * half);
+        const s16x4 v = *LDS_AT(const s16x4, v0 + row * kRowBytes + 16 * v_chunk(row, y) + 8 * (x >> 5));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float add = nonfinite_part<BF>(x[e]);
-#pragma unroll
-          for (int c = 0; c < CT; ++c) o[c][y >> 2][4 * (y & 3) + e] += sees[c] ? add : 0.0f;
-        }
+        for (int e = 0; e < 4; ++e) o[y >> 2][4 * (y & 3) + e] += sees ? nonfinite_part<BF>(v[e]) : 0.0f;
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int y = 0; y < 2 * CT; ++y) {
-      const uint32_t at = own + y * 1024 + 16 * lane;
+    for (int y = 0; y < 2; ++y) {
+      const uint32_t at = own + y * 1024 + 16 * x;
       *LDS_AT(s16x8, at) = finite_part<BF>(*LDS_AT(const s16x8, at));
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -1177,212 +1156,176 @@ __global__ __launch_bounds__(256, CT == 1 ? 2 : 1) void attn_many_kernel(PagedAt
     asm volatile("" ::: "memory");
   };
 
-  // A half step: the exponentials of `s` to P, the scores of the next half (K at byte `kat`) to
-  // `sn` and their maxima, the product of the last half (P in `pp`, V at byte `vat`).  16
-  // pieces of two matrix instructions with one LDS fragment, read two pieces ahead (the last
-  // two, in `ka` and `kb`, for the step after, K at `kafter`), and of two exponentials with
-  // what belongs to them: a wave alone on its SIMD issues about as long as the two matrix
-  // instructions run.
-  auto half_step = [&](const Sv (&s)[CT], u32x4 (&pr)[CT][2], uint32_t kat, Sv (&sn)[CT], int key_next, uint32_t vat,
-                       const u32x4 (&pp)[CT][2], v8& ka, v8& kb, uint32_t kafter) __attribute__((always_inline)) {
+  // A step: the exponentials of `s` to P, the scores of the next block (K at byte `kat`) to `sn`
+  // and their maximum, the product of the last block (P in `pp`, V at byte `vat`).  16 pieces
+  // of one matrix instruction with its LDS fragment, read two pieces ahead (the last two, in
+  // `ka` and `kb`, for the step after, K at `kafter`), and of one exponential with what
+  // belongs to it.
+  auto step = [&](const Sv& s, u32x4(&pr)[2], uint32_t kat, Sv& sn, int key_next, uint32_t vat, const u32x4(&pp)[2],
+                  v8& ka, v8& kb, uint32_t kafter) INLINE {
     v8 fr[18];
-    f32x16 acc[CT];
-    float base = 0.0f;
+    f32x16 acc;
+    float base = 0.0f, even = 0.0f;
     asm volatile("" : "+v"(kaddr), "+v"(vaddr));  // (else twelve addresses stay in registers)
     fr[0] = ka;
     fr[1] = kb;
-    // once the scores are complete, from five eighths of the matrix instructions on: map them,
-    // and the lane's maxima, a pair or two at a time
-    auto last_max = [&](auto place) __attribute__((always_inline)) {
-      constexpr int at = decltype(place)::value - 10 * CT, one = 4 * CT;
-      if constexpr (at >= 0) {
-        constexpr int first = at < one ? at : one + 2 * (at - one), last = at < one ? at + 1 : first + 2;
-        static_for<first, last>([&](auto two) __attribute__((always_inline)) {
-          constexpr int cc = decltype(two)::value >> 3, ee = 2 * (decltype(two)::value & 7);
-          if constexpr (MAP == 0) {
-            mx[cc] = ee == 0 ? fmaxf(acc[cc][0], acc[cc][1]) : fmaxf(fmaxf(mx[cc], acc[cc][ee]), acc[cc][ee + 1]);
-          } else {
-            if constexpr (ee == 0) base = bias_base(cc, key_next);
-            const float z0 = map_seen(acc[cc][ee], cc, ee, base), z1 = map_seen(acc[cc][ee + 1], cc, ee + 1, base);
-            sn[cc][ee] = z0;
-            sn[cc][ee + 1] = z1;
-            mx[cc] = ee == 0 ? fmaxf(z0, z1) : fmaxf(fmaxf(mx[cc], z0), z1);
-          }
-          asm volatile("" : "+v"(mx[cc]));
-        });
-      }
-    };
-    float even = 0.0f;
-    static_for<0, 16>([&](auto piece) __attribute__((always_inline)) {
+    static_for<0, 16>([&](auto piece) INLINE {
       constexpr int j = decltype(piece)::value;
       if constexpr (j < 6) fr[j + 2] = k_frag(kat, j + 2);
       else if constexpr (j < 14) fr[j + 2] = v_frag(vat, j - 6);
       else fr[j + 2] = k_frag(kafter, j - 14);
-      static_for<0, CT>([&](auto tile) __attribute__((always_inline)) {
-        constexpr int ct = decltype(tile)::value, at = CT * j + ct;  // matrix instruction; element of s
-        constexpr int c = at >> 4, e = at & 15;
-        const f32x16 zero = {};
-        if constexpr (j < 8) {
-          acc[ct] = Mx<BF>::mfma32(fr[j], qf[ct][j], j == 0 ? zero : acc[ct]);
-        } else {
-          constexpr int i = (j - 8) >> 2, d = j & 3;
-          o[ct][d] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[ct][i]), o[ct][d]);
-        }
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][e], c1, nr[c]));
-        if constexpr (e % 2 == 0) {
-          even = x;
-        } else {
-          const typename Mx<BF>::v2 pair = {(vt)even, (vt)x};
-          l[c] = Mx<BF>::add_pair(pair, l[c]);
-          // pinned: the compiler would move it to where it is used, behind the branch
-          uint32_t word = __builtin_bit_cast(uint32_t, pair);
-          asm volatile("" : "+v"(word), "+v"(l[c]));
-          pr[c][e >> 3][(e & 7) >> 1] = word;
-        }
-        last_max(std::integral_constant<int, at>());
-        __builtin_amdgcn_sched_barrier(0);
-      });
+      const f32x16 zero = {};
+      if constexpr (j < 8) acc = Mx<BF>::mfma32(fr[j], qf[j], j == 0 ? zero : acc);
+      else o[j & 3] = Mx<BF>::mfma32(fr[j], __builtin_bit_cast(v8, pp[(j - 8) >> 2]), o[j & 3]);
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j], c1, nr));
+      if constexpr (j % 2 == 0) {
+        even = x;
+      } else {
+        const typename Mx<BF>::v2 pair = {(vt)even, (vt)x};
+        l = Mx<BF>::add_pair(pair, l);
+        // pinned: the compiler would move it to where it is used, behind the branch
+        uint32_t word = __builtin_bit_cast(uint32_t, pair);
+        asm volatile("" : "+v"(word), "+v"(l));
+        pr[j >> 3][(j & 7) >> 1] = word;
+      }
+      // once the scores are complete: map them, and the maximum, a pair or two at a time
+      if constexpr (j >= 10) {
+        constexpr int first = j < 14 ? j - 10 : 4 + 2 * (j - 14), last = j < 14 ? first + 1 : first + 2;
+        static_for<first, last>([&](auto two) INLINE {
+          constexpr int e = 2 * decltype(two)::value;
+          if constexpr (MAP == 0) {
+            mx = e == 0 ? fmaxf(acc[0], acc[1]) : fmaxf(fmaxf(mx, acc[e]), acc[e + 1]);
+          } else {
+            if constexpr (e == 0) base = bias_base(key_next);
+            sn[e] = map_seen(acc[e], e, base);
+            sn[e + 1] = map_seen(acc[e + 1], e + 1, base);
+            mx = e == 0 ? fmaxf(sn[0], sn[1]) : fmaxf(fmaxf(mx, sn[e]), sn[e + 1]);
+          }
+          asm volatile("" : "+v"(mx));
+        });
+      }
+      __builtin_amdgcn_sched_barrier(0);
     });
-    if constexpr (MAP == 0) {
-#pragma unroll
-      for (int c = 0; c < CT; ++c) sn[c] = acc[c];
-    }
+    if constexpr (MAP == 0) sn = acc;
     ka = fr[16];
     kb = fr[17];
   };
+
   if (nb > 0) {
-    float f[CT];
-    int b = 0;
-    if constexpr (CT == 1) {  // K of block 4 takes the stage of block 0's
-      wait_vm<4>();
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      scores(stage(0), sa);
-    }
+    float f;
+    wait_vm<4>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    scores(stage(0), sa);  // before K of block 4 takes its stage
     advance(0);
     prepare(0);
-    if constexpr (CT == 2) scores(stage(0), sa);
-    map_half(sa, key0);
-    maxima(sa);
-    mask_half(sa, key0);
+    map_block(sa, key0);
+    mask_block(sa, key0);
     raise(f);  // (O is 0, or infinite)
-    scores(CT == 1 ? stage(1) : stage(0) + kHalf, sb);
+    scores(stage(1), sb);
     exponentials(sa, pa);
-    map_half(sb, key0 + 32);
-    maxima(sb);
-    mask_half(sb, key0 + 32);
+    map_block(sb, key0 + kBlock);
+    mask_block(sb, key0 + kBlock);
     // where it is raised, the product that is still to come is in the old scale: O follows after it
     bool up = raise(f);
-    v8 ka = k_frag(stage(3 - CT), 0), kb = k_frag(stage(3 - CT), 1);
-    if constexpr (CT == 1) {
+    v8 ka = k_frag(stage(2), 0), kb = k_frag(stage(2), 1);
+    int b = 1;
 #pragma unroll 1
-      for (b = 1; b + 1 < nb; b += 2) {  // halves b and b + 1
-        advance(b);
-        prepare(b);
-        half_step(sb, pb, stage(b + 1), sa, key0 + 32 * (b + 1), stage(b - 1), pa, ka, kb, stage(b + 2));
-        if (up) rescale(f);
-        mask_half(sa, key0 + 32 * (b + 1));
-        up = raise(f);
-        advance(b + 1);
-        prepare(b + 1);
-        half_step(sa, pa, stage(b + 2), sb, key0 + 32 * (b + 2), stage(b), pb, ka, kb, stage(b + 3));
-        if (up) rescale(f);
-        mask_half(sb, key0 + 32 * (b + 2));
-        up = raise(f);
-      }
+    for (; b + 1 < nb; b += 2) {  // blocks b and b + 1
       advance(b);
       prepare(b);
-    } else {
-#pragma unroll 1
-      for (; b + 1 < nb; ++b) {  // the second half of block b, the first half of block b + 1
-        const uint32_t s0 = stage(b), s1 = stage(b + 1), s2 = stage(b + 2);
-        const int key = key0 + (b + 1) * kKeys;
-        half_step(sb, pb, s1, sa, key, s0, pa, ka, kb, s1 + kHalf);
-        if (up) rescale(f);
-        mask_half(sa, key);
-        up = raise(f);
-        advance(b + 1);
-        prepare(b + 1);
-        half_step(sa, pa, s1 + kHalf, sb, key + 32, s0 + kHalf, pb, ka, kb, s2);
-        if (up) rescale(f);
-        mask_half(sb, key + 32);
-        up = raise(f);
-      }
+      step(sb, pb, stage(b + 1), sa, key0 + kBlock * (b + 1), stage(b - 1), pa, ka, kb, stage(b + 2));
+      if (up) rescale(f);
+      mask_block(sa, key0 + kBlock * (b + 1));
+      up = raise(f);
+      advance(b + 1);
+      prepare(b + 1);
+      step(sa, pa, stage(b + 2), sb, key0 + kBlock * (b + 2), stage(b), pb, ka, kb, stage(b + 3));
+      if (up) rescale(f);
+      mask_block(sb, key0 + kBlock * (b + 2));
+      up = raise(f);
     }
-    product(CT == 1 ? stage(b - 1) : stage(b), pa);
+    advance(b);
+    prepare(b);
+    product(stage(b - 1), pa);
     if (up) rescale(f);
     exponentials(sb, pb);
-    product(CT == 1 ? stage(b) : stage(b) + kHalf, pb);
+    product(stage(b), pb);
   }
 
   // ---- the output, or a part of it ----
   wait_vm<0>();
+  const int r = wave * 32 + lr;
+  l += __shfl_xor(l, 32, kWave);
+  if (r >= rows) return;
+  if (parts == 1) {
+    const int tok = r / G, g = r - tok * G;
+    uint16_t* op = p.out + ((t.a + t.tok0 + tok) * H * G + h * G + g) * kD + 4 * half;
+    const float f = 1.0f / l;
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int r = (wave * CT + c) * 32 + lr;
-    float lt = l[c] + __shfl_xor(l[c], 32, kWave);
-    if (r >= rows) continue;
-    if (parts == 1) {
-      const int tok = r / G, g = r - tok * G;
-      uint16_t* op = p.out + ((t.a + t.tok0 + tok) * H * G + h * G + g) * kD + 4 * half;
-      const float f = 1.0f / lt;
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+      for (int e = 0; e < 16; e += 4) {
+        vt y[4];
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          vt y[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = (vt)(lt == 0.0f ? 0.0f : o[c][d][e + i] * f);
-          *reinterpret_cast<u32x2*>(op + 32 * d + 2 * e) = *reinterpret_cast<u32x2*>(y);
-        }
-    } else {
-      const int64_t pr = (((int64_t)tile * H + h) * p.nsplit + part) * many_rows(CT) + r;
-      float* op = p.part_o + pr * kD + 4 * half;
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; e += 4)
-          *reinterpret_cast<f32x4*>(op + 32 * d + 2 * e) = (f32x4){o[c][d][e], o[c][d][e + 1], o[c][d][e + 2], o[c][d][e + 3]};
-      if (half == 0) {
-        p.part_ml[pr * 2] = Mx<BF>::kShift - nr[c];
-        p.part_ml[pr * 2 + 1] = lt;
+        for (int i = 0; i < 4; ++i) y[i] = (vt)(l == 0.0f ? 0.0f : o[d][e + i] * f);
+        *reinterpret_cast<u32x2*>(op + 32 * d + 2 * e) = *reinterpret_cast<u32x2*>(y);
       }
+  } else {
+    const int64_t pr = (((int64_t)tile * H + h) * p.nsplit + part) * kManyRows + r;
+    float* op = p.part_o + pr * kD + 4 * half;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<f32x4*>(op + 32 * d + 2 * e) = (f32x4){o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+    if (half == 0) {
+      p.part_ml[pr * 2] = Mx<BF>::kShift - nr;
+      p.part_ml[pr * 2 + 1] = l;
     }
   }
 }
 
-// The tiles whose keys were split, a workgroup 16 query rows.
-constexpr int kManyJoin = 16;
+// The tiles whose keys were split, a workgroup 16 query rows, 8 at a time, 32 threads and 4
+// channels a thread each; every part's sums are on their way before the first is used.
+constexpr int kManyJoin = 16, kMaxSplit = 8;
 template <bool BF>
-__global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p, int tile_rows) {
+__global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   int* before = reinterpret_cast<int*>(smem);
-  int* red = before + p.S + 1;
   uint32_t flags = 0;
-  many_plan(p, tile_rows / p.G, before, red, flags);
   const int H = p.c.H, G = p.G, tile = blockIdx.x / H, h = blockIdx.x % H;
-  if (tile >= before[p.S]) return;
-  const ManyTile t = many_tile(p, tile_rows / G, before, tile, h, red);
-  const int parts = parts_of(max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 0), p.nsplit), rows = t.toks * G;
+  ManyTile t;
+  if (!many_tile(p, kManyRows / G, tile, h, before, before + p.S + 1, &t, flags)) return;
+  const int parts = parts_of(units_of(t), p.nsplit), rows = t.toks * G;
   if (parts == 1) return;
-  const int64_t base = ((int64_t)tile * H + h) * p.nsplit * tile_rows;
-  // 8 rows at a time, 32 threads and 4 channels a thread each
+  const int64_t base = ((int64_t)tile * H + h) * p.nsplit * kManyRows;
   const int x = threadIdx.x & 31;
 #pragma unroll
   for (int i = 0; i < kManyJoin; i += 8) {
     const int r = blockIdx.y * kManyJoin + i + (threadIdx.x >> 5);
     if (r >= rows) return;
-    float M = -__builtin_huge_valf();
-    for (int c = 0; c < parts; ++c) M = fmaxf(M, p.part_ml[2 * (base + (int64_t)c * tile_rows + r)]);
+    float m[kMaxSplit], lp[kMaxSplit], M = -__builtin_huge_valf();
+    f32x4 v[kMaxSplit];
+#pragma unroll
+    for (int c = 0; c < kMaxSplit; ++c) {
+      m[c] = -__builtin_huge_valf();
+      if (c >= parts) continue;
+      const int64_t pr = base + (int64_t)c * kManyRows + r;
+      m[c] = p.part_ml[2 * pr];
+      lp[c] = p.part_ml[2 * pr + 1];
+      v[c] = *reinterpret_cast<const f32x4*>(p.part_o + pr * kD + 4 * x);
+    }
+#pragma unroll
+    for (int c = 0; c < kMaxSplit; ++c) M = fmaxf(M, m[c]);
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     float l = 0.0f;
-    for (int c = 0; c < parts; ++c) {
-      const int64_t pr = base + (int64_t)c * tile_rows + r;
-      const float m = p.part_ml[2 * pr];
-      if (m == -__builtin_huge_valf()) continue;
-      const float w = __builtin_amdgcn_exp2f(m - M);
-      l += w * p.part_ml[2 * pr + 1];
-      o += w * *reinterpret_cast<const f32x4*>(p.part_o + pr * kD + 4 * x);
+#pragma unroll
+    for (int c = 0; c < kMaxSplit; ++c) {
+      if (c >= parts) continue;
+      const float w = __builtin_amdgcn_exp2f(m[c] - M);
+      l += w * lp[c];
+      o += w * v[c];
     }
     const int tok = r / G, g = r - tok * G;
     typename Mx<BF>::t y[4];
@@ -1398,7 +1341,7 @@ struct PagedAttnPlan {
   int few, R;         // rows up to which a request goes to attn_few_kernel; the rows it is built for
   bool run_few, run_many;
   int64_t tiles;      // bound on attn_many_kernel's row tiles
-  int nsplit, ct;     // parts of a tile's keys at most; column tiles of a wave
+  int nsplit;         // parts of a tile's keys at most
   int64_t part_rows;  // rows of partial results
 };
 
@@ -1410,22 +1353,22 @@ static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) 
   a.run_many = most > kFewRows;
   // one request whose rows are all there are is known to be large; more may be of either kind
   a.run_few = !a.run_many || S > 1 || T <= kFewRows / G;
-  a.ct = getenv("FCT") ? atoi(getenv("FCT")) : 2;
-  const int tm = many_rows(a.ct) / G;
+  const int tm = kManyRows / G;
   a.nsplit = 1;
   if (a.run_many) {
     const int64_t large = T / (kFewRows / G + 1) < S ? T / (kFewRows / G + 1) : S;  // requests that can be large
     a.tiles = T / tm + large;
-    // fill 256 CUs: the fewest parts that leave at most a tenth of them idle in the last round
+    // two workgroups on each of 256 CUs: the fewest parts that leave at most a tenth of the
+    // places idle in the last round
     const int64_t wgs = (T + tm - 1) / tm * H;
-    for (int ns = 1; ns <= 8; ++ns) {
-      const int64_t rounds = (wgs * ns + 255) / 256;
+    for (int ns = 1; ns <= kMaxSplit; ++ns) {
+      const int64_t rounds = (wgs * ns + 511) / 512;
       a.nsplit = ns;
-      if (wgs * ns * 10 >= rounds * 256 * 9 || wgs * ns > 2048) break;
+      if (wgs * ns * 10 >= rounds * 512 * 9 || wgs * ns > 4096) break;
     }
   }
   const int64_t few_rows = a.run_few ? (int64_t)kFewWorkers * 2 * a.R : 0;
-  const int64_t many_part = a.run_many && a.nsplit > 1 ? a.tiles * H * a.nsplit * many_rows(a.ct) : 0;
+  const int64_t many_part = a.run_many && a.nsplit > 1 ? a.tiles * H * a.nsplit * kManyRows : 0;
   a.part_rows = few_rows > many_part ? few_rows : many_part;
   return a;
 }
@@ -1435,28 +1378,20 @@ size_t paged_attn_ws_bytes(int64_t T, int S, int H, int G, int64_t max_new) {
   return (size_t)a.part_rows * (kD + 2) * sizeof(float) + 1024;
 }
 
-template <bool BF, int CT>
-static void launch_many(const PagedAttnArgs& p, const PagedAttnPlan& a, size_t plan, hipStream_t s) {
-  const dim3 grid((unsigned)(a.tiles * a.nsplit * p.c.H)), threads(256);
-  const size_t lds = many_lds(CT) + plan;
-  if (p.softcap > 0.0f) hipLaunchKernelGGL((attn_many_kernel<BF, 2, CT>), grid, threads, lds, s, p);
-  else if (p.slopes || !(p.sm_scale > 0.0f)) hipLaunchKernelGGL((attn_many_kernel<BF, 1, CT>), grid, threads, lds, s, p);
-  else hipLaunchKernelGGL((attn_many_kernel<BF, 0, CT>), grid, threads, lds, s, p);
-}
-
 template <bool BF>
 static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) {
   const size_t plan = (size_t)(p.S + 1 + 12) * sizeof(int);
-  p.tiles = (int)a.tiles;
   p.nsplit = a.nsplit;
   p.few = a.few;
   if (a.run_many) {
-    if (a.ct == 1) launch_many<BF, 1>(p, a, plan, s);
-    else launch_many<BF, 2>(p, a, plan, s);
+    const dim3 grid((unsigned)(a.tiles * a.nsplit * p.c.H)), threads(256);
+    const size_t lds = kManyLds + plan;
+    if (p.softcap > 0.0f) hipLaunchKernelGGL((attn_many_kernel<BF, 2>), grid, threads, lds, s, p);
+    else if (p.slopes || !(p.sm_scale > 0.0f)) hipLaunchKernelGGL((attn_many_kernel<BF, 1>), grid, threads, lds, s, p);
+    else hipLaunchKernelGGL((attn_many_kernel<BF, 0>), grid, threads, lds, s, p);
     if (a.nsplit > 1)
-      hipLaunchKernelGGL((attn_many_join_kernel<BF>),
-                         dim3((unsigned)(a.tiles * p.c.H), (unsigned)(many_rows(a.ct) / kManyJoin)), dim3(256), plan, s,
-                         p, many_rows(a.ct));
+      hipLaunchKernelGGL((attn_many_join_kernel<BF>), dim3((unsigned)(a.tiles * p.c.H), kManyRows / kManyJoin), threads,
+                         plan, s, p);
   }
   if (a.run_few) {
     const dim3 grid(kFewWorkers / kFewWaves), threads(kFewWaves * kWave);
