@@ -487,7 +487,8 @@ fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fa
  * Scores, softmax statistics and sums are fp32; the probabilities of chunks (more
  * than 32 query rows, new*G, of a request) are rounded to the pages' type once, those of
  * fewer rows enter as a sum of two such values.  Sums are in an order that
- * depends on the lengths and sizes only.  1 <= G <= 8; T*H*G <= 2^30.
+ * depends on the lengths and sizes only.  1 <= G <= 8; T*H*G <= 2^30;
+ * S*ld_table*page <= 2^35.
  * Device status: BAD_N (n outside [0, ld_table*page], more new tokens than n or than
  * max_new, a start out of order or outside [0, T]: that request's rows are left as
  * they were), BAD_PAGE.

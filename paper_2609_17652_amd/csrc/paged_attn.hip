@@ -21,7 +21,7 @@
 // requests and heads are cut into equal shares, one per wave, whatever the
 // lengths are; each wave runs its share through two private LDS stages without
 // meeting the others, and pieces of a request join in attn_join_kernel.
-// attn_many_kernel takes the others, 256 query rows a workgroup, bound by the
+// attn_many_kernel takes the others, 128 query rows a workgroup, bound by the
 // matrix cores; keys are split over workgroups where the tiles are few.
 //
 // Rows that a query must not see get a probability of 0, but 0 * Inf is not 0:
@@ -59,7 +59,6 @@ constexpr int kBlockBytes = kBlock * kRowBytes;
 constexpr int kManyStages = 4;    // blocks in each of the rings of K and V
 constexpr int kManyLds = 2 * kManyStages * kBlockBytes;
 constexpr int kManyKeys = 64;     // keys are divided among workgroups by these
-constexpr int kNone = -(1 << 30);
 
 struct PagedAttnArgs {
   const uint16_t* q;
@@ -295,29 +294,39 @@ __device__ __forceinline__ int few_lo(const PagedAttnArgs& p, int64_t a, int row
 }
 
 // Blocks of 32 keys of the requests: before[s] those of the requests before s (of one
-// head), before[S] all.  Every thread of the workgroup; `part` one entry a wave.
+// head), before[S] all.  Every thread of the workgroup; `part` one entry a wave.  Up to 64
+// requests every wave writes the same by itself, a lane a request, without a barrier.
+__device__ __forceinline__ int few_blocks(const PagedAttnArgs& p, int s, uint32_t& flags) {
+  int64_t a, n;
+  const int rows = request_rows(p, s, &a, &n, flags);
+  if (rows == 0 || rows * p.G > p.few) return 0;  // else one block at least, for rows that see nothing
+  return max(((int)n - few_lo(p, a, rows, n) + kFewKeys - 1) / kFewKeys, 1);
+}
+__device__ __forceinline__ int scan_add(int v) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(v, o, kWave);
+    if ((int)(threadIdx.x & 63) >= o) v += x;
+  }
+  return v;
+}
 __device__ __forceinline__ void few_plan(const PagedAttnArgs& p, int* before, int* part, uint32_t& flags) {
   const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63, wave = tid >> 6;
+  if (p.S <= kWave) {
+    const int nb = lane < p.S ? few_blocks(p, lane, flags) : 0, inc = scan_add(nb);
+    if (lane < p.S) before[lane] = inc - nb;
+    if (lane == kWave - 1) before[p.S] = inc;
+    return;
+  }
   const int per = (p.S + nt - 1) / nt;
   int sum = 0;
   for (int i = 0; i < per; ++i) {
     const int s = tid * per + i;
-    int nb = 0;
-    if (s < p.S) {
-      int64_t a, n;
-      const int rows = request_rows(p, s, &a, &n, flags);
-      if (rows > 0 && rows * p.G <= p.few)  // one block at least, for rows that see nothing
-        nb = max(((int)n - few_lo(p, a, rows, n) + kFewKeys - 1) / kFewKeys, 1);
-      before[s] = sum;
-    }
-    sum += nb;
+    if (s >= p.S) break;
+    before[s] = sum;
+    sum += few_blocks(p, s, flags);
   }
-  int inc = sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(inc, o, kWave);
-    if (lane >= o) inc += x;
-  }
+  const int inc = scan_add(sum);
   if (lane == 63) part[wave] = inc;
   __syncthreads();
   int base = inc - sum;
@@ -424,13 +433,13 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
       x.n = uniform((int)fixed(p.n, x.s));
     }
   };
-  // page numbers of the 16-key groups of a place's block (-1: behind the end or absent)
+  // page numbers of the 16-key groups of a place's block (-1 behind the end)
   auto pages = [&](const Place& x, int (&id)[2]) {
     const int key = x.lo + kFewKeys * x.b;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int k = key + 16 * i;
-      id[i] = k < x.n ? page_uniform(p.c, x.s, k >> p.c.shift) : kNone;
+      id[i] = k < x.n ? page_uniform(p.c, x.s, k >> p.c.shift) : -1;
     }
   };
   auto issue = [&](const Place& x, const int (&id)[2], int stage) {
@@ -514,7 +523,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
       const int key = lo_key + kFewKeys * b;
       const int cur0 = id[0][0], cur1 = id[0][1];
       const bool in0 = (uint32_t)cur0 < (uint32_t)p.c.P, in1 = (uint32_t)cur1 < (uint32_t)p.c.P;
-      if ((!in0 && cur0 != kNone) || (!in1 && cur1 != kNone)) flags |= FATHOM_DEV_BAD_PAGE;
+      if ((!in0 && key < n) || (!in1 && key + 16 < n)) flags |= FATHOM_DEV_BAD_PAGE;
       const bool masked = key < lo_max || key + kFewKeys > hi_min || !in0 || !in1;
       if (masked && (key + kFewKeys > n || !in0 || !in1)) {  // rows that are not there: V is cleared
 #pragma unroll
@@ -664,12 +673,13 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
   if (flags && lane == 0) set_status(p.st, flags);
 }
 
-// The requests of attn_few_kernel whose blocks went to more than one wave: a workgroup a
-// query row, out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over the row's parts, in a
-// fixed order.  Block counts are recomputed from the lengths.  A trip to memory for the
-// lengths, one for every part's (m, l), a thread a part, and one for eight parts' sums at a
+// The requests and heads of attn_few_kernel whose blocks went to more than one wave: a
+// workgroup a query row, out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over the row's
+// parts, in a fixed order.  Block counts are recomputed from the lengths.  A trip to memory for
+// the lengths, one for every part's (m, l), a thread a part, and one for eight parts' sums at a
 // time, 32 threads and 4 channels a thread each (one part after another: 14 us for 128
-// parts, where this takes 5).
+// parts, where this takes 6).  blockIdx.x is the request and head or, where these are more than
+// the waves' bounds, the bound: the first inside of a request and head joins it.
 constexpr int kJoinGroups = 8, kJoinBatch = 8;
 template <bool BF>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) {
@@ -677,16 +687,22 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
   __shared__ float weight[kFewWorkers], red_m[4], red_l[4];
   __shared__ f32x4 acc[kJoinGroups][32];
   int* before = reinterpret_cast<int*>(smem);
-  const int s = blockIdx.x, h = blockIdx.y / R, r = blockIdx.y % R, H = p.c.H, G = p.G;
-  const int64_t a = fixed(p.start, s);
-  if (r >= (fixed(p.start, s + 1) - a) * G) return;
+  const int r = blockIdx.y, H = p.c.H, G = p.G;
+  const bool bounds = p.S * H >= kFewWorkers;
   uint32_t flags = 0;
   few_plan(p, before, before + p.S + 1, flags);
+  const int64_t W = (int64_t)uniform(before[p.S]) * H;
+  const int64_t at = share(blockIdx.x + 1, W), last = share(blockIdx.x, W);
+  if (bounds && (at == last || at >= W)) return;
+  const int s = bounds ? uniform(request_of(before, p.S, (int)quotient(at, H))) : blockIdx.x / H;
   const int nb = uniform(before[s + 1] - before[s]);
   if (nb == 0) return;
-  const int64_t W = (int64_t)uniform(before[p.S]) * H, g0 = (int64_t)uniform(before[s]) * H + (int64_t)h * nb;
+  const int64_t a = fixed(p.start, s);
+  if (r >= (fixed(p.start, s + 1) - a) * G) return;
+  const int h = bounds ? (int)quotient(at - (int64_t)uniform(before[s]) * H, nb) : blockIdx.x % H;
+  const int64_t g0 = (int64_t)uniform(before[s]) * H + (int64_t)h * nb;
   const int w0 = worker_of(g0, W), count = worker_of(g0 + nb - 1, W) - w0 + 1;
-  if (count == 1) return;
+  if (count == 1 || (bounds && (at == g0 || last > g0))) return;
   const int tid = threadIdx.x, x = tid & 31, g = tid >> 5;
   // a part is its wave's first piece, but for a wave that begins in an earlier request or head
   const int64_t row0 = (int64_t)w0 * 2 * R + r, step = 2 * R;
@@ -750,10 +766,17 @@ struct ManyTile {
   int64_t a;                       // the request's first row
 };
 
-// Tile `tile` of those of all requests with more than `few` query rows, tm tokens each (later
-// tiles, which see more, first); false where there are fewer.  Up to 64 requests a wave finds
-// it by itself, a lane a request; more go through `before` [S + 1] in LDS.  Every thread of
-// 256; red[12] is LDS.
+// The tile that is taken as the i-th of n (each by `times` workgroups): later ones, which see
+// more, first.  Where all workgroups run at once, two a CU, the second half goes the other way
+// up, so that long and short ones share a CU (2048 new tokens 61 us -> 56, 2 x 1024 48 -> 40).
+__device__ __forceinline__ int tile_order(int n, int i, int times) {
+  const int first = (n + 1) / 2;
+  return i >= first && i < n && n * times <= 512 ? i - first : n - 1 - i;
+}
+
+// Tile `tile` of those of all requests with more than `few` query rows, tm tokens each; false
+// where there are fewer.  Up to 64 requests a wave finds it by itself, a lane a request; more
+// go through `before` [S + 1] in LDS.  Every thread of 256; red[12] is LDS.
 __device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int tile, int h, int* before, int* red,
                                           ManyTile* t, uint32_t& flags) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -766,13 +789,8 @@ __device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int ti
       rows = request_rows(p, lane, &a, &n, flags);
       if (rows * p.G > p.few) tiles = (rows + tm - 1) / tm;
     }
-    int inc = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(inc, o, kWave);
-      if (lane >= o) inc += y;
-    }
-    x = __builtin_amdgcn_readlane(inc, kWave - 1) - 1 - tile;
+    const int inc = scan_add(tiles);
+    x = tile_order(__builtin_amdgcn_readlane(inc, kWave - 1), tile, p.c.H * p.nsplit);
     if (x < 0) return false;
     t->s = uniform(__builtin_popcountll(__ballot(inc <= x)));  // requests that end before tile x
     first = __builtin_amdgcn_readlane(inc - tiles, t->s);
@@ -790,12 +808,7 @@ __device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int ti
       before[s] = sum;
       if (rows * p.G > p.few) sum += (rows + tm - 1) / tm;
     }
-    int inc = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(inc, o, kWave);
-      if (lane >= o) inc += y;
-    }
+    const int inc = scan_add(sum);
     if (lane == 63) red[wave] = inc;
     __syncthreads();
     int base = inc - sum;
@@ -804,7 +817,7 @@ __device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int ti
       if (tid * per + i < p.S) before[tid * per + i] += base;
     if (tid == 255) before[p.S] = base + sum;
     __syncthreads();
-    x = uniform(before[p.S]) - 1 - tile;
+    x = tile_order(uniform(before[p.S]), tile, p.c.H * p.nsplit);
     if (x < 0) return false;
     t->s = uniform(request_of(before, p.S, x));
     first = uniform(before[t->s]);
@@ -1338,7 +1351,7 @@ __global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
 
 // ---------------------------------------------------------------- launches
 struct PagedAttnPlan {
-  int few, R;         // rows up to which a request goes to attn_few_kernel; the rows it is built for
+  int few, R, rows;   // rows up to which a request goes to attn_few_kernel, that it is built for and that there can be
   bool run_few, run_many;
   int64_t tiles;      // bound on attn_many_kernel's row tiles
   int nsplit;         // parts of a tile's keys at most
@@ -1350,6 +1363,7 @@ static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) 
   const int64_t most = (max_new < T ? max_new : T) * G;  // query rows of a request and head, at most
   a.few = kFewRows;
   a.R = most <= 16 ? 16 : kFewRows;
+  a.rows = (int)(most < kFewRows ? most : kFewRows);
   a.run_many = most > kFewRows;
   // one request whose rows are all there are is known to be large; more may be of either kind
   a.run_few = !a.run_many || S > 1 || T <= kFewRows / G;
@@ -1398,8 +1412,9 @@ static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) 
     const size_t lds = (size_t)kFewWaves * 2 * kFewStage + plan;
     if (a.R == 16) hipLaunchKernelGGL((attn_few_kernel<BF, 1>), grid, threads, lds, s, p);
     else hipLaunchKernelGGL((attn_few_kernel<BF, kFewRows / 16>), grid, threads, lds, s, p);
-    hipLaunchKernelGGL((attn_join_kernel<BF>), dim3((unsigned)p.S, (unsigned)(p.c.H * a.R)), dim3(256), plan, s, p,
-                       a.R);
+    const int pairs = p.S * p.c.H;
+    hipLaunchKernelGGL((attn_join_kernel<BF>), dim3((unsigned)(pairs < kFewWorkers ? pairs : kFewWorkers - 1), (unsigned)a.rows),
+                       dim3(256), plan, s, p, a.R);
   }
 }
 

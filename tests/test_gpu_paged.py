@@ -350,6 +350,23 @@ def test_attn_many_rows(i):
     attn_case(100 + i, reqs, H, G, page, dt, "head" if i % 2 else "token", pad=i % 3, lead=i % 2)
 
 
+CROWDS = [  # more requests than a wave has lanes, than a workgroup has threads, and more (request, head) than waves
+    ([(3000, 1)] + [(20 + i, 1) for i in range(69)], 1, 4, 16, "f16"),
+    ([(1 + 5 * (i % 7), 1 + (i % 7)) for i in range(330)] + [(900, 2)], 1, 3, 16, "bf16"),
+    ([(33 + i % 5, i % 3) for i in range(150)] + [(2500, 4), (600, 1)], 8, 2, 32, "bf16"),
+    ([(40 + i, 1 + (i % 3) * 20) for i in range(66)] + [(700, 500), (0, 0)], 2, 4, 32, "f16"),
+    ([(64, 33 if i % 90 == 7 else 1) for i in range(300)], 4, 1, 64, "bf16"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(CROWDS)))
+@pytest.mark.parametrize("docs", [False, True])
+def test_attn_many_requests(i, docs):
+    reqs, H, G, page, dt = CROWDS[i]
+    attn_case(200 + i, reqs, H, G, page, dt, "head" if i % 2 else "token",
+              docs=(lambda s, pos: pos // 50 * 50 + (s % 3 == 0) * 7) if docs else None)
+
+
 MIXED = [(400, 1), (300, 150), (90, 5), (129, 64), (40, 40), (700, 2)]
 
 
