@@ -60,6 +60,7 @@ constexpr int kManyStages = 4;    // blocks in each of the rings of K and V
 constexpr int kManyLds = 2 * kManyStages * kBlockBytes;
 constexpr int kManyKeys = 64;     // keys are divided among workgroups by these
 
+struct TileRecord;
 struct PagedAttnArgs {
   const uint16_t* q;
   int64_t ldq_tok, ldq_head;
@@ -73,6 +74,8 @@ struct PagedAttnArgs {
   uint16_t* out;
   float *part_o, *part_ml;  // partial results: rows of kD sums, and (maximum, sum) of each
   int nsplit;               // attn_many_kernel: parts of a tile's keys at most
+  TileRecord* tiles;        // its tiles, of more than 64 requests
+  int64_t ntiles;
   uint32_t* st;
 };
 
@@ -293,9 +296,6 @@ __device__ __forceinline__ int few_lo(const PagedAttnArgs& p, int64_t a, int row
   return (int)(lo & ~(int64_t)(kFewKeys - 1));
 }
 
-// Blocks of 32 keys of the requests: before[s] those of the requests before s (of one
-// head), before[S] all.  Every thread of the workgroup; `part` one entry a wave.  Up to 64
-// requests every wave writes the same by itself, a lane a request, without a barrier.
 __device__ __forceinline__ int few_blocks(const PagedAttnArgs& p, int s, uint32_t& flags) {
   int64_t a, n;
   const int rows = request_rows(p, s, &a, &n, flags);
@@ -310,31 +310,39 @@ __device__ __forceinline__ int scan_add(int v) {
   }
   return v;
 }
+// before[s] = the sum of count(r) over r < s, s <= S; every thread, `part` one entry a wave.
+template <class Fn>
+__device__ __forceinline__ void sums_before(int S, int* before, int* part, Fn count) {
+  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63, wave = tid >> 6, per = (S + nt - 1) / nt;
+  for (int s = tid; s < S; s += nt) before[s] = count(s);
+  __syncthreads();
+  int sum = 0;
+  for (int s = tid * per; s < min((tid + 1) * per, S); ++s) sum += before[s];
+  const int inc = scan_add(sum);
+  if (lane == 63) part[wave] = inc;
+  __syncthreads();
+  int base = inc - sum;
+  for (int w = 0; w < wave; ++w) base += part[w];
+  for (int s = tid * per; s < min((tid + 1) * per, S); ++s) {
+    const int x = before[s];
+    before[s] = base;
+    base += x;
+  }
+  if (tid == nt - 1) before[S] = base;
+  __syncthreads();
+}
+// Blocks of 32 keys of the requests: before[s] those of the requests before s (of one
+// head), before[S] all.  Every thread of the workgroup.  Up to 64 requests every wave writes
+// the same by itself, a lane a request, without a barrier.
 __device__ __forceinline__ void few_plan(const PagedAttnArgs& p, int* before, int* part, uint32_t& flags) {
-  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = threadIdx.x & 63;
   if (p.S <= kWave) {
     const int nb = lane < p.S ? few_blocks(p, lane, flags) : 0, inc = scan_add(nb);
     if (lane < p.S) before[lane] = inc - nb;
     if (lane == kWave - 1) before[p.S] = inc;
     return;
   }
-  const int per = (p.S + nt - 1) / nt;
-  int sum = 0;
-  for (int i = 0; i < per; ++i) {
-    const int s = tid * per + i;
-    if (s >= p.S) break;
-    before[s] = sum;
-    sum += few_blocks(p, s, flags);
-  }
-  const int inc = scan_add(sum);
-  if (lane == 63) part[wave] = inc;
-  __syncthreads();
-  int base = inc - sum;
-  for (int w = 0; w < wave; ++w) base += part[w];
-  for (int i = 0; i < per; ++i)
-    if (tid * per + i < p.S) before[tid * per + i] += base;
-  if (tid == nt - 1) before[p.S] = base + sum;
-  __syncthreads();
+  sums_before(p.S, before, part, [&](int s) { return few_blocks(p, s, flags); });
 }
 
 // The last s with before[s] <= x (x < before[S]): the request of block x.
@@ -681,13 +689,13 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
 // parts, where this takes 6).  blockIdx.x is the request and head or, where these are more than
 // the waves' bounds, the bound: the first inside of a request and head joins it.
 constexpr int kJoinGroups = 8, kJoinBatch = 8;
-template <bool BF>
+template <bool BF, bool LOOP>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ float weight[kFewWorkers], red_m[4], red_l[4];
   __shared__ f32x4 acc[kJoinGroups][32];
   int* before = reinterpret_cast<int*>(smem);
-  const int r = blockIdx.y, H = p.c.H, G = p.G;
+  const int H = p.c.H, G = p.G;
   const bool bounds = p.S * H >= kFewWorkers;
   uint32_t flags = 0;
   few_plan(p, before, before + p.S + 1, flags);
@@ -698,63 +706,69 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
   const int nb = uniform(before[s + 1] - before[s]);
   if (nb == 0) return;
   const int64_t a = fixed(p.start, s);
-  if (r >= (fixed(p.start, s + 1) - a) * G) return;
+  const int rows = (int)(fixed(p.start, s + 1) - a) * G;
   const int h = bounds ? (int)quotient(at - (int64_t)uniform(before[s]) * H, nb) : blockIdx.x % H;
   const int64_t g0 = (int64_t)uniform(before[s]) * H + (int64_t)h * nb;
   const int w0 = worker_of(g0, W), count = worker_of(g0 + nb - 1, W) - w0 + 1;
   if (count == 1 || (bounds && (at == g0 || last > g0))) return;
   const int tid = threadIdx.x, x = tid & 31, g = tid >> 5;
   // a part is its wave's first piece, but for a wave that begins in an earlier request or head
-  const int64_t row0 = (int64_t)w0 * 2 * R + r, step = 2 * R;
-  const int64_t late = share(w0, W) < g0 ? R : 0;
-  float M = -__builtin_huge_valf(), l = 0.0f;
-  for (int c = tid; c < count; c += 256) {
-    float m = -__builtin_huge_valf();
-    if (share(w0 + c, W) < share(w0 + c + 1, W)) m = p.part_ml[2 * (row0 + c * step + (c == 0 ? late : 0))];
-    weight[c] = m;
-    M = fmaxf(M, m);
-  }
-  M = wave_max(M);
-  if ((tid & 63) == 0) red_m[tid >> 6] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
-  for (int c = tid; c < count; c += 256) {
-    const float m = weight[c];
-    const float w = m == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(m - M);
-    weight[c] = w;
-    if (m != -__builtin_huge_valf()) l += w * p.part_ml[2 * (row0 + c * step + (c == 0 ? late : 0)) + 1];
-  }
-  l = wave_sum(l);
-  if ((tid & 63) == 0) red_l[tid >> 6] = l;
-  __syncthreads();
-  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int c0 = g; c0 < count; c0 += kJoinGroups * kJoinBatch) {
-    f32x4 v[kJoinBatch];
-    float w[kJoinBatch];
-#pragma unroll
-    for (int i = 0; i < kJoinBatch; ++i) {
-      const int c = c0 + i * kJoinGroups;
-      w[i] = c < count ? weight[c] : 0.0f;
-      v[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-      if (w[i] != 0.0f)  // a part without weight may not be there
-        v[i] = *reinterpret_cast<const f32x4*>(p.part_o + (row0 + c * step + (c == 0 ? late : 0)) * kD + 4 * x);
+  const int64_t step = 2 * R, late = share(w0, W) < g0 ? R : 0;
+  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+    const int64_t row0 = w0 * step + r;
+    float M = -__builtin_huge_valf(), l = 0.0f;
+    for (int c = tid; c < count; c += 256) {
+      float m = -__builtin_huge_valf();
+      if (share(w0 + c, W) < share(w0 + c + 1, W)) m = p.part_ml[2 * (row0 + c * step + (c == 0 ? late : 0))];
+      weight[c] = m;
+      M = fmaxf(M, m);
     }
+    M = wave_max(M);
+    if ((tid & 63) == 0) red_m[tid >> 6] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+    for (int c = tid; c < count; c += 256) {
+      const float m = weight[c];
+      const float w = m == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(m - M);
+      weight[c] = w;
+      if (m != -__builtin_huge_valf()) l += w * p.part_ml[2 * (row0 + c * step + (c == 0 ? late : 0)) + 1];
+    }
+    l = wave_sum(l);
+    if ((tid & 63) == 0) red_l[tid >> 6] = l;
+    __syncthreads();
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c0 = g; c0 < count; c0 += kJoinGroups * kJoinBatch) {
+      f32x4 v[kJoinBatch];
+      float w[kJoinBatch];
 #pragma unroll
-    for (int i = 0; i < kJoinBatch; ++i) o += w[i] * v[i];
+      for (int i = 0; i < kJoinBatch; ++i) {
+        const int c = c0 + i * kJoinGroups;
+        w[i] = c < count ? weight[c] : 0.0f;
+        v[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+        if (w[i] != 0.0f)  // a part without weight may not be there
+          v[i] = *reinterpret_cast<const f32x4*>(p.part_o + (row0 + c * step + (c == 0 ? late : 0)) * kD + 4 * x);
+      }
+#pragma unroll
+      for (int i = 0; i < kJoinBatch; ++i) o += w[i] * v[i];
+    }
+    acc[g][x] = o;
+    __syncthreads();
+    if (tid >= 32) {
+      if constexpr (LOOP) continue;
+      return;
+    }
+    const float den = (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
+    f32x4 sum = acc[0][tid];
+#pragma unroll
+    for (int i = 1; i < kJoinGroups; ++i) sum += acc[i][tid];
+    const int tok = r / G;
+    typename Mx<BF>::t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(den == 0.0f ? 0.0f : sum[e] / den);
+    *reinterpret_cast<u32x2*>(p.out + ((a + tok) * H * G + h * G + (r - tok * G)) * kD + 4 * tid) =
+        *reinterpret_cast<u32x2*>(y);
+    if constexpr (!LOOP) return;
   }
-  acc[g][x] = o;
-  __syncthreads();
-  if (tid >= 32) return;
-  const float den = (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
-  f32x4 sum = acc[0][tid];
-#pragma unroll
-  for (int i = 1; i < kJoinGroups; ++i) sum += acc[i][tid];
-  const int tok = r / G;
-  typename Mx<BF>::t y[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(den == 0.0f ? 0.0f : sum[e] / den);
-  *reinterpret_cast<u32x2*>(p.out + ((a + tok) * H * G + h * G + (r - tok * G)) * kD + 4 * tid) =
-      *reinterpret_cast<u32x2*>(y);
 }
 
 // ---------------------------------------------------------------- many query rows
@@ -774,14 +788,48 @@ __device__ __forceinline__ int tile_order(int n, int i, int times) {
   return i >= first && i < n && n * times <= 512 ? i - first : n - 1 - i;
 }
 
+// A tile as attn_tiles_kernel writes it; request -1: none.
+struct TileRecord {
+  int s, tok0, total, n;
+  int64_t a;
+};
+
+// Tiles of more than 64 requests with more than `few` query rows each, tm tokens a tile, in the
+// order in which workgroups take them: every workgroup sums over all requests, a thread takes a
+// tile.  (Sums in each of attn_many_kernel's workgroups: 4000 requests of 40 query rows 2.3 ms,
+// this way 1.0.)
+__global__ __launch_bounds__(256) void attn_tiles_kernel(PagedAttnArgs p, int tm) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  int *before = reinterpret_cast<int*>(smem), *part = before + p.S + 1;
+  const int tid = threadIdx.x;
+  uint32_t flags = 0;
+  sums_before(p.S, before, part, [&](int s) {
+    int64_t a, n;
+    const int rows = request_rows(p, s, &a, &n, flags);
+    return rows * p.G > p.few ? (rows + tm - 1) / tm : 0;
+  });
+  if (flags && blockIdx.x == 0) set_status(p.st, flags);
+  const int64_t tile = (int64_t)blockIdx.x * 256 + tid;
+  if (tile >= p.ntiles) return;
+  const int x = tile_order(before[p.S], (int)tile, p.c.H * p.nsplit);
+  TileRecord t = {-1, 0, 0, 0, 0};
+  if (x >= 0) {
+    t.s = request_of(before, p.S, x);
+    t.tok0 = (x - before[t.s]) * tm;
+    t.a = p.start[t.s];
+    t.total = (int)(p.start[t.s + 1] - t.a);
+    t.n = (int)p.n[t.s];
+  }
+  p.tiles[tile] = t;
+}
+
 // Tile `tile` of those of all requests with more than `few` query rows, tm tokens each; false
-// where there are fewer.  Up to 64 requests a wave finds it by itself, a lane a request; more
-// go through `before` [S + 1] in LDS.  Every thread of 256; red[12] is LDS.
-__device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int tile, int h, int* before, int* red,
-                                          ManyTile* t, uint32_t& flags) {
+// where there are fewer.  Up to 64 requests a wave finds it by itself, a lane a request; of more
+// it is read.  Every thread of 256; red[12] is LDS.
+__device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int tile, int h, int* red, ManyTile* t,
+                                          uint32_t& flags) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   t->h = h;
-  int x, first;
   if (p.S <= kWave) {
     int64_t a = 0, n = 0;
     int rows = 0, tiles = 0;
@@ -790,42 +838,22 @@ __device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int ti
       if (rows * p.G > p.few) tiles = (rows + tm - 1) / tm;
     }
     const int inc = scan_add(tiles);
-    x = tile_order(__builtin_amdgcn_readlane(inc, kWave - 1), tile, p.c.H * p.nsplit);
+    const int x = tile_order(__builtin_amdgcn_readlane(inc, kWave - 1), tile, p.c.H * p.nsplit);
     if (x < 0) return false;
     t->s = uniform(__builtin_popcountll(__ballot(inc <= x)));  // requests that end before tile x
-    first = __builtin_amdgcn_readlane(inc - tiles, t->s);
+    t->tok0 = (x - __builtin_amdgcn_readlane(inc - tiles, t->s)) * tm;
     t->total = __builtin_amdgcn_readlane(rows, t->s);
     t->n = __builtin_amdgcn_readlane((int)n, t->s);
     t->a = __builtin_amdgcn_readlane((int)a, t->s);  // (below 2^30)
   } else {
-    const int per = (p.S + 255) / 256;
-    int sum = 0;
-    for (int i = 0; i < per; ++i) {
-      const int s = tid * per + i;
-      if (s >= p.S) break;
-      int64_t a, n;
-      const int rows = request_rows(p, s, &a, &n, flags);
-      before[s] = sum;
-      if (rows * p.G > p.few) sum += (rows + tm - 1) / tm;
-    }
-    const int inc = scan_add(sum);
-    if (lane == 63) red[wave] = inc;
-    __syncthreads();
-    int base = inc - sum;
-    for (int w = 0; w < wave; ++w) base += red[w];
-    for (int i = 0; i < per; ++i)
-      if (tid * per + i < p.S) before[tid * per + i] += base;
-    if (tid == 255) before[p.S] = base + sum;
-    __syncthreads();
-    x = tile_order(uniform(before[p.S]), tile, p.c.H * p.nsplit);
-    if (x < 0) return false;
-    t->s = uniform(request_of(before, p.S, x));
-    first = uniform(before[t->s]);
-    t->a = fixed(p.start, t->s);
-    t->n = uniform((int)fixed(p.n, t->s));
-    t->total = uniform((int)(fixed(p.start, t->s + 1) - t->a));
+    const TileRecord* r = p.tiles + tile;
+    t->s = fixed(&r->s, 0);
+    if (t->s < 0) return false;
+    t->tok0 = fixed(&r->tok0, 0);
+    t->total = fixed(&r->total, 0);
+    t->n = fixed(&r->n, 0);
+    t->a = fixed(&r->a, 0);
   }
-  t->tok0 = (x - first) * tm;
   t->toks = min(tm, t->total - t->tok0);
   t->hi_min = t->n - t->total + t->tok0 + 1;
   if (!p.first && !p.prefix) {
@@ -858,9 +886,12 @@ __device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int ti
   return true;
 }
 
-// The keys of a tile in units of 64, and the parts that they are cut into, of at least 4 each.
-__device__ __forceinline__ int units_of(const ManyTile& t) { return max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 0); }
-__device__ __forceinline__ int parts_of(int units, int nsplit) { return max(min(nsplit, units / 4), 1); }
+// The keys of a tile in units of 64 (one where no query sees any: a loop that may not run costs
+// the kernel spilled registers), and the parts that they are cut into, of at least 4 each (8, 16
+// and 32 are slower).
+constexpr int kUnits = 4;
+__device__ __forceinline__ int units_of(const ManyTile& t) { return max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 1); }
+__device__ __forceinline__ int parts_of(int units, int nsplit) { return max(min(nsplit, units / kUnits), 1); }
 
 // Keys go by in blocks of 32.  While the matrix cores form the scores of the next block and
 // add the last block's product with V, the vector unit takes the exponentials of this one:
@@ -897,12 +928,11 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5, lr = lane & 31;
   const int H = p.c.H, G = p.G;
   const int bid = blockIdx.x, h = bid % H, part = (bid / H) % p.nsplit, tile = bid / H / p.nsplit;
-  int* before = reinterpret_cast<int*>(smem + kManyLds);
-  int* red = before + p.S + 1;
+  int* red = reinterpret_cast<int*>(smem + kManyLds);
   ManyTile t;
   {
     uint32_t flags = 0;
-    const bool some = many_tile(p, kManyRows / G, tile, h, before, red, &t, flags);
+    const bool some = many_tile(p, kManyRows / G, tile, h, red, &t, flags);
     if (flags && blockIdx.x == 0) set_status(p.st, flags);
     if (!some) return;
   }
@@ -1224,47 +1254,45 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
     kb = fr[17];
   };
 
-  if (nb > 0) {
-    float f;
-    wait_vm<4>();
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    scores(stage(0), sa);  // before K of block 4 takes its stage
-    advance(0);
-    prepare(0);
-    map_block(sa, key0);
-    mask_block(sa, key0);
-    raise(f);  // (O is 0, or infinite)
-    scores(stage(1), sb);
-    exponentials(sa, pa);
-    map_block(sb, key0 + kBlock);
-    mask_block(sb, key0 + kBlock);
-    // where it is raised, the product that is still to come is in the old scale: O follows after it
-    bool up = raise(f);
-    v8 ka = k_frag(stage(2), 0), kb = k_frag(stage(2), 1);
-    int b = 1;
+  float f;
+  wait_vm<4>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  scores(stage(0), sa);  // before K of block 4 takes its stage
+  advance(0);
+  prepare(0);
+  map_block(sa, key0);
+  mask_block(sa, key0);
+  raise(f);  // (O is 0, or infinite)
+  scores(stage(1), sb);
+  exponentials(sa, pa);
+  map_block(sb, key0 + kBlock);
+  mask_block(sb, key0 + kBlock);
+  // where it is raised, the product that is still to come is in the old scale: O follows after it
+  bool up = raise(f);
+  v8 ka = k_frag(stage(2), 0), kb = k_frag(stage(2), 1);
+  int b = 1;
 #pragma unroll 1
-    for (; b + 1 < nb; b += 2) {  // blocks b and b + 1
-      advance(b);
-      prepare(b);
-      step(sb, pb, stage(b + 1), sa, key0 + kBlock * (b + 1), stage(b - 1), pa, ka, kb, stage(b + 2));
-      if (up) rescale(f);
-      mask_block(sa, key0 + kBlock * (b + 1));
-      up = raise(f);
-      advance(b + 1);
-      prepare(b + 1);
-      step(sa, pa, stage(b + 2), sb, key0 + kBlock * (b + 2), stage(b), pb, ka, kb, stage(b + 3));
-      if (up) rescale(f);
-      mask_block(sb, key0 + kBlock * (b + 2));
-      up = raise(f);
-    }
+  for (; b + 1 < nb; b += 2) {  // blocks b and b + 1
     advance(b);
     prepare(b);
-    product(stage(b - 1), pa);
+    step(sb, pb, stage(b + 1), sa, key0 + kBlock * (b + 1), stage(b - 1), pa, ka, kb, stage(b + 2));
     if (up) rescale(f);
-    exponentials(sb, pb);
-    product(stage(b), pb);
+    mask_block(sa, key0 + kBlock * (b + 1));
+    up = raise(f);
+    advance(b + 1);
+    prepare(b + 1);
+    step(sa, pa, stage(b + 2), sb, key0 + kBlock * (b + 2), stage(b), pb, ka, kb, stage(b + 3));
+    if (up) rescale(f);
+    mask_block(sb, key0 + kBlock * (b + 2));
+    up = raise(f);
   }
+  advance(b);
+  prepare(b);
+  product(stage(b - 1), pa);
+  if (up) rescale(f);
+  exponentials(sb, pb);
+  product(stage(b), pb);
 
   // ---- the output, or a part of it ----
   wait_vm<0>();
@@ -1304,12 +1332,11 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
 constexpr int kManyJoin = 16, kMaxSplit = 8;
 template <bool BF>
 __global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  int* before = reinterpret_cast<int*>(smem);
+  __shared__ int red[12];
   uint32_t flags = 0;
   const int H = p.c.H, G = p.G, tile = blockIdx.x / H, h = blockIdx.x % H;
   ManyTile t;
-  if (!many_tile(p, kManyRows / G, tile, h, before, before + p.S + 1, &t, flags)) return;
+  if (!many_tile(p, kManyRows / G, tile, h, red, &t, flags)) return;
   const int parts = parts_of(units_of(t), p.nsplit), rows = t.toks * G;
   if (parts == 1) return;
   const int64_t base = ((int64_t)tile * H + h) * p.nsplit * kManyRows;
@@ -1351,11 +1378,12 @@ __global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
 
 // ---------------------------------------------------------------- launches
 struct PagedAttnPlan {
-  int few, R, rows;   // rows up to which a request goes to attn_few_kernel, that it is built for and that there can be
+  int few, R, rows;   // rows up to which a request goes to attn_few_kernel, that it is built for, that there can be
   bool run_few, run_many;
   int64_t tiles;      // bound on attn_many_kernel's row tiles
   int nsplit;         // parts of a tile's keys at most
   int64_t part_rows;  // rows of partial results
+  int64_t records;    // tiles that attn_tiles_kernel writes
 };
 
 static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) {
@@ -1384,37 +1412,41 @@ static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) 
   const int64_t few_rows = a.run_few ? (int64_t)kFewWorkers * 2 * a.R : 0;
   const int64_t many_part = a.run_many && a.nsplit > 1 ? a.tiles * H * a.nsplit * kManyRows : 0;
   a.part_rows = few_rows > many_part ? few_rows : many_part;
+  a.records = S > kWave ? a.tiles : 0;
   return a;
 }
 
 size_t paged_attn_ws_bytes(int64_t T, int S, int H, int G, int64_t max_new) {
   const PagedAttnPlan a = attn_plan(T, S, H, G, max_new);
-  return (size_t)a.part_rows * (kD + 2) * sizeof(float) + 1024;
+  return (size_t)a.part_rows * (kD + 2) * sizeof(float) + (size_t)a.records * sizeof(TileRecord) + 1024;
 }
 
 template <bool BF>
 static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) {
-  const size_t plan = (size_t)(p.S + 1 + 12) * sizeof(int);
-  p.nsplit = a.nsplit;
+  const size_t plan = (size_t)(p.S + 1 + 4) * sizeof(int);
+  const int64_t most = (p.c.ld_table << p.c.shift) / kManyKeys / kUnits;  // parts of the longest request
+  p.nsplit = (int)(most < a.nsplit ? (most > 1 ? most : 1) : a.nsplit);
   p.few = a.few;
   if (a.run_many) {
-    const dim3 grid((unsigned)(a.tiles * a.nsplit * p.c.H)), threads(256);
-    const size_t lds = kManyLds + plan;
+    const dim3 grid((unsigned)(a.tiles * p.nsplit * p.c.H)), threads(256);
+    const size_t lds = kManyLds + 12 * sizeof(int);
+    if (a.records > 0)
+      hipLaunchKernelGGL(attn_tiles_kernel, dim3((unsigned)((a.records + 255) / 256)), threads, plan, s, p, kManyRows / p.G);
     if (p.softcap > 0.0f) hipLaunchKernelGGL((attn_many_kernel<BF, 2>), grid, threads, lds, s, p);
     else if (p.slopes || !(p.sm_scale > 0.0f)) hipLaunchKernelGGL((attn_many_kernel<BF, 1>), grid, threads, lds, s, p);
     else hipLaunchKernelGGL((attn_many_kernel<BF, 0>), grid, threads, lds, s, p);
-    if (a.nsplit > 1)
+    if (p.nsplit > 1)
       hipLaunchKernelGGL((attn_many_join_kernel<BF>), dim3((unsigned)(a.tiles * p.c.H), kManyRows / kManyJoin), threads,
-                         plan, s, p);
+                         0, s, p);
   }
   if (a.run_few) {
     const dim3 grid(kFewWorkers / kFewWaves), threads(kFewWaves * kWave);
     const size_t lds = (size_t)kFewWaves * 2 * kFewStage + plan;
     if (a.R == 16) hipLaunchKernelGGL((attn_few_kernel<BF, 1>), grid, threads, lds, s, p);
     else hipLaunchKernelGGL((attn_few_kernel<BF, kFewRows / 16>), grid, threads, lds, s, p);
-    const int pairs = p.S * p.c.H;
-    hipLaunchKernelGGL((attn_join_kernel<BF>), dim3((unsigned)(pairs < kFewWorkers ? pairs : kFewWorkers - 1), (unsigned)a.rows),
-                       dim3(256), plan, s, p, a.R);
+    const int pairs = p.S * p.c.H, units = pairs < kFewWorkers ? pairs : kFewWorkers - 1;
+    if (a.run_many) hipLaunchKernelGGL((attn_join_kernel<BF, true>), dim3(units, p.G), dim3(256), plan, s, p, a.R);
+    else hipLaunchKernelGGL((attn_join_kernel<BF, false>), dim3(units, a.rows), dim3(256), plan, s, p, a.R);
   }
 }
 
@@ -1442,6 +1474,8 @@ fathom_status launch_paged_attn(const void* q, int64_t ldq_tok, int64_t ldq_head
   p.out = reinterpret_cast<uint16_t*>(out);
   p.part_o = reinterpret_cast<float*>(ws);
   p.part_ml = p.part_o + a.part_rows * kD;
+  p.tiles = reinterpret_cast<TileRecord*>(p.part_ml + a.part_rows * 2);
+  p.ntiles = a.records;
   p.st = st;
   if (bf16) launch_attn<true>(p, a, s);
   else launch_attn<false>(p, a, s);
