@@ -476,7 +476,9 @@ fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fa
  *            rows of T outside every request are left as they were in out.
  *   n        [S] int64 (device): tokens of each request, the new ones among them.
  *   max_new  host bound on start[s + 1] - start[s]; selects work and sizes the launch.
- *   sm_scale, softcap  finite; softcap 0: none.      slopes [H*G] fp32 or NULL.
+ *   sm_scale finite.   softcap 0 (none) or in [2^-10, 2^10]; its tanh is good to 2^-21 of
+ *            softcap, which is why larger ones are not served.
+ *   slopes   [H*G] fp32 or NULL.
  *   prefix   [S] int64 or NULL: leading positions that every token of the request
  *            sees, later ones among them.
  *   first    [T] int64 or NULL: the first position that a token sees (the start of

@@ -421,6 +421,7 @@ fathom_status fathom_paged_attn(const void* q, int64_t ldq_tok, int64_t ldq_head
   if (((int64_t)S * ld_table << c.shift) > ((int64_t)1 << 35)) return FATHOM_ERR_UNSUPPORTED;  // blocks are counted in 32 bits
   if (G < 1 || G > kMaxG || T > ((int64_t)1 << 30) / (c.H * G)) return FATHOM_ERR_UNSUPPORTED;
   if (!(sm_scale - sm_scale == 0.0f) || !(softcap >= 0.0f) || softcap - softcap != 0.0f) return FATHOM_ERR_INVALID;
+  if (softcap > 0.0f && !(softcap >= 0x1p-10f && softcap <= 0x1p10f)) return FATHOM_ERR_UNSUPPORTED;
   if (ldq_tok < 0 || ldq_head < 0 || ((ldq_tok | ldq_head) & 7)) return FATHOM_ERR_INVALID;
   if (S == 0 || T == 0 || max_new == 0) return FATHOM_OK;
   if (!q || !start || !n || !out || !table || ld_table < 1 || pages->P < 1) return FATHOM_ERR_INVALID;

@@ -278,7 +278,8 @@ __device__ __forceinline__ float mapped(const ScoreMap& m, float slope, float s,
 }
 __device__ __forceinline__ ScoreMap score_map(const PagedAttnArgs& p) {
   ScoreMap m;
-  m.c1 = p.softcap > 0.0f ? 2.0f * kLog2e * (p.sm_scale / p.softcap) : p.sm_scale * kLog2e;
+  const float c1 = p.softcap > 0.0f ? 2.0f * kLog2e * (p.sm_scale / p.softcap) : p.sm_scale * kLog2e;
+  m.c1 = fminf(fmaxf(c1, -3.4e38f), 3.4e38f);  // a score of 0 stays 0
   m.cap = p.softcap > 0.0f ? p.softcap * kLog2e : 0.0f;
   return m;
 }

@@ -74,6 +74,21 @@ def test_attn_refusals(fl):
     assert _attn(fl, pg, S=0) == 0 and _attn(fl, pg, T=0, ws_bytes=0) == 0  # nothing to do
 
 
+@pytest.mark.parametrize("cap,code", [(1e-30, "U"), (2.0 ** -11, "U"), (1025.0, "U"), (1e30, "U"), (2.0 ** -10, "ok"),
+                                      (1024.0, "ok"), (0.0, "ok")])
+def test_attn_cap_range(fl, cap, code):
+    """No rows: nothing is launched."""
+    assert _attn(fl, _pg(fl), cap=cap, T=0) == (fl.FATHOM_ERR_UNSUPPORTED if code == "U" else 0)
+
+
+def test_attn_table_positions_are_counted_in_32_bits(fl):
+    """4096 requests of 2^23 positions are the most: S*ld_table*page <= 2^35."""
+    pg = _pg(fl)
+    most = (1 << 23) // pg.page
+    assert _attn(fl, pg, S=4096, ld_table=most, T=0) == 0
+    assert _attn(fl, pg, S=4096, ld_table=most + 1, T=0) == fl.FATHOM_ERR_UNSUPPORTED
+
+
 def test_write_pack_sparse_refusals(fl):
     L, pg = fl.lib(), _pg(fl)
     I, U = fl.FATHOM_ERR_INVALID, fl.FATHOM_ERR_UNSUPPORTED

@@ -367,6 +367,52 @@ def test_attn_many_requests(i, docs):
               docs=(lambda s, pos: pos // 50 * 50 + (s % 3 == 0) * 7) if docs else None)
 
 
+def test_attn_bad_lengths_among_many_requests():
+    """One of 70 requests does not fit together, of few rows or of many: BAD_N, its rows are left, the others served."""
+    rng = np.random.default_rng(21)
+    G, S, bad = 2, 70, 33
+    for new in (1, 20):
+        news, lengths = [new] * S, [30 + i for i in range(S)]
+        table, K, V, Kr, Vr = pools(rng, lengths, 1, 16, torch.float16)
+        q = torch.from_numpy(rng.standard_normal((new * S, G, D)).astype(np.float32)).half()
+        start = [new * i for i in range(S + 1)]
+        said = list(lengths)
+        said[bad] = -1 if new == 1 else 10 ** 12
+        st = F.new_status()
+        out = torch.full((new * S, G, D), 5.0, dtype=torch.float16, device=DEV)
+        F.fathom_paged_attn(q.to(DEV), K, V, table, i64(start), i64(said), new, out=out, dev_status=st)
+        assert status(st) == F.FATHOM_DEV_BAD_N
+        out = out.double().cpu().numpy()
+        for s in range(S):
+            rows = slice(new * s, new * (s + 1))
+            if s == bad:
+                assert (out[rows] == 5.0).all()
+                continue
+            ref, mag, _ = O.paged_attn(q[rows].double().numpy(), Kr[s][0].double().numpy(), Vr[s][0].double().numpy(),
+                                       lengths[s], G, 1 / np.sqrt(D))
+            assert (np.abs(out[rows] - ref) <= 2.0 ** -11 * np.abs(ref) + mag * (2.0 ** -11 + 1e-4)).all()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attn_page_numbers_of_every_kind(new):
+    """A request of nothing but absent pages gives 0 and BAD_PAGE, whatever the numbers are."""
+    rng = np.random.default_rng(22)
+    table, K, V, _, _ = pools(rng, [64], 1, 16, torch.bfloat16)
+    q = torch.from_numpy(rng.standard_normal((new, 2, D)).astype(np.float32)).bfloat16().to(DEV)
+    for bad in (-1, -(1 << 30), -(1 << 31), (1 << 31) - 1, 1 << 30, K.shape[0]):
+        table.fill_(bad)
+        st = F.new_status()
+        out = F.fathom_paged_attn(q, K, V, table, i64([0, new]), i64([64]), new, dev_status=st)
+        assert status(st) == F.FATHOM_DEV_BAD_PAGE and (out == 0).all(), bad
+
+
+@pytest.mark.parametrize("kw", [dict(scale=0.0), dict(scale=0.0, softcap=2.0), dict(softcap=2.0 ** -10), dict(softcap=1024.0),
+                                dict(scale=-0.3, softcap=5.0), dict(scale=0.02, bias=True)])
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_attn_scales_and_caps(kw, dt):
+    attn_case(23, [(300, 1), (200, 70), (64, 6)], 2, 4, 16, dt, **kw)
+
+
 MIXED = [(400, 1), (300, 150), (90, 5), (129, 64), (40, 40), (700, 2)]
 
 
