@@ -391,8 +391,8 @@ typedef struct {
  *   n_now[s]  = n[s], and n_unit[s*H + h] = n_now[s] for the per-unit calls.
  * A request that cannot be served keeps n_now = n_old, takes no page, and its
  * slots are -1: with PAGES_SHORT from the first request on whose pages exceed
- * those left (and all after it that need pages); with BAD_N where its rows end
- * past T.  Lengths outside [0, ld_table*page]: BAD_N, no rows, n_now = n_old, or
+ * those left (and all after it that need pages); with BAD_N where it has rows that
+ * end past T.  Lengths outside [0, ld_table*page]: BAD_N, no rows, n_now = n_old, or
  * 0 where n_old is outside.
  *
  *   n_old, n  [S] int64 (device).      table [S][ld_table] int32 (device, updated).

@@ -30,7 +30,7 @@ def paged_map(n_old, n, page, table, ring, state, T, H):
         need = max(pb - pa, 0)
         taken += need
         returned += [table[s, j] for j in range(pb, pa)]
-        if at > T:
+        if new and at > T:
             bad_n = True
         elif need and taken > count:
             short = True

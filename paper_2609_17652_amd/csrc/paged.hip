@@ -134,7 +134,7 @@ __global__ __launch_bounds__(THREADS) void paged_map_kernel(MapArgs a) {
     const int s = tid * kPer + i;
     const bool ok_old = no[i] >= 0 && no[i] <= cap, ok = ok_old && nn[i] >= 0 && nn[i] <= cap;
     first[i] = at[0];
-    const bool fits = at[0] + add[i][0] <= a.T, pages = add[i][1] == 0 || at[1] + add[i][1] <= count;
+    const bool fits = add[i][0] == 0 || at[0] + add[i][0] <= a.T, pages = add[i][1] == 0 || at[1] + add[i][1] <= count;
     served[i] = ok && fits && pages;
     if (s < S) {
       if (!ok || !fits) flags |= FATHOM_DEV_BAD_N;

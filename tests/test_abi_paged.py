@@ -166,3 +166,12 @@ def test_plain_map_by_hand():
     assert slots.tolist() == [90, 91, 92, 93, 94, 95, 112, 113, -1]
     assert start.tolist() == [0, 8, 8] and now.tolist() == [18, 0] and unit.tolist() == [18, 18, 0, 0]
     assert st.tolist() == [2, 5] and not short and not bad
+
+
+def test_map_ends_requests_behind_rows_that_do_not_fit():
+    """A request without new rows is served wherever it stands: the pages it returns are no longer its own."""
+    table = np.array([[-1, -1], [4, 2], [3, -1]], np.int32)
+    args = [0, 30, 16], [20, 0, 5], 16, table, np.array([0, 1, 5, -1, -1, -1], np.int32), [0, 3], 10
+    _, ring, slots, start, n_now, _, state, short, bad_n = P.paged_map(*args, 1)
+    assert n_now.tolist() == [0, 0, 5] and ring.tolist() == [0, 1, 5, 4, 2, -1] and state.tolist() == [0, 5]
+    assert (slots == -1).all() and start.tolist() == [0, 20, 20, 20] and bad_n and not short

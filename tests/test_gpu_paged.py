@@ -125,6 +125,17 @@ def test_map_bad_lengths_and_empty_calls():
     assert out[2].tolist() == [-1] * 3 and out[3].tolist() == [0] and out[6].tolist() == [7, 9] and out[7] == 0
 
 
+def test_map_ends_requests_behind_rows_that_do_not_fit():
+    """A request without new rows is served wherever it stands: the pages it returns are no longer its own."""
+    table = np.array([[-1, -1], [4, 2], [3, -1]], np.int32)
+    args = [0, 30, 16], [20, 0, 5], 16, table, np.array([0, 1, 5, -1, -1, -1], np.int32), [0, 3], 10
+    out = run_map(*args, 1)
+    for got, want in zip(out[:7], O.paged_map(*args, 1)):
+        assert np.array_equal(got, want)
+    assert out[4].tolist() == [0, 0, 5] and out[1].tolist() == [0, 1, 5, 4, 2, -1] and out[6].tolist() == [0, 5]
+    assert out[7] == F.FATHOM_DEV_BAD_N
+
+
 def test_map_bad_state_and_pages():
     table, ring = np.array([[9, -1], [-5, -1]], np.int32), np.array([1, 2, 3, 99], np.int32)
     for state in ([4, 1], [-1, 1], [0, 5], [0, -1]):  # nothing is taken
