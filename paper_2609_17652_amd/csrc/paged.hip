@@ -14,8 +14,9 @@
 // the caller's are in place and the others still read them, a second launch does.
 //
 // Write.  A copy of rows: 16 lanes take a row's 256 bytes of output, the row's
-// slot gives the page.  Bound by bytes where they are many and by one trip to
-// memory after another (slot, row, store) where they are few.
+// slot gives the page.  Bound by bytes where they are many (139315 tokens of 8 heads, fp32 to
+// bf16, 1.7 GB: 0.33 ms, 5.2 TB/s) and by one trip to memory after another (slot and row, store)
+// where they are few.
 #include "paged.hpp"
 
 namespace fathom {
@@ -240,18 +241,19 @@ fathom_status launch_paged_map(const int64_t* n_old, const int64_t* n, int S, in
   const MapArgs a = {n_old, n,     S, H,     shift, table, ld_table, ring, P,
                      state, slots, T, start, n_now, n_unit, state_out, st};
   const size_t lds = (size_t)5 * S * sizeof(int32_t);
-  // A step that moves few tokens is one launch of one workgroup.  (Pages taken are bounded by
-  // the new tokens; pages that come back are not, but a workgroup moves 1000 in about a
-  // microsecond.)
-  if (T <= 8 * kMapFew && S <= kMapFew) {
+  // A step that moves few tokens is one small workgroup (64 requests' one token 5.4 us, 8.4 in a
+  // large one; 933 tokens 9.4 and 9.3; 1096 11.9 and 11.0); else a slot a thread, over two
+  // workgroups a CU at most, all writing what they find (1811 tokens 9.4 us, 13.6 in one
+  // workgroup).  (Pages taken are bounded by the new tokens; pages that come back are not, but a
+  // workgroup moves 1000 in about a microsecond.)
+  if (T <= 4 * kMapFew && S <= kMapFew) {
     hipLaunchKernelGGL((paged_map_kernel<kMapFew, true, true>), dim3(1), dim3(kMapFew), lds, s, a);
-  } else if (T <= 8 * kMapThreads) {
-    hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, true>), dim3(1), dim3(kMapThreads), lds, s, a);
   } else {
-    // a slot a thread, over two workgroups a CU at most
-    const int64_t wgs = T / kMapThreads + 1;
-    const dim3 grid((unsigned)(wgs < 512 ? wgs : 512));
-    if (n_now != n_old && n_now != n && state_out != state) {
+    const bool apart = n_now != n_old && n_now != n && state_out != state;
+    // in place: one workgroup, or a launch of its own for lengths and state (about 4 us)
+    const int64_t wgs = !apart && T <= 2 * kMapThreads ? 1 : (T + kMapThreads - 1) / kMapThreads;
+    const dim3 grid((unsigned)(wgs < 1 ? 1 : wgs < 512 ? wgs : 512));
+    if (apart || wgs <= 1) {
       hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, true>), grid, dim3(kMapThreads), lds, s, a);
     } else {
       hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, false>), grid, dim3(kMapThreads), lds, s, a);
@@ -290,67 +292,38 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b, bool bf) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// F32: fp32 rows, rounded; otherwise a copy.  ROWS rows (of 16 lanes) per lane group.
-template <bool F32, bool BF, int ROWS>
+// F32: fp32 rows, rounded; otherwise a copy.  A row per 16 lanes (four, their loads in flight at
+// once, are slower at every size: 512 rows 3.6 us against 2.8, 524288 rows 107 against 101).
+template <bool F32, bool BF>
 __global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(WriteArgs a) {
   const int x = threadIdx.x & 15, g = threadIdx.x >> 4;
   const bool v_side = blockIdx.y != 0;
   const void* src = v_side ? a.V : a.K;
   uint16_t* dst = v_side ? a.Vp : a.Kp;
   const int64_t ls_tok = v_side ? a.ldv_tok : a.ldk_tok, ls_head = v_side ? a.ldv_head : a.ldk_head;
-  constexpr int kGroups = kWriteThreads / 16;
-  int64_t slot[ROWS];
-  uint32_t head[ROWS];
-  u32x4 w[ROWS], w2[ROWS];
-  const uint32_t r0 = blockIdx.x * (uint32_t)(kGroups * ROWS) + g;
+  const uint32_t r = blockIdx.x * (uint32_t)(kWriteThreads / 16) + g;
+  if (r >= a.rows) return;
+  const uint32_t t = r / (uint32_t)a.H, h = r - t * (uint32_t)a.H;
+  const int64_t slot = a.slots[t], o = (int64_t)t * ls_tok + (int64_t)h * ls_head + 8 * x;
+  u32x4 v;
+  if constexpr (F32) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(reinterpret_cast<const float*>(src) + o);
+    const u32x4 lo = p[0], hi = p[1];
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const uint32_t r = r0 + i * kGroups;
-    slot[i] = -1;
-    head[i] = 0;
-    if (r < a.rows) {
-      const uint32_t t = r / (uint32_t)a.H, h = r - t * (uint32_t)a.H;
-      slot[i] = a.slots[t];
-      head[i] = h;
-      const int64_t o = (int64_t)t * ls_tok + (int64_t)h * ls_head + 8 * x;
-      if constexpr (F32) {
-        const u32x4* p = reinterpret_cast<const u32x4*>(reinterpret_cast<const float*>(src) + o);
-        w[i] = p[0];
-        w2[i] = p[1];
-      } else {
-        w[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(src) + o);
-      }
+    for (int e = 0; e < 2; ++e) {
+      v[e] = pack_pair(__uint_as_float(lo[2 * e]), __uint_as_float(lo[2 * e + 1]), BF);
+      v[2 + e] = pack_pair(__uint_as_float(hi[2 * e]), __uint_as_float(hi[2 * e + 1]), BF);
     }
+  } else {
+    v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(src) + o);
   }
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    if (slot[i] < 0) continue;
-    if (slot[i] >= a.cap) {
-      if (x == 0) set_status(a.st, FATHOM_DEV_BAD_PAGE);
-      continue;
-    }
-    u32x4 v = w[i];
-    if constexpr (F32) {
-      const u32x4 lo = w[i], hi = w2[i];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        v[e] = pack_pair(__uint_as_float(lo[2 * e]), __uint_as_float(lo[2 * e + 1]), BF);
-        v[2 + e] = pack_pair(__uint_as_float(hi[2 * e]), __uint_as_float(hi[2 * e + 1]), BF);
-      }
-    }
-    const int64_t o = (slot[i] >> a.shift) * a.ld_page + (int64_t)head[i] * a.ld_head +
-                      (slot[i] & ((1 << a.shift) - 1)) * a.ld_tok + 8 * x;
-    *reinterpret_cast<u32x4*>(dst + o) = v;
+  if (slot < 0) return;
+  if (slot >= a.cap) {
+    if (x == 0) set_status(a.st, FATHOM_DEV_BAD_PAGE);
+    return;
   }
-}
-
-template <int ROWS>
-static void launch_write(const WriteArgs& a, bool f32, bool bf, hipStream_t s) {
-  constexpr uint32_t per = kWriteThreads / 16 * ROWS;
-  const dim3 grid((a.rows + per - 1) / per, 2);
-  if (!f32) hipLaunchKernelGGL((paged_write_kernel<false, false, ROWS>), grid, dim3(kWriteThreads), 0, s, a);
-  else if (bf) hipLaunchKernelGGL((paged_write_kernel<true, true, ROWS>), grid, dim3(kWriteThreads), 0, s, a);
-  else hipLaunchKernelGGL((paged_write_kernel<true, false, ROWS>), grid, dim3(kWriteThreads), 0, s, a);
+  *reinterpret_cast<u32x4*>(dst + (slot >> a.shift) * a.ld_page + (int64_t)h * a.ld_head +
+                            (slot & ((1 << a.shift) - 1)) * a.ld_tok + 8 * x) = v;
 }
 
 fathom_status launch_paged_write(const void* K, const void* V, fathom_dtype sdt, int64_t ldk_tok, int64_t ldk_head,
@@ -360,9 +333,10 @@ fathom_status launch_paged_write(const void* K, const void* V, fathom_dtype sdt,
   const WriteArgs a = {K, V, ldk_tok, ldk_head, ldv_tok, ldv_head, slots, (uint32_t)(T * p.H),
                        reinterpret_cast<uint16_t*>(p.K), reinterpret_cast<uint16_t*>(p.V), p.H, shift, p.P << shift,
                        p.ld_page, p.ld_head, p.ld_tok, st};
-  // few rows: one a lane group, so that they reach more CUs; many: four in flight
-  if (a.rows <= 16384) launch_write<1>(a, sdt == FATHOM_F32, p.dt == FATHOM_BF16, s);
-  else launch_write<4>(a, sdt == FATHOM_F32, p.dt == FATHOM_BF16, s);
+  const dim3 grid((a.rows + kWriteThreads / 16 - 1) / (kWriteThreads / 16), 2), threads(kWriteThreads);
+  if (sdt != FATHOM_F32) hipLaunchKernelGGL((paged_write_kernel<false, false>), grid, threads, 0, s, a);
+  else if (p.dt == FATHOM_BF16) hipLaunchKernelGGL((paged_write_kernel<true, true>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((paged_write_kernel<true, false>), grid, threads, 0, s, a);
   FATHOM_LAUNCH_CHECK();
   return FATHOM_OK;
 }
