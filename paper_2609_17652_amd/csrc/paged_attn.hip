@@ -682,13 +682,15 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
   if (flags && lane == 0) set_status(p.st, flags);
 }
 
-// The requests and heads of attn_few_kernel whose blocks went to more than one wave: a
-// workgroup a query row, out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over the row's
-// parts, in a fixed order.  Block counts are recomputed from the lengths.  A trip to memory for
-// the lengths, one for every part's (m, l), a thread a part, and one for eight parts' sums at a
-// time, 32 threads and 4 channels a thread each (one part after another: 14 us for 128
-// parts, where this takes 6).  blockIdx.x is the request and head or, where these are more than
-// the waves' bounds, the bound: the first inside of a request and head joins it.
+// The requests and heads of attn_few_kernel whose blocks went to more than one wave:
+// out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over a row's parts, in a fixed order.
+// Block counts are recomputed from the lengths.  Bound by trips to memory: one for the lengths,
+// one for every part's (m, l), a thread a part, and one for eight parts' sums at a time, 32
+// threads and 4 channels a thread each (one part after another: 14 us for 128 parts, where this
+// takes 6).  Of at most eight parts, eight rows at a time take one trip for all (64 requests of
+// 32 rows 146 us with attention, this way 117).  blockIdx.x is the request and head or, where
+// these are more than the waves' bounds, the bound: the first inside of a request and head joins
+// it (4000 requests 10.3 ms with attention, 0.47).
 constexpr int kJoinGroups = 8, kJoinBatch = 8;
 template <bool BF, bool LOOP>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) {
@@ -713,8 +715,43 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
   const int w0 = worker_of(g0, W), count = worker_of(g0 + nb - 1, W) - w0 + 1;
   if (count == 1 || (bounds && (at == g0 || last > g0))) return;
   const int tid = threadIdx.x, x = tid & 31, g = tid >> 5;
+  auto store = [&](int r, f32x4 o, float l) {  // the 4 channels from 4 x
+    const int tok = r / G;
+    typename Mx<BF>::t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(l == 0.0f ? 0.0f : o[e] / l);
+    *reinterpret_cast<u32x2*>(p.out + ((a + tok) * H * G + h * G + (r - tok * G)) * kD + 4 * x) =
+        *reinterpret_cast<u32x2*>(y);
+  };
   // a part is its wave's first piece, but for a wave that begins in an earlier request or head
   const int64_t step = 2 * R, late = share(w0, W) < g0 ? R : 0;
+  if (count <= kJoinBatch) {
+    for (int r = blockIdx.y * kJoinGroups + g; r < rows; r += gridDim.y * kJoinGroups) {
+      const int64_t row0 = w0 * step + r;
+      float m[kJoinBatch], lp[kJoinBatch], M = -__builtin_huge_valf(), l = 0.0f;
+      f32x4 v[kJoinBatch], o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < kJoinBatch; ++c) {
+        m[c] = -__builtin_huge_valf();
+        if (c >= count || share(w0 + c, W) == share(w0 + c + 1, W)) continue;
+        const int64_t at = row0 + c * step + (c == 0 ? late : 0);
+        m[c] = p.part_ml[2 * at];
+        lp[c] = p.part_ml[2 * at + 1];
+        v[c] = *reinterpret_cast<const f32x4*>(p.part_o + at * kD + 4 * x);
+      }
+#pragma unroll
+      for (int c = 0; c < kJoinBatch; ++c) M = fmaxf(M, m[c]);
+#pragma unroll
+      for (int c = 0; c < kJoinBatch; ++c) {
+        if (m[c] == -__builtin_huge_valf()) continue;
+        const float w = __builtin_amdgcn_exp2f(m[c] - M);
+        l += w * lp[c];
+        o += w * v[c];
+      }
+      store(r, o, l);
+    }
+    return;
+  }
   for (int r = blockIdx.y; r < rows; r += gridDim.y) {
     const int64_t row0 = w0 * step + r;
     float M = -__builtin_huge_valf(), l = 0.0f;
@@ -762,12 +799,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
     f32x4 sum = acc[0][tid];
 #pragma unroll
     for (int i = 1; i < kJoinGroups; ++i) sum += acc[i][tid];
-    const int tok = r / G;
-    typename Mx<BF>::t y[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(den == 0.0f ? 0.0f : sum[e] / den);
-    *reinterpret_cast<u32x2*>(p.out + ((a + tok) * H * G + h * G + (r - tok * G)) * kD + 4 * tid) =
-        *reinterpret_cast<u32x2*>(y);
+    store(r, sum, den);
     if constexpr (!LOOP) return;
   }
 }
@@ -1445,9 +1477,12 @@ static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) 
     const size_t lds = (size_t)kFewWaves * 2 * kFewStage + plan;
     if (a.R == 16) hipLaunchKernelGGL((attn_few_kernel<BF, 1>), grid, threads, lds, s, p);
     else hipLaunchKernelGGL((attn_few_kernel<BF, kFewRows / 16>), grid, threads, lds, s, p);
+    // A request and head of more than eight parts is joined a workgroup a row where these are few,
+    // and where they are many, so that most have few parts, by a few workgroups that go over the rows.
     const int pairs = p.S * p.c.H, units = pairs < kFewWorkers ? pairs : kFewWorkers - 1;
-    if (a.run_many) hipLaunchKernelGGL((attn_join_kernel<BF, true>), dim3(units, p.G), dim3(256), plan, s, p, a.R);
-    else hipLaunchKernelGGL((attn_join_kernel<BF, false>), dim3(units, a.rows), dim3(256), plan, s, p, a.R);
+    const int y = a.run_many || pairs >= 128 ? (a.rows < 4 ? a.rows : 4) : a.rows;
+    if (y < a.rows) hipLaunchKernelGGL((attn_join_kernel<BF, true>), dim3(units, y), dim3(256), plan, s, p, a.R);
+    else hipLaunchKernelGGL((attn_join_kernel<BF, false>), dim3(units, y), dim3(256), plan, s, p, a.R);
   }
 }
 
