@@ -73,7 +73,8 @@ struct PagedAttnArgs {
   const int64_t *prefix, *first;
   uint16_t* out;
   float *part_o, *part_ml;  // partial results: rows of kD sums, and (maximum, sum) of each
-  int nsplit;               // attn_many_kernel: parts of a tile's keys at most
+  int nsplit, part_units;   // attn_many_kernel: parts of a tile's keys at most, units of 64 keys of a part at least
+  bool all_parts;           // as many as there may be, or one
   TileRecord* tiles;        // its tiles, of more than 64 requests
   int64_t ntiles;
   uint32_t* st;
@@ -731,16 +732,17 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
       float m[kJoinBatch], lp[kJoinBatch], M = -__builtin_huge_valf(), l = 0.0f;
       f32x4 v[kJoinBatch], o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int c = 0; c < kJoinBatch; ++c) {
-        m[c] = -__builtin_huge_valf();
-        if (c >= count || share(w0 + c, W) == share(w0 + c + 1, W)) continue;
-        const int64_t at = row0 + c * step + (c == 0 ? late : 0);
+      for (int c = 0; c < kJoinBatch; ++c) {  // (behind the last part: that one again, unused)
+        const int64_t at = row0 + min(c, count - 1) * step + (c == 0 ? late : 0);
         m[c] = p.part_ml[2 * at];
         lp[c] = p.part_ml[2 * at + 1];
         v[c] = *reinterpret_cast<const f32x4*>(p.part_o + at * kD + 4 * x);
       }
 #pragma unroll
-      for (int c = 0; c < kJoinBatch; ++c) M = fmaxf(M, m[c]);
+      for (int c = 0; c < kJoinBatch; ++c) {
+        if (c >= count || share(w0 + c, W) == share(w0 + c + 1, W)) m[c] = -__builtin_huge_valf();
+        M = fmaxf(M, m[c]);
+      }
 #pragma unroll
       for (int c = 0; c < kJoinBatch; ++c) {
         if (m[c] == -__builtin_huge_valf()) continue;
@@ -920,11 +922,12 @@ __device__ __forceinline__ bool many_tile(const PagedAttnArgs& p, int tm, int ti
 }
 
 // The keys of a tile in units of 64 (one where no query sees any: a loop that may not run costs
-// the kernel spilled registers), and the parts that they are cut into, of at least 4 each (8, 16
-// and 32 are slower).
-constexpr int kUnits = 4;
+// the kernel spilled registers), and the parts that they are cut into.
 __device__ __forceinline__ int units_of(const ManyTile& t) { return max((t.hi - t.lo + kManyKeys - 1) / kManyKeys, 1); }
-__device__ __forceinline__ int parts_of(int units, int nsplit) { return max(min(nsplit, units / kUnits), 1); }
+__device__ __forceinline__ int parts_of(const PagedAttnArgs& p, int units) {
+  const int most = units / p.part_units;
+  return most >= p.nsplit ? p.nsplit : p.all_parts ? 1 : max(most, 1);
+}
 
 // Keys go by in blocks of 32.  While the matrix cores form the scores of the next block and
 // add the last block's product with V, the vector unit takes the exponentials of this one:
@@ -969,7 +972,7 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
     if (flags && blockIdx.x == 0) set_status(p.st, flags);
     if (!some) return;
   }
-  const int units = units_of(t), parts = parts_of(units, p.nsplit);
+  const int units = units_of(t), parts = parts_of(p, units);
   if (part >= parts) return;
   const int unit0 = (int)((int64_t)units * part / parts), unit1 = (int)((int64_t)units * (part + 1) / parts);
   // blocks, an even number
@@ -1361,8 +1364,10 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
 }
 
 // The tiles whose keys were split, a workgroup 16 query rows, 8 at a time, 32 threads and 4
-// channels a thread each; every part's sums are on their way before the first is used.
-constexpr int kManyJoin = 16, kMaxSplit = 8;
+// channels a thread each.  Bound by reading the parts: four parts' loads are on their way at
+// once, whatever the number is (behind the last: that one again, unused; loads that depend on it
+// came one after another).
+constexpr int kManyJoin = 16, kMaxSplit = 8, kManyBatch = 4;
 template <bool BF>
 __global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
   __shared__ int red[12];
@@ -1370,7 +1375,7 @@ __global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
   const int H = p.c.H, G = p.G, tile = blockIdx.x / H, h = blockIdx.x % H;
   ManyTile t;
   if (!many_tile(p, kManyRows / G, tile, h, red, &t, flags)) return;
-  const int parts = parts_of(units_of(t), p.nsplit), rows = t.toks * G;
+  const int parts = parts_of(p, units_of(t)), rows = t.toks * G;
   if (parts == 1) return;
   const int64_t base = ((int64_t)tile * H + h) * p.nsplit * kManyRows;
   const int x = threadIdx.x & 31;
@@ -1378,33 +1383,37 @@ __global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
   for (int i = 0; i < kManyJoin; i += 8) {
     const int r = blockIdx.y * kManyJoin + i + (threadIdx.x >> 5);
     if (r >= rows) return;
-    float m[kMaxSplit], lp[kMaxSplit], M = -__builtin_huge_valf();
-    f32x4 v[kMaxSplit];
-#pragma unroll
-    for (int c = 0; c < kMaxSplit; ++c) {
-      m[c] = -__builtin_huge_valf();
-      if (c >= parts) continue;
-      const int64_t pr = base + (int64_t)c * kManyRows + r;
-      m[c] = p.part_ml[2 * pr];
-      lp[c] = p.part_ml[2 * pr + 1];
-      v[c] = *reinterpret_cast<const f32x4*>(p.part_o + pr * kD + 4 * x);
-    }
-#pragma unroll
-    for (int c = 0; c < kMaxSplit; ++c) M = fmaxf(M, m[c]);
+    float M = -__builtin_huge_valf(), l = 0.0f;  // (a part's maximum is a number: the reference it was taken against)
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    float l = 0.0f;
+    for (int c0 = 0; c0 < parts; c0 += kManyBatch) {
+      float m[kManyBatch], lp[kManyBatch], top = M;
+      f32x4 v[kManyBatch];
 #pragma unroll
-    for (int c = 0; c < kMaxSplit; ++c) {
-      if (c >= parts) continue;
-      const float w = __builtin_amdgcn_exp2f(m[c] - M);
-      l += w * lp[c];
-      o += w * v[c];
+      for (int c = 0; c < kManyBatch; ++c) {
+        const int64_t pr = base + (int64_t)min(c0 + c, parts - 1) * kManyRows + r;
+        m[c] = p.part_ml[2 * pr];
+        lp[c] = p.part_ml[2 * pr + 1];
+        v[c] = *reinterpret_cast<const f32x4*>(p.part_o + pr * kD + 4 * x);
+      }
+#pragma unroll
+      for (int c = 0; c < kManyBatch; ++c) top = fmaxf(top, m[c]);
+      const float f = c0 == 0 ? 1.0f : __builtin_amdgcn_exp2f(M - top);
+      M = top;
+      l *= f;
+      o *= f;
+#pragma unroll
+      for (int c = 0; c < kManyBatch; ++c) {
+        if (c0 + c >= parts) continue;
+        const float w = __builtin_amdgcn_exp2f(m[c] - M);
+        l += w * lp[c];
+        o += w * v[c];
+      }
     }
-    const int tok = r / G, g = r - tok * G;
+    const int tok = r / G;
     typename Mx<BF>::t y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = (typename Mx<BF>::t)(l == 0.0f ? 0.0f : o[e] / l);
-    *reinterpret_cast<u32x2*>(p.out + ((t.a + t.tok0 + tok) * H * G + h * G + g) * kD + 4 * x) =
+    *reinterpret_cast<u32x2*>(p.out + ((t.a + t.tok0 + tok) * H * G + h * G + (r - tok * G)) * kD + 4 * x) =
         *reinterpret_cast<u32x2*>(y);
   }
 }
@@ -1414,7 +1423,8 @@ struct PagedAttnPlan {
   int few, R, rows;   // rows up to which a request goes to attn_few_kernel, that it is built for, that there can be
   bool run_few, run_many;
   int64_t tiles;      // bound on attn_many_kernel's row tiles
-  int nsplit;         // parts of a tile's keys at most
+  int nsplit, part_units;  // parts of a tile's keys at most, units of 64 keys of a part at least
+  bool all_parts;          // that many or one
   int64_t part_rows;  // rows of partial results
   int64_t records;    // tiles that attn_tiles_kernel writes
 };
@@ -1429,17 +1439,26 @@ static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) 
   // one request whose rows are all there are is known to be large; more may be of either kind
   a.run_few = !a.run_many || S > 1 || T <= kFewRows / G;
   const int tm = kManyRows / G;
-  a.nsplit = 1;
+  a.nsplit = a.part_units = 1;
   if (a.run_many) {
     const int64_t large = T / (kFewRows / G + 1) < S ? T / (kFewRows / G + 1) : S;  // requests that can be large
     a.tiles = T / tm + large;
-    // two workgroups on each of 256 CUs: the fewest parts that leave at most a tenth of the
-    // places idle in the last round
-    const int64_t wgs = (T + tm - 1) / tm * H;
-    for (int ns = 1; ns <= kMaxSplit; ++ns) {
+    // two workgroups on each of 256 CUs: the parts that leave the fewest places idle in the last
+    // round, the first that leave at most a tenth.  A part costs its sums' way to memory and back,
+    // so it has some keys at least: where the tiles alone fill few of the CUs 4 units (64 tokens
+    // over 4000 24 us, 39 with 16), then 8 and 16 (1024 over none 35 and 30, over 1000 49 and 60;
+    // 1500 over none 47 and 42), and where they fill all, 32 in each of the parts or none are made
+    // (2336 over none to 2000 177 us, 224 in one or two parts; over 8000 407, 482 in one).
+    const int64_t wgs = ((T + tm - 1) / tm + large / 2) * H;
+    a.all_parts = wgs >= 512;
+    a.part_units = wgs >= 512 ? 32 : wgs > 256 ? 16 : wgs >= 64 ? 8 : 4;
+    double best = 0.0;
+    for (int ns = 1; ns <= kMaxSplit && best < 0.9; ++ns) {
       const int64_t rounds = (wgs * ns + 511) / 512;
+      const double used = (double)(wgs * ns) / (double)(rounds * 512);
+      if (used <= best || (ns > 1 && wgs * ns > 2048)) continue;
+      best = used;
       a.nsplit = ns;
-      if (wgs * ns * 10 >= rounds * 512 * 9 || wgs * ns > 4096) break;
     }
   }
   const int64_t few_rows = a.run_few ? (int64_t)kFewWorkers * 2 * a.R : 0;
@@ -1457,8 +1476,10 @@ size_t paged_attn_ws_bytes(int64_t T, int S, int H, int G, int64_t max_new) {
 template <bool BF>
 static void launch_attn(PagedAttnArgs p, const PagedAttnPlan& a, hipStream_t s) {
   const size_t plan = (size_t)(p.S + 1 + 4) * sizeof(int);
-  const int64_t most = (p.c.ld_table << p.c.shift) / kManyKeys / kUnits;  // parts of the longest request
-  p.nsplit = (int)(most < a.nsplit ? (most > 1 ? most : 1) : a.nsplit);
+  const int64_t most = (p.c.ld_table << p.c.shift) / kManyKeys / a.part_units;  // parts of the longest request
+  p.nsplit = (int)(most >= a.nsplit ? a.nsplit : a.all_parts || most < 1 ? 1 : most);
+  p.part_units = a.part_units;
+  p.all_parts = a.all_parts;
   p.few = a.few;
   if (a.run_many) {
     const dim3 grid((unsigned)(a.tiles * p.nsplit * p.c.H)), threads(256);

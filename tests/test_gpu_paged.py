@@ -572,6 +572,24 @@ def test_attn_repeats_bit_for_bit_and_long_split():
         assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("H,G,new,n", [(64, 8, 130, 6300), (64, 8, 130, 700), (24, 8, 100, 1200), (1, 8, 60, 5000)])
+def test_attn_splits_of_many_rows(H, G, new, n):
+    """Tiles that fill the card, half of it or little, keys cut into parts or not: heads at both ends against 64 bits."""
+    gen = torch.Generator(device=DEV).manual_seed(24)
+    page = 64
+    P = O.pages_of(n, page)
+    K, V = (torch.randn((P, H, page, D), generator=gen, device=DEV).half() for _ in range(2))
+    table = torch.randperm(P, generator=gen, device=DEV).to(torch.int32)[None]
+    q = torch.randn((new, H * G, D), generator=gen, device=DEV).half()
+    out = F.fathom_paged_attn(q, K, V, table, i64([0, new]), i64([n]), new).double().cpu().numpy()
+    for h in {0, H - 1}:
+        rows = [x[table[0].long(), h].reshape(-1, D)[:n].double().cpu().numpy() for x in (K, V)]
+        mine = slice(h * G, (h + 1) * G)
+        ref, mag, top = O.paged_attn(q[:, mine].double().cpu().numpy(), *rows, n, G, 1 / np.sqrt(D))
+        tol = 2.0 ** -11 * np.abs(ref) + mag * (2.0 ** -11 + 2 * (D + 8) * 2.0 ** -24 * top[..., None] + 64 * 2.0 ** -24) * 1.001
+        assert (np.abs(out[:, mine] - ref) <= tol).all(), h
+
+
 # ---------------------------------------------------------------- together
 class Serving:
     """A serving loop over the paged calls: map, write, attention over all rows; the bit-plane store alongside and
