@@ -783,13 +783,15 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
 #pragma unroll
       for (int i = 0; i < kJoinBatch; ++i) {
         const int c = c0 + i * kJoinGroups;
-        w[i] = c < count ? weight[c] : 0.0f;
-        v[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-        if (w[i] != 0.0f)  // a part without weight may not be there
-          v[i] = *reinterpret_cast<const f32x4*>(p.part_o + (row0 + c * step + (c == 0 ? late : 0)) * kD + 4 * x);
+        const int cc = min(c, count - 1);  // (behind the last: that one again, unused)
+        w[i] = c < count ? weight[cc] : 0.0f;
+        v[i] = *reinterpret_cast<const f32x4*>(p.part_o + (row0 + cc * step + (cc == 0 ? late : 0)) * kD + 4 * x);
       }
 #pragma unroll
-      for (int i = 0; i < kJoinBatch; ++i) o += w[i] * v[i];
+      for (int i = 0; i < kJoinBatch; ++i) {
+        const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+        o += w[i] != 0.0f ? w[i] * v[i] : z;  // a part without weight may not be there
+      }
     }
     acc[g][x] = o;
     __syncthreads();
