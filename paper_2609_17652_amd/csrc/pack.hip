@@ -31,7 +31,9 @@
 //
 // The keys are a unit's rows one after another, or rows in pages (PagedKeys): 16
 // tokens from a multiple of 16 lie in one page, so a lane of an item looks up one
-// page number; an append's lane its own.
+// page number; an append's lane its own.  That look-up costs 2 to 5 %: 275080 tokens of
+// 8 heads in pages of 128 229 us (of 16: 235), one after another 224; one token more of
+// 256 units 9.5 and 9.0.
 //
 // Append (n_old given): a block's fp16 scale depends on every token in it, so
 // a unit growing from n_old to n tokens re-packs blocks floor(n_old/64) ..

@@ -940,11 +940,11 @@ __device__ __forceinline__ int parts_of(const PagedAttnArgs& p, int units) {
 // sums, and Mx::kShift leaves room for it in the probabilities), so the sums are rarely
 // rescaled.
 //
-// Bound by the matrix cores' power: 2048 tokens over 65536 take 2.1 ms, 1.05 PFLOP/s, where
-// a large matrix product of this type reaches 1.2; with neither exponentials nor LDS reads
-// the same instructions take 1.75 ms.  64 rows a wave and one workgroup a CU need half of
-// the LDS reads and are as fast there, and slower where tiles are short (28 prompts of 700
-// tokens 154 us against 137; 6 requests of documents 307 against 235).
+// Bound by the matrix cores' power: 2048 tokens over 65536 take 2.0 to 2.3 ms (as cards
+// differ), 1.0 to 1.1 PFLOP/s, where a large matrix product of this type reaches 1.2; with
+// neither exponentials nor LDS reads the same instructions take 1.75 ms.  64 rows a wave and
+// one workgroup a CU need half of the LDS reads and are up to 5 % faster there, and slower where
+// tiles are short (6 requests of documents 303 us against 188).
 constexpr float kSlack = 6.0f;
 
 // A block's scores between two steps: as the matrix instructions leave them, or, mapped, as
