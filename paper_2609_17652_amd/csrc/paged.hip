@@ -13,8 +13,8 @@
 // sums (16 bytes a request from L2); the first of them writes lengths and state, or, where
 // the caller's are in place and the others still read them, a second launch does.  Bound by
 // latency: launch, lengths, sums, then a search and two trips to memory a slot; 64 requests' one
-// token 5 us, 420000 slots of 512 requests 18 (two launches and slots one request after
-// another: 13 and 23).
+// token 4.8 us, 450000 slots of 512 requests 15.6 (two launches and slots one request after
+// another: 13 and 23; pages moved by the threads that have slots: 18).
 //
 // Write.  A copy of rows: 16 lanes take a row's 256 bytes of output, the row's
 // slot gives the page.  Bound by bytes where they are many (139315 tokens of 8 heads, fp32 to
@@ -24,8 +24,8 @@
 
 namespace fathom {
 
-// Threads of a workgroup and requests of a thread: up to 256 requests of a call 256 and 1
-// (its 4 waves meet sooner), up to the limit 1024 and 4.
+// Threads of a workgroup and requests of a thread: up to 256 requests of a small call 256 and 1
+// (its 4 waves meet sooner), up to 1024 requests 1024 and 1, up to the limit 1024 and 4.
 constexpr int kMapThreads = 1024;
 constexpr int kMapFew = 256;
 static_assert(kMaxSeqs % kMapThreads == 0, "requests divide over the threads");
@@ -85,10 +85,9 @@ __device__ __forceinline__ int last_at_most(const int32_t* a, int count, int32_t
 __device__ __forceinline__ int32_t clip31(int64_t x) { return (int32_t)(x < 0x7fffffff ? x : 0x7fffffff); }
 
 // FILL: slots, table and ring.  FINISH: start, lengths and state, after every read.
-template <int THREADS, bool FILL, bool FINISH>
+template <int THREADS, int kPer, bool FILL, bool FINISH>
 __global__ __launch_bounds__(THREADS) void paged_map_kernel(MapArgs a) {
   extern __shared__ int32_t sm[];
-  constexpr int kPer = THREADS == kMapFew ? kMapFew / THREADS : kMaxSeqs / THREADS;
   __shared__ int64_t part[3][THREADS / kWave];
   __shared__ int64_t tot[4];  // rows, pages returned; pages taken by those served
   const int S = a.S, tid = threadIdx.x;
@@ -189,24 +188,20 @@ __global__ __launch_bounds__(THREADS) void paged_map_kernel(MapArgs a) {
       }
       a.slots[t] = slot;
     }
+    // pages that move, from the other end: the last threads have no slot
 #pragma unroll 2
-    for (int64_t j = gt; j < taken; j += step) {
-      const int s = last_at_most(s_taken, S, (int32_t)j);
-      int64_t r = head + j;
-      if (r >= a.P) r -= a.P;
-      const int32_t id = a.ring[r];
-      if (id < 0 || id >= a.P) flags |= FATHOM_DEV_BAD_PAGE;
-      const int64_t before = ((int64_t)s_old[s] + rnd) >> a.shift;
-      a.table[(int64_t)s * a.ld_table + before + (j - s_taken[s])] = id;
-    }
-#pragma unroll 4
-    for (int64_t j = gt; j < back; j += step) {
-      const int s = last_at_most(s_back, S, (int32_t)j);
-      int64_t r = head + count + j;
+    for (int64_t m = step - 1 - gt; m < taken + back; m += step) {
+      const bool take = m < taken;
+      const int64_t j = take ? m : m - taken;
+      const int s = last_at_most(take ? s_taken : s_back, S, (int32_t)j);
+      int64_t r = head + (take ? j : count + j);
       while (r >= a.P) r -= a.P;
-      const int32_t id = a.table[(int64_t)s * a.ld_table + s_after[s] + (j - s_back[s])];
+      int32_t *ring = a.ring + r, *entry = a.table + (int64_t)s * a.ld_table;
+      if (take) entry += (((int64_t)s_old[s] + rnd) >> a.shift) + (j - s_taken[s]);
+      else entry += s_after[s] + (j - s_back[s]);
+      const int32_t id = *(take ? ring : entry);
       if (id < 0 || id >= a.P) flags |= FATHOM_DEV_BAD_PAGE;
-      a.ring[r] = id;
+      *(take ? entry : ring) = id;
     }
   }
   if constexpr (FINISH) {
@@ -237,32 +232,37 @@ __global__ __launch_bounds__(THREADS) void paged_map_kernel(MapArgs a) {
   if (flags) set_status(a.st, flags);
 }
 
+// Lengths and state with the slots, or (in place, several workgroups) in a launch of their own.
+template <int THREADS, int PER>
+static void launch_map(const MapArgs& a, int64_t wgs, bool apart, hipStream_t s) {
+  const size_t lds = (size_t)5 * a.S * sizeof(int32_t);
+  const dim3 grid((unsigned)(wgs < 1 ? 1 : wgs < 512 ? wgs : 512)), threads(THREADS);
+  if (apart || wgs <= 1) {
+    hipLaunchKernelGGL((paged_map_kernel<THREADS, PER, true, true>), grid, threads, lds, s, a);
+  } else {
+    hipLaunchKernelGGL((paged_map_kernel<THREADS, PER, true, false>), grid, threads, lds, s, a);
+    hipLaunchKernelGGL((paged_map_kernel<THREADS, PER, false, true>), dim3(1), threads, lds, s, a);
+  }
+}
+
 fathom_status launch_paged_map(const int64_t* n_old, const int64_t* n, int S, int H, int shift, int32_t* table,
                                int64_t ld_table, int32_t* ring, int64_t P, const int64_t* state, int64_t* slots,
                                int64_t T, int64_t* start, int64_t* n_now, int64_t* n_unit, int64_t* state_out,
                                uint32_t* st, hipStream_t s) {
   const MapArgs a = {n_old, n,     S, H,     shift, table, ld_table, ring, P,
                      state, slots, T, start, n_now, n_unit, state_out, st};
-  const size_t lds = (size_t)5 * S * sizeof(int32_t);
-  // A step that moves few tokens is one small workgroup (64 requests' one token 5.4 us, 8.4 in a
-  // large one; 933 tokens 9.4 and 9.3; 1096 11.9 and 11.0); else a slot a thread, over two
-  // workgroups a CU at most, all writing what they find (1811 tokens 9.4 us, 13.6 in one
+  // A step that moves few tokens is one small workgroup (64 requests' one token 4.8 us, 6.7 in a
+  // large one; 462 tokens 6.7 and 7.2; 538 8.7 and 7.9); else a slot a thread, over two
+  // workgroups a CU at most, all writing what they find (1811 tokens 7.5 us, 13.6 in one
   // workgroup).  (Pages taken are bounded by the new tokens; pages that come back are not, but a
   // workgroup moves 1000 in about a microsecond.)
-  if (T <= 4 * kMapFew && S <= kMapFew) {
-    hipLaunchKernelGGL((paged_map_kernel<kMapFew, true, true>), dim3(1), dim3(kMapFew), lds, s, a);
-  } else {
-    const bool apart = n_now != n_old && n_now != n && state_out != state;
-    // in place: one workgroup, or a launch of its own for lengths and state (about 4 us)
-    const int64_t wgs = !apart && T <= 2 * kMapThreads ? 1 : (T + kMapThreads - 1) / kMapThreads;
-    const dim3 grid((unsigned)(wgs < 1 ? 1 : wgs < 512 ? wgs : 512));
-    if (apart || wgs <= 1) {
-      hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, true>), grid, dim3(kMapThreads), lds, s, a);
-    } else {
-      hipLaunchKernelGGL((paged_map_kernel<kMapThreads, true, false>), grid, dim3(kMapThreads), lds, s, a);
-      hipLaunchKernelGGL((paged_map_kernel<kMapThreads, false, true>), dim3(1), dim3(kMapThreads), lds, s, a);
-    }
-  }
+  const bool apart = n_now != n_old && n_now != n && state_out != state;
+  // in place: one workgroup, or a launch of its own for lengths and state (about 4 us); else a
+  // quarter more than the slots need, which has the pages that move
+  const int64_t wgs = !apart && T <= 2 * kMapThreads ? 1 : (T + T / 4 + kMapThreads - 1) / kMapThreads;
+  if (T <= 2 * kMapFew && S <= kMapFew) launch_map<kMapFew, 1>(a, 1, apart, s);
+  else if (S <= kMapThreads) launch_map<kMapThreads, 1>(a, wgs, apart, s);
+  else launch_map<kMapThreads, kMaxSeqs / kMapThreads>(a, wgs, apart, s);
   FATHOM_LAUNCH_CHECK();
   return FATHOM_OK;
 }
