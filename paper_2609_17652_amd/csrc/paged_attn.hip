@@ -136,7 +136,7 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, const void* from, cons
         "global_load_lds_dwordx4 %1, %5\n\t"
         "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
         "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds),
+        "global_load_lds_dwordx4 %4, %5 offset:3*1024" ::"s"(lds),
         "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base)
         : "memory");
   } else {
