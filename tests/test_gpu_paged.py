@@ -734,3 +734,104 @@ def test_two_graphs_and_two_streams():
     torch.cuda.synchronize()
     for s, w in zip(sets, want):
         assert torch.equal(s["out"], w)
+
+
+def test_a_step_of_all_calls_in_a_graph():
+    """Map, write, attention, pack and sparse attention captured together; lengths and rows change between replays, a
+    request ends and begins again.  Every replay gives what the same calls give eagerly on a state of their own."""
+    rng = np.random.default_rng(25)
+    S, H, G, page, L, P, k = 3, 2, 4, 16, 20, 60, 30
+    i32 = dict(dtype=torch.int32, device=DEV)
+    half = dict(dtype=torch.float16, device=DEV)
+    idx = torch.from_numpy(rng.integers(0, 200, (S * H, G, k)).astype(np.int32)).to(DEV)
+
+    def state():
+        nb = (L * page + 63) // 64
+        return dict(table=torch.full((S, L), -1, **i32), ring=torch.arange(P, **i32), head=i64([0, P]), n=i64([0] * S),
+                    to=i64([0] * S), K=torch.zeros((P, H, page, D), **half), V=torch.zeros((P, H, page, D), **half),
+                    planes=torch.zeros((S * H, D, 4, nb), dtype=torch.int64, device=DEV),
+                    scales=torch.zeros((S * H, D, nb), dtype=torch.int16, device=DEV), st=F.new_status())
+
+    def step(x, rows, max_new):
+        slots, start, now, unit, _ = F.fathom_paged_map(x["n"], x["to"], page, x["table"], x["ring"], x["head"],
+                                                        rows["q"].shape[0], H, state_out=x["head"], dev_status=x["st"])
+        F.fathom_paged_write(rows["K"], rows["V"], slots, x["K"], x["V"], dev_status=x["st"])
+        out = torch.zeros_like(rows["q"])
+        F.fathom_paged_attn(rows["q"], x["K"], x["V"], x["table"], start, now, max_new, out=out, dev_status=x["st"])
+        F.fathom_paged_pack(x["K"], x["table"], now, x["planes"], x["scales"], torch.minimum(x["n"], now), max_new,
+                            dev_status=x["st"])
+        sparse = F.fathom_paged_sparse_attn(rows["qs"], x["K"], x["V"], x["table"], now, idx, 2, 5, dev_status=x["st"])
+        torch.add(now, 0, out=x["n"])
+        return out, sparse, unit
+
+    def new_rows(T):
+        r = {m: torch.from_numpy(rng.standard_normal((T, c, D)).astype(np.float32)).half().to(DEV)
+             for m, c in (("q", H * G), ("K", H), ("V", H))}
+        r["qs"] = torch.from_numpy(rng.standard_normal((S * H, G, D)).astype(np.float32)).to(DEV)
+        return r
+
+    a, b = state(), state()
+    prompts = new_rows(130 + 63 + 64)
+    for x in (a, b):
+        x["to"].copy_(i64([130, 63, 64]))
+        step(x, prompts, 130)
+    rows = new_rows(S)
+    torch.cuda.synchronize()
+    kept = {m: x.clone() for m, x in b.items()}  # the capture's warm-up below moves it
+    b["to"].copy_(b["n"] + 1)
+    step(b, rows, 1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(b, rows, 1)
+    for m, x in kept.items():
+        b[m].copy_(x)
+    n = [130, 63, 64]
+    for i in range(6):
+        n = [n[0] + 1, 0 if i == 2 else n[1] + 1, n[2] + (i != 4)]
+        fresh = new_rows(S)
+        for m in rows:
+            rows[m].copy_(fresh[m])
+        for x in (a, b):
+            x["to"].copy_(i64(n))
+        want = step(a, rows, 1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert b["n"].tolist() == n and status(a["st"]) == status(b["st"]) == 0, i
+        for w, g in zip(want, got):
+            assert torch.equal(w, g), i
+        for m in ("table", "ring", "head", "K", "V", "planes", "scales"):
+            assert torch.equal(a[m], b[m]), (i, m)
+
+
+@pytest.mark.parametrize("new", [1, 30])
+def test_interleaved_pools_and_shared_pages(new):
+    """K and V in one buffer (strides of their own), and two requests that begin with the same pages."""
+    rng = np.random.default_rng(26)
+    H, G, page, n = 2, 3, 16, 90
+    buf = torch.full((20, 2, H, page, D), float("nan"), dtype=torch.bfloat16, device=DEV)
+    K, V = buf[:, 0], buf[:, 1]
+    table = torch.tensor([[3, 9, 1, 4, 12, 7], [3, 9, 1, 15, 2, 6]], dtype=torch.int32, device=DEV)
+    slots = lambda s, lo, hi: i64([int(table[s, p // page]) * page + p % page for p in range(lo, hi)])  # noqa: E731
+    kv = [torch.from_numpy(rng.standard_normal((n, H, D)).astype(np.float32)).bfloat16() for _ in range(4)]
+    for s in range(2):  # the first 48 rows are request 0's for both
+        lo = 0 if s == 0 else 48
+        F.fathom_paged_write(kv[2 * s][lo:].to(DEV), kv[2 * s + 1][lo:].to(DEV), slots(s, lo, n), K, V)
+    for i in (2, 3):
+        kv[i][:48] = kv[i - 2][:48]
+    q = torch.from_numpy(rng.standard_normal((2 * new, H * G, D)).astype(np.float32)).bfloat16()
+    out = F.fathom_paged_attn(q.to(DEV), K, V, table, i64([0, new, 2 * new]), i64([n, n]), new).double().cpu().numpy()
+    eps = 2.0 ** -8
+    for s in range(2):
+        for h in range(H):
+            mine = slice(s * new, (s + 1) * new), slice(h * G, (h + 1) * G)
+            ref, mag, _ = O.paged_attn(q[mine].double().numpy(), kv[2 * s][:, h].double().numpy(),
+                                       kv[2 * s + 1][:, h].double().numpy(), n, G, 1 / np.sqrt(D))
+            assert (np.abs(out[mine] - ref) <= eps * np.abs(ref) + mag * (eps + 1e-4)).all()
+    nn = i64([n, n])
+    planes = torch.empty((2 * H, D, 4, 2), dtype=torch.int64, device=DEV)
+    scales = torch.empty((2 * H, D, 2), dtype=torch.int16, device=DEV)
+    F.fathom_paged_pack(K, table, nn, planes, scales)
+    flat = [torch.stack([kv[2 * s + i][:, h] for s in range(2) for h in range(H)]).to(DEV) for i in range(2)]
+    want = F.fathom_pack(flat[0].float(), nn.repeat_interleave(H), 2)
+    assert torch.equal(planes, want[0]) and torch.equal(scales, want[1])
