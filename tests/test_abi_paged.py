@@ -175,3 +175,13 @@ def test_map_ends_requests_behind_rows_that_do_not_fit():
     _, ring, slots, start, n_now, _, state, short, bad_n = P.paged_map(*args, 1)
     assert n_now.tolist() == [0, 0, 5] and ring.tolist() == [0, 1, 5, 4, 2, -1] and state.tolist() == [0, 5]
     assert (slots == -1).all() and start.tolist() == [0, 20, 20, 20] and bad_n and not short
+
+
+def test_packed_pages_are_the_structure(fl):
+    """The binding's bytes are fathom_pages as ctypes lays it out."""
+    args = 0x1000, 0x2000, fl.FATHOM_BF16, 8, 64, 12345, 1 << 40, 1 << 20, 1 << 7
+    assert fl._pack_pages(*args) == bytes(fl._Pages(*args))
+    K = torch.zeros((3, 2, 16, 128), dtype=torch.float16)
+    pg, H, D = fl._pages(K, None)
+    want = fl._Pages(K.data_ptr(), None, fl.FATHOM_F16, 2, 16, 3, 4096, 2048, 128)
+    assert pg == bytes(want) and (H, D) == (2, 128)
