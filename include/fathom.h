@@ -475,7 +475,9 @@ fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fa
  *   start    [S + 1] int64 (device), non-decreasing, 0 <= start[0], start[S] <= T:
  *            rows of T outside every request are left as they were in out.
  *   n        [S] int64 (device): tokens of each request, the new ones among them.
- *   max_new  host bound on start[s + 1] - start[s]; selects work and sizes the launch.
+ *   max_new  host bound on start[s + 1] - start[s]; selects work and sizes the launch.  It and T
+ *            may be above what the requests have (a padded batch, a captured call), at the
+ *            cost of a call that has as much.
  *   sm_scale finite.   softcap 0 (none) or in [2^-10, 2^10]; its tanh is good to 2^-21 of
  *            softcap, which is why larger ones are not served.
  *   slopes   [H*G] fp32 or NULL.
@@ -487,8 +489,9 @@ fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fa
  *   ws       device workspace of at least fathom_paged_attn_workspace_size(T, S,
  *            H, G, max_new) bytes, 256-byte aligned (any contents).
  * Scores, softmax statistics and sums are fp32; the probabilities of chunks (more
- * than 32 query rows, new*G, of a request) are rounded to the pages' type once, those of
- * fewer rows enter as a sum of two such values.  Sums are in an order that
+ * than 32 query rows, new*G, of a request, or of a call's only request, more than 32 that
+ * T and max_new allow) are rounded to the pages' type once, those of fewer rows enter as a
+ * sum of two such values.  Sums are in an order that
  * depends on the lengths and sizes only.  1 <= G <= 8; T*H*G <= 2^30;
  * S*ld_table*page <= 2^35.
  * Device status: BAD_N (n outside [0, ld_table*page], more new tokens than n or than

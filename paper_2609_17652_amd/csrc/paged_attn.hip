@@ -21,8 +21,9 @@
 // requests and heads are cut into equal shares, one per wave, whatever the
 // lengths are; each wave runs its share through two private LDS stages without
 // meeting the others, and pieces of a request join in attn_join_kernel.
-// attn_many_kernel takes the others, 128 query rows a workgroup, bound by the
-// matrix cores; keys are split over workgroups where the tiles are few.
+// attn_many_kernel takes the others, and a request that is the only one of a call whose bounds
+// allow more rows, 128 query rows a workgroup, bound by the matrix cores; keys are
+// split over workgroups where the tiles are few.
 //
 // Rows that a query must not see get a probability of 0, but 0 * Inf is not 0:
 // V rows behind the end are cleared in LDS, and in steps with masked places
@@ -1461,16 +1462,20 @@ struct PagedAttnPlan {
 static PagedAttnPlan attn_plan(int64_t T, int S, int H, int G, int64_t max_new) {
   PagedAttnPlan a = {};
   const int64_t most = (max_new < T ? max_new : T) * G;  // query rows of a request and head, at most
-  a.few = kFewRows;
   a.R = most <= 16 ? 16 : kFewRows;
   a.rows = (int)(most < kFewRows ? most : kFewRows);
   a.run_many = most > kFewRows;
-  // one request whose rows are all there are is known to be large; more may be of either kind
-  a.run_few = !a.run_many || S > 1 || T <= kFewRows / G;
+  // T and max_new are bounds, so what may be large may also be small.  Of several requests both
+  // kernels take theirs; one request, which is most often as large as its bounds, is
+  // attn_many_kernel's whatever it has (attn_few_kernel and its join without rows cost 8 us, a
+  // third of a prompt of 500 tokens).
+  a.run_few = !a.run_many || S > 1;
+  a.few = a.run_few ? kFewRows : 0;
   const int tm = kManyRows / G;
   a.nsplit = a.part_units = 1;
   if (a.run_many) {
-    const int64_t large = T / (kFewRows / G + 1) < S ? T / (kFewRows / G + 1) : S;  // requests that can be large
+    // requests that attn_many_kernel can have (of one, T is more than kFewRows / G)
+    const int64_t large = T / (kFewRows / G + 1) < S ? T / (kFewRows / G + 1) : S;
     a.tiles = T / tm + large;
     // two workgroups on each of 256 CUs: the parts that leave the fewest places idle in the last
     // round, the first that leave at most a tenth.  A part costs its sums' way to memory and back,

@@ -835,3 +835,65 @@ def test_interleaved_pools_and_shared_pages(new):
     flat = [torch.stack([kv[2 * s + i][:, h] for s in range(2) for h in range(H)]).to(DEV) for i in range(2)]
     want = F.fathom_pack(flat[0].float(), nn.repeat_interleave(H), 2)
     assert torch.equal(planes, want[0]) and torch.equal(scales, want[1])
+
+
+# ---------------------------------------------------------------- one request under loose bounds
+def close(got, q, K, V, n, G, chunk, sm=1 / np.sqrt(D)):
+    """Whether the rows [new][G][D] of one request and head are within the tolerance above; chunk: probabilities are
+    rounded once.  Outputs below the type's normal numbers are off by half of their step."""
+    t = q.dtype
+    eps = torch.finfo(t).eps
+    ref, mag, top = O.paged_attn(q.double().numpy(), K.double().numpy(), V.double().numpy(), n, G, sm)
+    dz = (D + 8) * 2.0 ** -24 * top[..., None]
+    tol = eps / 2 * np.abs(ref) + mag * ((eps / 2 if chunk else eps * eps) + 2 * dz + 64 * 2.0 ** -24) * (1 + eps)
+    return (np.abs(got.double().cpu().numpy() - ref) <= tol + torch.finfo(t).smallest_normal * eps / 2).all()
+
+
+@pytest.mark.parametrize("new", [0, 1, "few", "more"])
+@pytest.mark.parametrize("H,G,n,T,max_new,lead,dt", [(2, 4, 150, 16, 16, 0, "f16"), (2, 4, 3000, 64, 64, 3, "bf16"),
+                                                     (8, 4, 200, 2048, 2048, 5, "f16"), (1, 8, 100, 40, 33, 3, "bf16"),
+                                                     (2, 1, 90, 100, 64, 1, "f16"), (1, 3, 5000, 300, 1 << 40, 7, "bf16")])
+def test_attn_one_request_below_its_bounds(H, G, n, T, max_new, lead, dt, new):
+    """max_new and T are bounds: one request may have any number of tokens below them, few query rows among them."""
+    new = {"few": 32 // G, "more": 32 // G + 1}.get(new, new)
+    rng = np.random.default_rng(31)
+    table, K, V, Kr, Vr = pools(rng, [n], H, 32, TYPES[dt])
+    q = torch.from_numpy(rng.standard_normal((T, H * G, D)).astype(np.float32) * 2).to(TYPES[dt])
+    out, st = torch.full((T, H * G, D), 5.0, dtype=TYPES[dt], device=DEV), F.new_status()
+    F.fathom_paged_attn(q.to(DEV), K, V, table, i64([lead, lead + new]), i64([n]), max_new, out=out, dev_status=st)
+    assert status(st) == 0
+    mine = slice(lead, lead + new)
+    for h in range(H if new else 0):
+        heads = slice(h * G, (h + 1) * G)
+        assert close(out[mine, heads], q[mine, heads], Kr[0][h], Vr[0][h], n, G, True), h
+    out[mine] = 5.0
+    assert (out == 5.0).all()
+
+
+def test_attn_one_request_in_a_graph_with_other_lengths():
+    """A call captured for up to 16 tokens, replayed with fewer, none and all of them."""
+    rng = np.random.default_rng(32)
+    H, G, T, n = 2, 4, 16, 300
+    table, K, V, Kr, Vr = pools(rng, [n], H, 16, torch.float16)
+    q = torch.from_numpy(rng.standard_normal((T, H * G, D)).astype(np.float32) * 2).half()
+    qd, start, out = q.to(DEV), i64([0, T]), torch.zeros((T, H * G, D), dtype=torch.float16, device=DEV)
+    ws = torch.empty((F.fathom_paged_attn_workspace_size(T, 1, H, G, T),), dtype=torch.uint8, device=DEV)
+
+    def call():
+        return F.fathom_paged_attn(qd, K, V, table, start, i64n, T, out=out, ws=ws)
+
+    i64n = i64([n])
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for a, b in ((0, 16), (0, 1), (3, 11), (5, 5), (7, 16), (15, 16)):
+        start.copy_(i64([a, b]))
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for h in range(H if b > a else 0):
+            heads = slice(h * G, (h + 1) * G)
+            assert close(out[a:b, heads], q[a:b, heads], Kr[0][h], Vr[0][h], n, G, True), (a, b)
+        assert (out[:a] == 5.0).all() and (out[b:] == 5.0).all()
