@@ -3,12 +3,14 @@
 A thin ctypes binding over ``libfathom.so`` (declared in ``include/fathom.h``):
 the functions below carry the C names and only marshal arguments -- tensors
 in, device pointers and sizes out to the C ABI, the caller's current HIP
-stream, status codes turned into exceptions.  Every step of the path runs in
+stream (or the torch stream given as ``stream``, on which what the call makes is
+allocated too), status codes turned into exceptions.  Every step of the path runs in
 the library's HIP kernels; PyTorch provides device memory and streams.  There
 is no CPU fallback: if the library is not built, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import struct
@@ -172,6 +174,17 @@ def _dev(*ts):
             raise ValueError("fathom calls take device tensors")
 
 
+def _empty(stream, shape, **kw):
+    """A tensor that a call returns, from the memory of the stream that the call launches on: whoever had that memory before
+    is done with it in that stream's order, and the caller's own stream may read it for as long as the caller holds it."""
+    if stream is None:
+        return torch.empty(shape, **kw)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, **kw)
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def new_status(device=None) -> torch.Tensor:
     """A zeroed device status word (int32 view of the uint32 the kernels OR into)."""
     return torch.zeros(1, dtype=torch.int32, device=device or "cuda")
@@ -186,9 +199,9 @@ def fathom_pack(K, n, nb_cap=None, planes=None, scales=None, dev_status=None, st
         raise ValueError("K channel stride must be 1")
     nb_cap = (ntok + 63) // 64 if nb_cap is None else int(nb_cap)
     if planes is None:
-        planes = torch.empty((U, D, 4, nb_cap), dtype=torch.int64, device=K.device)
+        planes = _empty(stream, (U, D, 4, nb_cap), dtype=torch.int64, device=K.device)
     if scales is None:
-        scales = torch.empty((U, D, nb_cap), dtype=torch.int16, device=K.device)
+        scales = _empty(stream, (U, D, nb_cap), dtype=torch.int16, device=K.device)
     _check(lib().fathom_pack(_p(K), _dt(K), K.stride(1), K.stride(0), _p(n), U, D, nb_cap, _p(planes), _p(scales),
                              _p(dev_status), _stream(stream)), "fathom_pack")
     return planes, scales
@@ -229,9 +242,9 @@ def fathom_alloc_depths(q, var, mode=FATHOM_WATERFILL, budget_or_r=48, depths=No
     if not q.is_contiguous() or (var is not None and not var.is_contiguous()):
         raise ValueError("q and var must be contiguous")
     if depths is None:
-        depths = torch.empty((U, D), dtype=torch.uint8, device=q.device)
+        depths = _empty(stream, (U, D), dtype=torch.uint8, device=q.device)
     if theta is None:
-        theta = torch.empty((U,), dtype=torch.float32, device=q.device)
+        theta = _empty(stream, (U,), dtype=torch.float32, device=q.device)
     _check(lib().fathom_alloc_depths(_p(q), _dt(q), U, G, D, _p(var), int(mode), int(budget_or_r), _p(depths),
                                      _p(theta), _p(dev_status), _stream(stream)), "fathom_alloc_depths")
     return depths, theta
@@ -244,7 +257,7 @@ def fathom_scan(planes, scales, n, q, depths, scores=None, ld_s=None, dev_status
     G = q.shape[1]
     if scores is None:
         ld_s = 64 * nb_cap if ld_s is None else int(ld_s)
-        scores = torch.empty((U, G, ld_s), dtype=torch.float32, device=q.device)
+        scores = _empty(stream, (U, G, ld_s), dtype=torch.float32, device=q.device)
     else:
         ld_s = scores.shape[-1] if ld_s is None else int(ld_s)
     _check(lib().fathom_scan(_p(planes), _p(scales), _p(n), U, D, nb_cap, _p(q), _dt(q), G, _p(depths), _p(scores),
@@ -260,9 +273,11 @@ def fathom_scan_topk_workspace_size(U, G, max_n, k) -> int:
     return int(lib().fathom_scan_topk_workspace_size(int(U), int(G), int(max_n), int(k)))
 
 
-def _ws(nbytes, ws, device):
+def _ws(nbytes, ws, device, stream):
+    """A workspace for one call, from the memory of its stream: dropped on return, it goes to later work of that stream."""
     if ws is None:
-        ws = torch.empty((max(int(nbytes), 1),), dtype=torch.uint8, device=device)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            ws = torch.empty((max(int(nbytes), 1),), dtype=torch.uint8, device=device)
     return ws
 
 
@@ -271,10 +286,10 @@ def fathom_topk(scores, n, k, lo=0, tail=0, idx=None, val=None, ws=None, dev_sta
     _dev(scores, n)
     U, G, ld_s = scores.shape
     if idx is None:
-        idx = torch.empty((U, G, k), dtype=torch.int32, device=scores.device)
+        idx = _empty(stream, (U, G, k), dtype=torch.int32, device=scores.device)
     if val is None:
-        val = torch.empty((U, G, k), dtype=torch.float32, device=scores.device)
-    ws = _ws(fathom_topk_workspace_size(U, G, ld_s, k), ws, scores.device)
+        val = _empty(stream, (U, G, k), dtype=torch.float32, device=scores.device)
+    ws = _ws(fathom_topk_workspace_size(U, G, ld_s, k), ws, scores.device, stream)
     _check(lib().fathom_topk(_p(scores), ld_s, _p(n), U, G, int(k), int(lo), int(tail), _p(idx), _p(val), _p(ws),
                              ws.numel() * ws.element_size(), _p(dev_status), _stream(stream)), "fathom_topk")
     return idx, val
@@ -288,10 +303,10 @@ def fathom_scan_topk(planes, scales, n, q, depths, k, lo=0, tail=0, idx=None, va
     U, D, _, nb_cap = planes.shape
     G = q.shape[1]
     if idx is None:
-        idx = torch.empty((U, G, k), dtype=torch.int32, device=q.device)
+        idx = _empty(stream, (U, G, k), dtype=torch.int32, device=q.device)
     if val is None:
-        val = torch.empty((U, G, k), dtype=torch.float32, device=q.device)
-    ws = _ws(fathom_scan_topk_workspace_size(U, G, 64 * nb_cap, k), ws, q.device)
+        val = _empty(stream, (U, G, k), dtype=torch.float32, device=q.device)
+    ws = _ws(fathom_scan_topk_workspace_size(U, G, 64 * nb_cap, k), ws, q.device, stream)
     _check(lib().fathom_scan_topk_ex(_p(planes), _p(scales), _p(n), U, D, nb_cap, _p(q), _dt(q), G, _p(depths),
                                      int(k), int(lo), int(tail), int(max_unit_bits), _p(idx), _p(val), _p(ws),
                                      ws.numel() * ws.element_size(), _p(dev_status), _stream(stream)),
@@ -333,9 +348,9 @@ def fathom_sparse_attn(q, Krows, Vrows, n, idx, n_sink=0, n_local=0, sm_scale=No
     if sm_scale is None:
         sm_scale = 1.0 / (D ** 0.5)
     if out is None:
-        out = torch.empty((U, G, D), dtype=torch.float32, device=q.device)
+        out = _empty(stream, (U, G, D), dtype=torch.float32, device=q.device)
     wsb = fathom_sparse_attn_workspace_size(U, G, k, n_sink, n_local)
-    ws = _ws(wsb, ws, q.device)
+    ws = _ws(wsb, ws, q.device, stream)
     _check(lib().fathom_sparse_attn(_p(q), _dt(q), _p(Krows), _p(Vrows), Krows.stride(1), Krows.stride(0), _p(n),
                                     U, G, D, _p(idx), k, int(n_sink), int(n_local), C.c_float(sm_scale), _p(out),
                                     _p(ws), ws.numel(), _p(dev_status), _stream(stream)), "fathom_sparse_attn")
@@ -355,10 +370,10 @@ def fathom_klt_calibrate(K, n, mu=None, V=None, lam=None, ws=None, dev_status=No
     if K.stride(2) != 1:
         raise ValueError("K channel stride must be 1")
     f32 = dict(dtype=torch.float32, device=K.device)
-    mu = torch.empty((U, D), **f32) if mu is None else mu
-    V = torch.empty((U, D, D), **f32) if V is None else V
-    lam = torch.empty((U, D), **f32) if lam is None else lam
-    ws = _ws(fathom_klt_calibrate_workspace_size(U), ws, K.device)
+    mu = _empty(stream, (U, D), **f32) if mu is None else mu
+    V = _empty(stream, (U, D, D), **f32) if V is None else V
+    lam = _empty(stream, (U, D), **f32) if lam is None else lam
+    ws = _ws(fathom_klt_calibrate_workspace_size(U), ws, K.device, stream)
     _check(lib().fathom_klt_calibrate(_p(K), _dt(K), K.stride(1), K.stride(0), _p(n), ncap, U, D, _p(mu), _p(V),
                                       _p(lam), _p(ws), ws.numel(), _p(dev_status), _stream(stream)),
            "fathom_klt_calibrate")
@@ -376,7 +391,7 @@ def fathom_klt_rotate_keys(K, n, mu, V, out=None, dev_status=None, stream=None):
     if mu.dtype != torch.float32 or V.dtype != torch.float32:
         raise TypeError("mu and V must be fp32")
     if out is None:
-        out = torch.empty((U, ncap, D), dtype=torch.float32, device=K.device)
+        out = _empty(stream, (U, ncap, D), dtype=torch.float32, device=K.device)
     if out.dtype != torch.float32 or out.stride(2) != 1 or out.stride(1) != D:
         raise ValueError("out must be fp32 rows of D floats")
     _check(lib().fathom_klt_rotate_keys(_p(K), _dt(K), K.stride(1), K.stride(0), _p(n), ncap, U, D, _p(mu), _p(V),
@@ -392,7 +407,7 @@ def fathom_klt_rotate_q(q, V, out=None, stream=None):
     if not q.is_contiguous() or not V.is_contiguous() or V.dtype != torch.float32:
         raise ValueError("q contiguous; V contiguous fp32")
     if out is None:
-        out = torch.empty((U, G, D), dtype=torch.float32, device=q.device)
+        out = _empty(stream, (U, G, D), dtype=torch.float32, device=q.device)
     _check(lib().fathom_klt_rotate_q(_p(q), _dt(q), U, G, D, _p(V), _p(out), _stream(stream)), "fathom_klt_rotate_q")
     return out
 
@@ -457,11 +472,11 @@ def fathom_paged_map(n_old, n, page, table, ring, state, T, H=1, slots=None, sta
     S, ld = _table(table)
     T, H = int(T), int(H)
     i64 = dict(dtype=torch.int64, device=table.device)
-    slots = torch.empty((T,), **i64) if slots is None else slots
-    start = torch.empty((S + 1,), **i64) if start is None else start
-    n_now = torch.empty((S,), **i64) if n_now is None else n_now
-    n_unit = torch.empty((S * H,), **i64) if n_unit is None else n_unit
-    state_out = torch.empty((2,), **i64) if state_out is None else state_out
+    slots = _empty(stream, (T,), **i64) if slots is None else slots
+    start = _empty(stream, (S + 1,), **i64) if start is None else start
+    n_now = _empty(stream, (S,), **i64) if n_now is None else n_now
+    n_unit = _empty(stream, (S * H,), **i64) if n_unit is None else n_unit
+    state_out = _empty(stream, (2,), **i64) if state_out is None else state_out
     st = _here(stream, (table, n_old, n, ring, state, slots, start, n_now, n_unit, state_out, dev_status))
     _int64("n_old", n_old, S)
     _int64("n", n, S)
@@ -530,11 +545,11 @@ def fathom_paged_sparse_attn(q, Kpages, Vpages, table, n, idx, n_sink=0, n_local
     k = 0 if idx is None else idx.shape[-1]
     sm_scale = 1.0 / (D ** 0.5) if sm_scale is None else sm_scale
     if out is None:
-        out = torch.empty((U, G, D), dtype=torch.float32, device=q.device)
+        out = _empty(stream, (U, G, D), dtype=torch.float32, device=q.device)
     elif out.dtype is not torch.float32 or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("out is contiguous fp32 [S*H][G][D]")
     if ws is None:
-        ws = _ws(fathom_sparse_attn_workspace_size(U, G, k, n_sink, n_local), ws, q.device)
+        ws = _ws(fathom_sparse_attn_workspace_size(U, G, k, n_sink, n_local), ws, q.device, stream)
     _check(lib().fathom_paged_sparse_attn(_a(q), _paged_dt(q), pg, _a(table), ld, _a(n), S, G, D, _a(idx), k,
                                           int(n_sink), int(n_local), sm_scale, _a(out), _a(ws),
                                           ws.numel() * ws.element_size(), _a(dev_status), st), "fathom_paged_sparse_attn")
@@ -568,11 +583,11 @@ def fathom_paged_attn(q, Kpages, Vpages, table, start, n, max_new, sm_scale=None
         raise ValueError("slopes is contiguous fp32 [H*G]")
     sm_scale = 1.0 / (D ** 0.5) if sm_scale is None else sm_scale
     if out is None:
-        out = torch.empty((T, HG, D), dtype=q.dtype, device=q.device)
+        out = _empty(stream, (T, HG, D), dtype=q.dtype, device=q.device)
     elif out.dtype is not q.dtype or out.shape != q.shape or not out.is_contiguous():
         raise ValueError("out is contiguous [T][H*G][D] of the pages' type")
     if ws is None:
-        ws = _ws(fathom_paged_attn_workspace_size(T, S, H, HG // H, max_new), ws, q.device)
+        ws = _ws(fathom_paged_attn_workspace_size(T, S, H, HG // H, max_new), ws, q.device, stream)
     _check(lib().fathom_paged_attn(_a(q), qs[0], qs[1], pg, _a(table), ld, _a(start), _a(n), S, T, int(max_new),
                                    HG // H, D, sm_scale, softcap, _a(slopes), _a(prefix), _a(first), _a(out), _a(ws),
                                    ws.numel() * ws.element_size(), _a(dev_status), st), "fathom_paged_attn")

@@ -897,3 +897,63 @@ def test_attn_one_request_in_a_graph_with_other_lengths():
             heads = slice(h * G, (h + 1) * G)
             assert close(out[a:b, heads], q[a:b, heads], Kr[0][h], Vr[0][h], n, G, True), (a, b)
         assert (out[:a] == 5.0).all() and (out[b:] == 5.0).all()
+
+
+# ---------------------------------------------------------------- streams
+def pool_of(stream):
+    """Address ranges of the memory that the allocator keeps for a stream."""
+    return [(x["address"], x["address"] + x["total_size"]) for x in torch.cuda.memory_snapshot()
+            if x["stream"] == stream.cuda_stream]
+
+
+def test_what_a_call_makes_is_of_its_stream():
+    """With stream= given, outputs and workspaces made by a call lie in that stream's memory (the current stream's may be
+    handed out again while the call runs), for the paged calls and those over contiguous rows."""
+    rng = np.random.default_rng(35)
+    H, G, n = 2, 4, 500
+    table, K, V, _, _ = pools(rng, [n], H, 16, torch.float16, fill=0.0)
+    q = torch.from_numpy(rng.standard_normal((1, H * G, D)).astype(np.float32)).half().to(DEV)
+    qu, flat = q.view(H, G, D), torch.randn((H, n, D), device=DEV)
+    rows = flat.half()
+    nn, nu, var = i64([n]), i64([n] * H), torch.ones((H, D), device=DEV)
+    idx = torch.arange(60, dtype=torch.int32, device=DEV).expand(H, G, 60).contiguous()
+    torch.cuda.synchronize()
+    x = torch.cuda.Stream()
+    kw = dict(stream=x)
+    made = [F.fathom_paged_attn(q, K, V, table, i64([0, 1]), nn, 1, **kw)]
+    need = F.fathom_paged_attn_workspace_size(1, 1, H, G, 1)
+    assert sum(b - a for a, b in pool_of(x)) >= need  # the workspace was there
+    made += F.fathom_paged_map(nn, nn + 1, 16, table.clone(), torch.arange(8, dtype=torch.int32, device=DEV), i64([0, 8]), 1,
+                               H, **kw)
+    made += [F.fathom_paged_sparse_attn(qu, K, V, table, nn, idx, **kw), F.fathom_sparse_attn(qu, rows, rows, nu, idx, **kw)]
+    planes, scales = F.fathom_pack(flat, nu, **kw)
+    dep, th = F.fathom_alloc_depths(qu, var, **kw)
+    scores = F.fathom_scan(planes, scales, nu, qu, dep, **kw)
+    made += [planes, scales, dep, th, scores, *F.fathom_topk(scores, nu, 30, **kw)]
+    made += F.fathom_scan_topk(planes, scales, nu, qu, dep, 30, **kw)
+    mu, basis, lam = F.fathom_klt_calibrate(flat, nu, **kw)
+    made += [mu, basis, lam, F.fathom_klt_rotate_keys(flat, nu, mu, basis, **kw), F.fathom_klt_rotate_q(qu, basis, **kw)]
+    torch.cuda.synchronize()
+    ranges = pool_of(x)
+    for i, t in enumerate(made):
+        assert any(a <= t.data_ptr() < b for a, b in ranges), (i, t.shape)
+
+
+def test_calls_on_two_streams_make_their_own_workspaces():
+    """Calls on two streams in turn, each with a workspace and an output of its own making."""
+    rng = np.random.default_rng(36)
+    H, G = 2, 4
+    cases = []
+    for lengths, new in (([3000, 90], 1), ([64, 5000], 1), ([700, 400], 90), ([9000, 20], 8)):
+        table, K, V, _, _ = pools(rng, lengths, H, 32, torch.float16)
+        news = [min(new, m) for m in lengths]
+        q = torch.from_numpy(rng.standard_normal((sum(news), H * G, D)).astype(np.float32)).half().to(DEV)
+        cases.append((q, K, V, table, i64([0, news[0], sum(news)]), i64(lengths), max(news)))
+    want = [F.fathom_paged_attn(*c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = [F.fathom_paged_attn(*c, stream=streams[i % 2]) for i, c in enumerate(cases)]
+        torch.cuda.synchronize()
+        for w, g in zip(want, got):
+            assert torch.equal(w, g)
