@@ -423,7 +423,7 @@ def _a(t):
 
 
 def _here(stream, ts):
-    """The raw stream, after a check that the tensors are on the current device: the launch goes to it."""
+    """The raw stream, after a check that it and the tensors are of the current device: the launch goes to it."""
     if not ts[0].is_cuda:
         raise ValueError("fathom calls take device tensors")
     dev = _get_device()
@@ -431,6 +431,8 @@ def _here(stream, ts):
         if t is not None and t.get_device() != dev:
             raise ValueError("paged calls take tensors of the current device")
     if stream is not None:
+        if stream.device_index != dev:
+            raise ValueError("paged calls take a stream of the current device")
         return stream.cuda_stream
     return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 

@@ -957,3 +957,16 @@ def test_calls_on_two_streams_make_their_own_workspaces():
         torch.cuda.synchronize()
         for w, g in zip(want, got):
             assert torch.equal(w, g)
+
+
+def test_a_stream_of_another_device_is_refused():
+    class Other:  # as a torch stream of the next device looks
+        device_index, cuda_stream = torch.cuda.current_device() + 1, 0
+
+    K, V = (torch.zeros((2, 1, 16, D), dtype=torch.float16, device=DEV) for _ in range(2))
+    x = torch.ones((1, 1, D), dtype=torch.float16, device=DEV)
+    with pytest.raises(ValueError, match="stream of the current device"):
+        F.fathom_paged_write(x, x, i64([3]), K, V, stream=Other())
+    F.fathom_paged_write(x, x, i64([3]), K, V, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    assert (K[0, 0, 3] == 1).all() and float(K.float().sum()) == D
