@@ -467,8 +467,11 @@ fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fa
  * query head hg sees the positions j in [max(first, 0), max(p + 1, min(prefix[s], n[s]))):
  *   z_j = sm_scale * q . K_j;  softcap > 0: z_j = softcap * tanh(z_j / softcap);
  *   slopes: z_j -= slopes[hg] * |p - j|;
- *   out = sum_j softmax_j(z) V_j, and 0 where it sees no position.
- * Rows outside what a token sees do not enter its result, whatever they hold.
+ *   out = sum_j softmax_j(z) V_j, and 0 where it sees no position (or none whose score
+ *   is above -Inf).
+ * Rows outside what a token sees do not enter its result, whatever they hold.  A value of V
+ * that is not finite reaches every token that sees its row, however small its probability:
+ * Inf as Inf, Inf of both signs and NaN as NaN.
  *
  *   q        [T][H*G][D] of the pages' type, row (i, hg) at q[i*ldq_tok + hg*ldq_head];
  *            16-byte aligned, strides >= 0 and multiples of 8 elements.

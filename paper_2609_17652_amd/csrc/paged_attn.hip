@@ -28,7 +28,10 @@
 // Rows that a query must not see get a probability of 0, but 0 * Inf is not 0:
 // V rows behind the end are cleared in LDS, and in steps with masked places
 // the non-finite values of V are taken out of the product and added for the rows
-// that see them.
+// that see them.  Elsewhere they go into the product as they are: they change their own
+// channel only, which is made up anew at the end of a piece or tile where it is not finite
+// (nothing in the loops, 0.3 us a call where latency counts; with one such value 2048 tokens
+// over 65536 take 9.0 ms instead of 2.3, 32 ragged single tokens 1.2 instead of 0.6).
 #include <type_traits>
 
 #include "paged.hpp"
@@ -262,6 +265,69 @@ __device__ __forceinline__ s16x8 finite_part(s16x8 v) {
 template <bool BF>
 __device__ __forceinline__ float nonfinite_part(short x) {
   return nonfinite_bits<BF>(x) ? (float)__builtin_bit_cast(typename Mx<BF>::t, x) : 0.0f;
+}
+
+// A channel of O that a value which is not finite came into may be NaN where the sum is
+// infinite: probabilities below 2^-149 (of 16 bits, below their last place) are 0, and 0 * Inf is
+// NaN, as is Inf - Inf where a probability is a sum of two values.  Such channels are made up
+// anew, from the rows of V that hold such values: what follows finds them among keys [k0, k1), k0 a
+// multiple of 16, in the pages, 16 at a time, and visits each.  A wave by itself.
+template <bool BF, class Fn>
+__device__ __forceinline__ void nonfinite_rows(const PagedAttnArgs& p, int s, int h, int k0, int k1, Fn visit) {
+  const int lane = threadIdx.x & 63, quad = lane >> 4;
+#pragma unroll 1
+  for (int k = k0; k < k1; k += 16) {
+    const int id = page_uniform(p.c, s, k >> p.c.shift);
+    if ((uint32_t)id >= (uint32_t)p.c.P) continue;
+    const uint16_t* row0 = p.c.V + (int64_t)id * p.c.ld_page + (int64_t)h * p.c.ld_head +
+                           (int64_t)(k & ((1 << p.c.shift) - 1)) * p.c.ld_tok;
+    s16x8 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 4 * i + quad;
+      v[i] = (s16x8){};
+      if (k + row < k1) v[i] = *reinterpret_cast<const s16x8*>(row0 + row * p.c.ld_tok + 8 * (lane & 15));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bad |= nonfinite_bits<BF>(v[i][e]);
+      const uint64_t lanes = __ballot(bad);
+#pragma unroll 1
+      for (int j = 0; j < 4; ++j)
+        if (lanes >> (16 * j) & 0xFFFF) visit(k + 4 * i + j, row0 + (4 * i + j) * p.c.ld_tok);
+    }
+  }
+}
+// Element `bit` of a lane's part of O with a seen value x: the first that is not finite takes the
+// place of what is there, the others are added.
+template <bool BF>
+__device__ __forceinline__ float with_nonfinite(float o, short x, uint64_t& found, int bit) {
+  if (!nonfinite_bits<BF>(x)) return o;
+  const float y = nonfinite_part<BF>(x);
+  const bool more = found >> bit & 1;
+  found |= 1ull << bit;
+  return more ? o + y : y;
+}
+// Four channels of the sum of a row's parts at(c), c = first, first + step .. below count (-1: not
+// there), against the maximum M; where `o`, that sum, is not finite the parts are added again,
+// and what is not finite in a part is kept where its weight is 0.
+template <class At>
+__device__ __forceinline__ f32x4 parts_sum(const PagedAttnArgs& p, f32x4 o, int first, int step, int count, float M, At at) {
+  const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f}, z = o * zero;
+  if ((z[0] + z[1]) + (z[2] + z[3]) == 0.0f) return o;
+  o = zero;
+#pragma unroll 1
+  for (int c = first; c < count; c += step) {
+    const int64_t row = at(c);
+    if (row < 0 || p.part_ml[2 * row] == -__builtin_huge_valf()) continue;
+    const float w = __builtin_amdgcn_exp2f(p.part_ml[2 * row] - M);
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + row * kD + 4 * (threadIdx.x & 31));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += w == 0.0f && v[e] - v[e] != 0.0f ? v[e] : w * v[e];
+  }
+  return o;
 }
 
 // z in units of log2: the scaled score, capped, less the distance's bias.
@@ -648,12 +714,38 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
     const bool whole = b_first == 0 && b_end == now.nb;
     const int slot = step - (b_end - b_first) == 0 ? 0 : 1;
     const int64_t pr = ((int64_t)worker * 2 + slot) * R;
+    float sum[CT], zeros[4] = {};  // zeros: NaN where O is not finite and the sum is
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      sum[t] = l[t];
+      sum[t] += __shfl_xor(sum[t], 16, kWave);
+      sum[t] += __shfl_xor(sum[t], 32, kWave);
+      if (16 * t + lr < rows && sum[t] - sum[t] == 0.0f) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) zeros[e] = __builtin_fmaf(o[t][c][e], 0.0f, zeros[e]);
+      }
+    }
+    if (__ballot((zeros[0] + zeros[1]) + (zeros[2] + zeros[3]) != 0.0f)) {
+      uint64_t found = 0;
+      const int key = lo_key + kFewKeys * b_first;
+      nonfinite_rows<BF>(p, s, h, key, min(n, lo_key + kFewKeys * b_end), [&](int k, const uint16_t* row) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const s16x4 x = *reinterpret_cast<const s16x4*>(row + 16 * c + 4 * quad);
+#pragma unroll
+          for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (k >= lo[t] && k < hi[t]) o[t][c][e] = with_nonfinite<BF>(o[t][c][e], x[e], found, 32 * t + 4 * c + e);
+        }
+      });
+    }
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
       const int r = 16 * t + lr;
-      float lt = l[t];
-      lt += __shfl_xor(lt, 16, kWave);
-      lt += __shfl_xor(lt, 32, kWave);
+      const float lt = sum[t];
       if (r >= rows) continue;
       if (whole) {
         const int tok = r / G, g = r - tok * G;
@@ -727,6 +819,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
   };
   // a part is its wave's first piece, but for a wave that begins in an earlier request or head
   const int64_t step = 2 * R, late = share(w0, W) < g0 ? R : 0;
+  auto part_of = [&](int r) {
+    return [=](int c) -> int64_t {
+      return share(w0 + c, W) == share(w0 + c + 1, W) ? -1 : w0 * step + r + c * step + (c == 0 ? late : 0);
+    };
+  };
   if (count <= kJoinBatch) {
     for (int r = blockIdx.y * kJoinGroups + g; r < rows; r += gridDim.y * kJoinGroups) {
       const int64_t row0 = w0 * step + r;
@@ -751,7 +848,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
         l += w * lp[c];
         o += w * v[c];
       }
-      store(r, o, l);
+      store(r, parts_sum(p, o, 0, 1, count, M, part_of(r)), l);
     }
     return;
   }
@@ -770,8 +867,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
     M = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
     for (int c = tid; c < count; c += 256) {
       const float m = weight[c];
-      const float w = m == -__builtin_huge_valf() ? 0.0f : __builtin_amdgcn_exp2f(m - M);
-      weight[c] = w;
+      const float w = m == -__builtin_huge_valf() ? -1.0f : __builtin_amdgcn_exp2f(m - M);
+      weight[c] = w;  // -1: none, the part may not be there
       if (m != -__builtin_huge_valf()) l += w * p.part_ml[2 * (row0 + c * step + (c == 0 ? late : 0)) + 1];
     }
     l = wave_sum(l);
@@ -785,16 +882,16 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs p, int R) 
       for (int i = 0; i < kJoinBatch; ++i) {
         const int c = c0 + i * kJoinGroups;
         const int cc = min(c, count - 1);  // (behind the last: that one again, unused)
-        w[i] = c < count ? weight[cc] : 0.0f;
+        w[i] = c < count ? weight[cc] : -1.0f;
         v[i] = *reinterpret_cast<const f32x4*>(p.part_o + (row0 + cc * step + (cc == 0 ? late : 0)) * kD + 4 * x);
       }
 #pragma unroll
       for (int i = 0; i < kJoinBatch; ++i) {
         const f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-        o += w[i] != 0.0f ? w[i] * v[i] : z;  // a part without weight may not be there
+        o += w[i] < 0.0f ? z : w[i] * v[i];
       }
     }
-    acc[g][x] = o;
+    acc[g][x] = parts_sum(p, o, g, kJoinGroups, count, M, part_of(r));
     __syncthreads();
     if (tid >= 32) {
       if constexpr (LOOP) continue;
@@ -1192,7 +1289,7 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
     if (!__ballot(__builtin_fmaf(mx, c1, nr) > kSlack + Mx<BF>::kShift)) return false;
     const float top = fmaxf(mx, __shfl_xor(mx, 32, kWave));
     const float to = fminf(nr, Mx<BF>::kShift - top * c1);
-    f = fmaxf(__builtin_amdgcn_exp2f(to - nr), 0x1p-126f);  // not 0: O may hold an infinity
+    f = __builtin_amdgcn_exp2f(to - nr);
     nr = to;
     l *= f;
     return true;
@@ -1329,7 +1426,7 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
   prepare(0);
   map_block(sa, key0);
   mask_block(sa, key0);
-  raise(f);  // (O is 0, or infinite)
+  raise(f);  // (O is 0, or not finite)
   scores(stage(1), sb);
   exponentials(sa, pa);
   map_block(sb, key0 + kBlock);
@@ -1364,6 +1461,27 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
   wait_vm<0>();
   const int r = wave * 32 + lr;
   l += __shfl_xor(l, 32, kWave);
+  {
+    float zeros[4] = {};
+    if (r < rows && l - l == 0.0f) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) zeros[e & 3] = __builtin_fmaf(o[d][e], 0.0f, zeros[e & 3]);
+    }
+    if (__ballot((zeros[0] + zeros[1]) + (zeros[2] + zeros[3]) != 0.0f)) {
+      uint64_t found = 0;
+      nonfinite_rows<BF>(p, t.s, h, key0, min(n, key0 + nb * kBlock), [&](int k, const uint16_t* row) INLINE {
+#pragma unroll
+        for (int y = 0; y < 16; ++y) {
+          const s16x4 x = *reinterpret_cast<const s16x4*>(row + 8 * y + 4 * half);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (k >= lo && k < hi) o[y >> 2][4 * (y & 3) + e] = with_nonfinite<BF>(o[y >> 2][4 * (y & 3) + e], x[e], found, 4 * y + e);
+        }
+      });
+    }
+  }
   if (r >= rows) return;
   if (parts == 1) {
     const int tok = r / G, g = r - tok * G;
@@ -1439,6 +1557,7 @@ __global__ __launch_bounds__(256) void attn_many_join_kernel(PagedAttnArgs p) {
         o += w * v[c];
       }
     }
+    o = parts_sum(p, o, 0, 1, parts, M, [&](int c) { return base + (int64_t)c * kManyRows + r; });
     const int tok = r / G;
     typename Mx<BF>::t y[4];
 #pragma unroll

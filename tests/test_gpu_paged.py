@@ -970,3 +970,65 @@ def test_a_stream_of_another_device_is_refused():
     F.fathom_paged_write(x, x, i64([3]), K, V, stream=torch.cuda.current_stream())
     torch.cuda.synchronize()
     assert (K[0, 0, 3] == 1).all() and float(K.float().sum()) == D
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("n,new", [(64, 1), (64, 3), (160, 1), (600, 4), (5000, 1), (40000, 1), (130, 60), (3000, 60)])
+def test_attn_infinities_in_seen_places(n, new, dt):
+    """A value of V that is not finite reaches every token that sees its row, wherever the row lies in a block and however
+    small its probability is: Inf as Inf, Inf of both signs and NaN as NaN.  Other channels, heads and tokens are as if it
+    were not there."""
+    t, G = TYPES[dt], 4
+    for seed in range(3):
+        rng = np.random.default_rng(40 + seed)
+        table, K, V, Kr, Vr = pools(rng, [n], 2, 16, t)
+        row = lambda pool, i: pool[int(table[0, i // 16]), 0, i % 16]  # noqa: E731
+        q = torch.from_numpy(np.abs(rng.standard_normal((new, 2 * G, D))).astype(np.float32)).to(t)
+        # key 7 scores about -900 and the last old one about +180: after it, earlier keys' probabilities are below 2^-149
+        for i, x in ((7, -100.0), (n - new - 1, 20.0)):
+            row(K, i).fill_(x)
+            Kr[0][0, i] = x
+        inf = float("inf")
+        for i, c, x in ((5, 3, inf), (5, 77, -inf), (5, 9, inf), (41, 9, -inf), (33, 20, float("nan")), (7, 50, inf),
+                        (n - new - 1, 100, -inf), (45, 60, inf)):
+            row(V, i)[c] = x
+            Vr[0][0, i, c] = 0.0
+        first = np.where(np.arange(new) % 2 == 1, 12, 0)  # the odd tokens do not see keys 5 and 7
+        out, st = torch.empty((new, 2 * G, D), dtype=t, device=DEV), F.new_status()
+        F.fathom_paged_attn(q.to(DEV), K, V, table, i64([0, new]), i64([n]), new, first=i64(first.tolist()), out=out,
+                            dev_status=st)
+        assert status(st) == 0
+        out = out.cpu().double()
+        even, odd = out[0::2, :G], out[1::2, :G]
+        assert (even[..., 3] == inf).all() and (even[..., 77] == -inf).all() and (even[..., 50] == inf).all()
+        assert torch.isnan(even[..., 9]).all() and (odd[..., 9] == -inf).all()
+        for part in (even, odd):
+            assert torch.isnan(part[..., 20]).all() and (part[..., 100] == -inf).all() and (part[..., 60] == inf).all()
+        eps = torch.finfo(t).eps
+        for h in range(2):
+            got = out[:, h * G:(h + 1) * G].numpy()
+            ref, mag, top = O.paged_attn(q[:, h * G:(h + 1) * G].double().numpy(), Kr[0][h].double().numpy(),
+                                         Vr[0][h].double().numpy(), n, G, 1 / np.sqrt(D), first=first)
+            # the tolerance above; head 0's scores reach some hundreds, whose fp32 error its last term counts
+            tol = eps / 2 * np.abs(ref) + mag * ((eps / 2 if new * G > 32 else eps * eps) + 64 * 2.0 ** -24 +
+                                                 2 * (D + 8) * 2.0 ** -24 * top[..., None]) * (1 + eps) + 2.0 ** -25
+            on = np.ones((new, G, D), bool)
+            if h == 0:
+                on[:, :, [9, 20, 60, 100]] = False
+                on[0::2, :, [3, 50, 77]] = False
+            err = np.abs(np.where(on, got, ref) - ref)
+            assert (err <= tol).all(), (seed, h)
+
+
+def test_sparse_and_dense_agree_on_infinities():
+    """One token over all of its rows, dense and selected: infinities come out alike."""
+    rng = np.random.default_rng(44)
+    n = 96
+    table, K, V, _, _ = pools(rng, [n], 1, 16, torch.float16)
+    for i, c in ((0, 1), (40, 2), (95, 3)):
+        V[int(table[0, i // 16]), 0, i % 16, c] = float("inf")
+    q = torch.from_numpy(rng.standard_normal((1, 4, D)).astype(np.float32)).half().to(DEV)
+    idx = torch.arange(n, dtype=torch.int32, device=DEV).expand(1, 4, n).contiguous()
+    a = F.fathom_paged_attn(q, K, V, table, i64([0, 1]), i64([n]), 1).float()
+    b = F.fathom_paged_sparse_attn(q, K, V, table, i64([n]), idx)
+    assert torch.equal(torch.isinf(a), torch.isinf(b)) and torch.isinf(a[..., 1:4]).all()
