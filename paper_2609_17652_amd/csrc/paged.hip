@@ -304,7 +304,7 @@ __global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(WriteArgs a)
   const void* src = v_side ? a.V : a.K;
   uint16_t* dst = v_side ? a.Vp : a.Kp;
   const int64_t ls_tok = v_side ? a.ldv_tok : a.ldk_tok, ls_head = v_side ? a.ldv_head : a.ldk_head;
-  const uint32_t r = blockIdx.x * (uint32_t)(kWriteThreads / 16) + g;
+  const uint32_t r = (blockIdx.z * gridDim.x + blockIdx.x) * (uint32_t)(kWriteThreads / 16) + g;
   if (r >= a.rows) return;
   const uint32_t t = r / (uint32_t)a.H, h = r - t * (uint32_t)a.H;
   const int64_t slot = a.slots[t], o = (int64_t)t * ls_tok + (int64_t)h * ls_head + 8 * x;
@@ -336,7 +336,10 @@ fathom_status launch_paged_write(const void* K, const void* V, fathom_dtype sdt,
   const WriteArgs a = {K, V, ldk_tok, ldk_head, ldv_tok, ldv_head, slots, (uint32_t)(T * p.H),
                        reinterpret_cast<uint16_t*>(p.K), reinterpret_cast<uint16_t*>(p.V), p.H, shift, p.P << shift,
                        p.ld_page, p.ld_head, p.ld_tok, st};
-  const dim3 grid((a.rows + kWriteThreads / 16 - 1) / (kWriteThreads / 16), 2), threads(kWriteThreads);
+  // an axis of a grid has fewer than 2^32 threads: beyond 2^22 groups of rows a second one goes on
+  const uint32_t groups = (a.rows + kWriteThreads / 16 - 1) / (kWriteThreads / 16), wide = 1u << 22;
+  const uint32_t deep = (groups + wide - 1) / wide;
+  const dim3 grid(deep > 1 ? wide : groups, 2, deep), threads(kWriteThreads);
   if (sdt != FATHOM_F32) hipLaunchKernelGGL((paged_write_kernel<false, false>), grid, threads, 0, s, a);
   else if (p.dt == FATHOM_BF16) hipLaunchKernelGGL((paged_write_kernel<true, true>), grid, threads, 0, s, a);
   else hipLaunchKernelGGL((paged_write_kernel<true, false>), grid, threads, 0, s, a);

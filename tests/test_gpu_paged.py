@@ -1032,3 +1032,21 @@ def test_sparse_and_dense_agree_on_infinities():
     a = F.fathom_paged_attn(q, K, V, table, i64([0, 1]), i64([n]), 1).float()
     b = F.fathom_paged_sparse_attn(q, K, V, table, i64([n]), idx)
     assert torch.equal(torch.isinf(a), torch.isinf(b)) and torch.isinf(a[..., 1:4]).all()
+
+
+def test_write_up_to_its_limit_of_rows():
+    """2^28 rows and more (of one source row, stride 0): more threads than a grid's axis counts."""
+    H, page, P = 1024, 16, 3
+    K, V = (torch.zeros((P, H, page, D), dtype=torch.float16, device=DEV) for _ in range(2))
+    x = torch.arange(D, dtype=torch.float32, device=DEV).half()
+    for T in ((1 << 18), (1 << 18) + 5, 1 << 20):
+        K.zero_(), V.zero_()
+        slots = torch.full((T,), -1, dtype=torch.int64, device=DEV)
+        at = {0: 3, T // 2: 17, T - 1: P * page - 1}
+        for i, s in at.items():
+            slots[i] = s
+        F.fathom_paged_write(x.expand(T, H, D), (2 * x).expand(T, H, D), slots, K, V)
+        for pool, want in ((K, x), (V, 2 * x)):
+            rows = pool.transpose(1, 2).reshape(P * page, H, D)
+            for s in range(P * page):
+                assert (rows[s] == (want if s in at.values() else 0 * want)).all(), (T, s)
