@@ -393,7 +393,12 @@ typedef struct {
  * slots are -1: with PAGES_SHORT from the first request on whose pages exceed
  * those left (and all after it that need pages); with BAD_N where it has rows that
  * end past T.  Lengths outside [0, ld_table*page]: BAD_N, no rows, n_now = n_old, or
- * 0 where n_old is outside.
+ * 0 where n_old is outside.  start counts the rows of a request that is not served all
+ * the same: fathom_paged_write skips them, but fathom_paged_attn, given n_now, takes
+ * them for the last of its n_old tokens (or, more than n_old, leaves them with BAD_N).
+ * What it writes for the rows of a request with n_now[s] != n[s] means nothing: after
+ * PAGES_SHORT or BAD_N a caller (with n_now apart from n) drops those rows.  The others
+ * are not affected.
  *
  *   n_old, n  [S] int64 (device).      table [S][ld_table] int32 (device, updated).
  *   ring      [P] int32 (device, updated): the free pages are ring[(head + i) % P],

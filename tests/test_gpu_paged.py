@@ -1050,3 +1050,65 @@ def test_write_up_to_its_limit_of_rows():
             rows = pool.transpose(1, 2).reshape(P * page, H, D)
             for s in range(P * page):
                 assert (rows[s] == (want if s in at.values() else 0 * want)).all(), (T, s)
+
+
+# ---------------------------------------------------------------- map, more
+@pytest.mark.parametrize("S,page,L", [(3, 16, 5), (64, 32, 9), (300, 16, 40), (1500, 64, 20)])
+@pytest.mark.parametrize("alias", ["n", "n and state", "n_old"])
+def test_map_in_place_of_its_inputs(S, page, L, alias):
+    """n_now may be n or n_old, state_out may be state: the same results, in one workgroup and in two launches."""
+    rng = np.random.default_rng(S + 1)
+    n_old, n, table, ring, state, T = random_map(rng, S, page, L, 3, 4)
+    want = O.paged_map(n_old, n, page, table, ring, state, T, 2)
+    t, r, st = torch.from_numpy(table).to(DEV), torch.from_numpy(ring).to(DEV), F.new_status()
+    a, b, s0 = i64(n_old), i64(n), i64(state)
+    kw = dict(n_now=a if alias == "n_old" else b)
+    if "state" in alias:
+        kw["state_out"] = s0
+    got = F.fathom_paged_map(a, b, page, t, r, s0, T, 2, dev_status=st, **kw)
+    for name, g, w in zip(("table", "ring", "slots", "start", "n_now", "n_unit", "state"), (t, r, *got), want):
+        assert np.array_equal(g.cpu().numpy(), w), name
+    assert status(st) == (F.FATHOM_DEV_PAGES_SHORT if want[7] else 0) | (F.FATHOM_DEV_BAD_N if want[8] else 0)
+
+
+def test_a_step_with_too_few_pages():
+    """The ring runs dry in the middle of a step: requests that are served come out right, the rows of one that is not are
+    the last of its old tokens to the attention, or left where it has fewer, and what is cached stays as it was."""
+    rng = np.random.default_rng(37)
+    H, G, page, L = 2, 4, 16, 12
+    old, new = [40, 30, 5, 64, 50], [12, 40, 30, 1, 20]  # two free pages: request 0 takes one, request 1 wants three
+    n = [a + b for a, b in zip(old, new)]
+    table, K, V, Kr, Vr = pools(rng, old, H, page, torch.float16, spare=2)
+    table = torch.cat([table, torch.full((5, L - table.shape[1]), -1, dtype=torch.int32, device=DEV)], 1)
+    P = K.shape[0]
+    free = sorted(set(range(P)) - set(table[table >= 0].tolist()))
+    ring = torch.tensor(free + [-1] * (P - len(free)), dtype=torch.int32, device=DEV)
+    T, st = sum(new), F.new_status()
+    rows = [torch.from_numpy(rng.standard_normal((T, m, D)).astype(np.float32)).half() for m in (H * G, H, H)]
+    slots, start, now, _, state = F.fathom_paged_map(i64(old), i64(n), page, table, ring, i64([0, len(free)]), T, H,
+                                                     dev_status=st)
+    assert status(st) == F.FATHOM_DEV_PAGES_SHORT
+    served = (now == i64(n)).tolist()  # how a caller tells them
+    assert served == [True, False, False, False, False]
+    assert start.tolist() == [0, *np.cumsum(new).tolist()] and now.tolist() == [52, 30, 5, 64, 50]
+    before = K.clone(), V.clone()
+    F.fathom_paged_write(rows[1].to(DEV), rows[2].to(DEV), slots, K, V, dev_status=st)
+    out = torch.full((T, H * G, D), 5.0, dtype=torch.float16, device=DEV)
+    F.fathom_paged_attn(rows[0].to(DEV), K, V, table, start, now, max(new), out=out, dev_status=st)
+    assert status(st) == F.FATHOM_DEV_PAGES_SHORT | F.FATHOM_DEV_BAD_N  # requests 1 and 2 have more rows than tokens
+    for s in range(5):
+        a, b = sum(new[:s]), sum(new[:s + 1])
+        if not served[s] and new[s] > old[s]:
+            assert (out[a:b] == 5.0).all()
+            continue
+        for h in range(H):
+            kv = [x[s][h] for x in (Kr, Vr)]
+            if served[s]:
+                kv = [torch.cat([x, y[a:b, h]]) for x, y in zip(kv, rows[1:])]
+            heads = slice(h * G, (h + 1) * G)
+            m = n[s] if served[s] else old[s]
+            assert close(out[a:b, heads], rows[0][a:b, heads], *kv, m, G, new[s] * G > 32), (s, h)
+    taken = sorted({int(x) // page for x in slots.tolist() if x >= 0})
+    kept = [p for p in range(P) if p not in taken]
+    for x, y in zip(before, (K, V)):
+        assert torch.equal(x[kept].nan_to_num(9.0), y[kept].nan_to_num(9.0))
