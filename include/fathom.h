@@ -476,7 +476,8 @@ fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fa
  *   is above -Inf).
  * Rows outside what a token sees do not enter its result, whatever they hold.  A value of V
  * that is not finite reaches every token that sees its row, however small its probability:
- * Inf as Inf, Inf of both signs and NaN as NaN.
+ * Inf as Inf, Inf of both signs and NaN as NaN.  The largest z_j that a token sees is at most
+ * 2^25 in magnitude (where the steps of a score in fp32 are 2; smaller ones may be anything).
  *
  *   q        [T][H*G][D] of the pages' type, row (i, hg) at q[i*ldq_tok + hg*ldq_head];
  *            16-byte aligned, strides >= 0 and multiples of 8 elements.

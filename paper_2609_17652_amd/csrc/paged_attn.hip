@@ -654,11 +654,12 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
 #pragma unroll
           for (int c = 0; c < 8; ++c) o[t][c] *= f;
         }
-        const float ref = m[t] == -__builtin_huge_valf() ? 0.0f : m[t] - Mx<BF>::kShift;
+        const float ref = m[t] == -__builtin_huge_valf() ? 0.0f : m[t];
         float sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float x = __builtin_amdgcn_exp2f(z[e] - ref);
+          // (the shift after the difference: m less the shift would be rounded, by 8 and more of large scores)
+          const float x = __builtin_amdgcn_exp2f((z[e] - ref) + Mx<BF>::kShift);
           sum += x;
           const typename Mx<BF>::t xh = (typename Mx<BF>::t)x;
           ph[t][e] = xh;
@@ -1288,7 +1289,8 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
   auto raise = [&](float& f) INLINE -> bool {
     if (!__ballot(__builtin_fmaf(mx, c1, nr) > kSlack + Mx<BF>::kShift)) return false;
     const float top = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-    const float to = fminf(nr, Mx<BF>::kShift - top * c1);
+    // scores far from 0 round it: downwards, or the probabilities taken against it overflow
+    const float at = __builtin_fmaf(-top, c1, Mx<BF>::kShift), to = fminf(nr, __builtin_fmaf(fabsf(at), -0x1p-23f, at));
     f = __builtin_amdgcn_exp2f(to - nr);
     nr = to;
     l *= f;

@@ -1112,3 +1112,30 @@ def test_a_step_with_too_few_pages():
     kept = [p for p in range(P) if p not in taken]
     for x, y in zip(before, (K, V)):
         assert torch.equal(x[kept].nan_to_num(9.0), y[kept].nan_to_num(9.0))
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("slope", [2.0 ** 16, 2.0 ** 20, 1e6])
+def test_attn_bias_that_leaves_one_key(slope, new, dt):
+    """Scores of far keys of -10^9 and below: the probabilities taken against them stay finite, and a token is left with its
+    own key."""
+    rng = np.random.default_rng(33)
+    n, t = 20000, TYPES[dt]
+    table, K, V, _, Vr = pools(rng, [n], 1, 64, t)
+    q = torch.from_numpy(rng.standard_normal((new, 2, D)).astype(np.float32)).to(t).to(DEV)
+    out = F.fathom_paged_attn(q, K, V, table, i64([0, new]), i64([n]), new,
+                              slopes=torch.full((2,), slope, dtype=torch.float32, device=DEV)).cpu()
+    assert torch.equal(out, Vr[0][0, n - new:, None].expand(new, 2, D))
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_attn_large_scores(new):
+    """One key's score is 2^25, the others' some tens: it is all that counts."""
+    rng = np.random.default_rng(34)
+    n = 300
+    table, K, V, Kr, Vr = pools(rng, [n], 1, 16, torch.float16, scale=0.01)
+    K[int(table[0, 100 // 16]), 0, 100 % 16] = 1024.0
+    q = torch.full((new, 2, D), 1024.0, dtype=torch.float16, device=DEV)
+    out = F.fathom_paged_attn(q, K, V, table, i64([0, new]), i64([n]), new, sm_scale=0.25).cpu()
+    assert torch.equal(out, Vr[0][0, 100].expand(new, 2, D))
