@@ -360,7 +360,7 @@ fathom_status fathom_klt_rotate_q(const void* q, fathom_dtype qdt, int U, int G,
  * request s, and query heads h*G .. h*G + G - 1 of a request are its G heads.
  *
  * All calls: page a power of two in 16 .. 1024; 1 <= H <= 1024; S <=
- * FATHOM_MAX_SEQS; ld_table*page < 2^31; K and V 16-byte aligned with strides
+ * FATHOM_MAX_SEQS; ld_table*page <= 2^31 - 1024; K and V 16-byte aligned with strides
  * that are multiples of 8 elements, ld_tok in [D, 2^20]; dt FATHOM_F16 or
  * FATHOM_BF16.  Outside these: FATHOM_ERR_UNSUPPORTED for sizes and types,
  * FATHOM_ERR_INVALID for pointers and strides.

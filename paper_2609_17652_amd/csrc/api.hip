@@ -77,7 +77,7 @@ fathom_status check_pages(const fathom_pages* p, int D, bool v, const int32_t* t
   if (D != kD || (p->dt != FATHOM_F16 && p->dt != FATHOM_BF16)) return FATHOM_ERR_UNSUPPORTED;
   if (S > kMaxSeqs || p->H < 1 || p->H > 1024) return FATHOM_ERR_UNSUPPORTED;
   if (p->page < 16 || p->page > 1024 || (p->page & (p->page - 1))) return FATHOM_ERR_UNSUPPORTED;
-  if (p->P > 0x7fffffff || ld_table > 0x7fffffff / p->page) return FATHOM_ERR_UNSUPPORTED;
+  if (p->P > 0x7fffffff || ld_table > kMaxTokens / p->page) return FATHOM_ERR_UNSUPPORTED;
   if (p->ld_tok > ((int64_t)1 << 20)) return FATHOM_ERR_UNSUPPORTED;
   if (p->ld_tok < D || p->ld_head < 0 || p->ld_page < 0) return FATHOM_ERR_INVALID;
   if ((p->ld_tok | p->ld_head | p->ld_page) & 7) return FATHOM_ERR_INVALID;
@@ -337,7 +337,7 @@ fathom_status fathom_paged_map(const int64_t* n_old, const int64_t* n, int S, in
   if (S < 0 || ld_table < 0 || P < 0 || T < 0) return FATHOM_ERR_INVALID;
   if (S > kMaxSeqs || H < 1 || H > 1024) return FATHOM_ERR_UNSUPPORTED;
   if (page < 16 || page > 1024 || (page & (page - 1))) return FATHOM_ERR_UNSUPPORTED;
-  if (P > 0x7fffffff || T > 0x7fffffff || ld_table > 0x7fffffff / page) return FATHOM_ERR_UNSUPPORTED;
+  if (P > 0x7fffffff || T > 0x7fffffff || ld_table > kMaxTokens / page) return FATHOM_ERR_UNSUPPORTED;
   if (!state || !start || !state_out) return FATHOM_ERR_INVALID;
   if (S > 0 && (!n_old || !n || !n_now)) return FATHOM_ERR_INVALID;
   if ((S > 0 && ld_table > 0 && !table) || (P > 0 && !ring) || (T > 0 && !slots)) return FATHOM_ERR_INVALID;

@@ -6,6 +6,8 @@
 namespace fathom {
 
 constexpr int kMaxSeqs = FATHOM_MAX_SEQS;
+// Positions of a request at most: those of some blocks behind the last are still 32-bit numbers.
+constexpr int64_t kMaxTokens = 0x7fffffff - 1023;
 
 // Pages with the block tables of a call's requests.  page = 1 << shift.
 struct Paged {

@@ -1184,8 +1184,8 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
   hi_min = uniform(hi_min);
   // ---- absent pages among the keys: all blocks count as masked then ----
   {
-    const int e1 = min(key0 + nb * kBlock, n);
-    for (int k = key0 + 16 * tid; k < e1; k += 16 * 256)
+    const uint32_t e1 = min(key0 + nb * kBlock, n);  // (a step behind it may pass 2^31)
+    for (uint32_t k = (uint32_t)key0 + 16u * (uint32_t)tid; k < e1; k += 16 * 256)
       absent |= (uint32_t)page_of(p.c, t.s, k >> p.c.shift) >= (uint32_t)p.c.P;
     const bool any = __ballot(absent) != 0;
     if (lane == 0) red[wave] = any;

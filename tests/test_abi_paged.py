@@ -185,3 +185,19 @@ def test_packed_pages_are_the_structure(fl):
     pg, H, D = fl._pages(K, None)
     want = fl._Pages(K.data_ptr(), None, fl.FATHOM_F16, 2, 16, 3, 4096, 2048, 128)
     assert pg == bytes(want) and (H, D) == (2, 128)
+
+
+@pytest.mark.parametrize("page", [16, 64, 1024])
+def test_positions_leave_room_in_32_bits(fl, page):
+    """2^31 - 1024 positions a request are the most, for every call that takes a table; blocks behind the last are counted
+    beyond."""
+    most = ((1 << 31) - 1024) // page
+    L, pg = fl.lib(), _pg(fl, page=page)
+    for ld, want in ((most, 0), (most + 1, fl.FATHOM_ERR_UNSUPPORTED)):
+        assert _attn(fl, pg, ld_table=ld, T=0) == want
+        assert L.fathom_paged_pack(C.byref(pg), FAKE, ld, None, FAKE, 0, 0, 128, 4, FAKE, FAKE, None, S0) == want
+        assert L.fathom_paged_sparse_attn(FAKE, 0, C.byref(pg), FAKE, ld, FAKE, 0, 4, 128, FAKE, 8, 4, 32, C.c_float(1.0),
+                                          FAKE, FAKE, 1 << 20, None, S0) == want
+        # (without its lengths: refused for them where the table is not)
+        assert L.fathom_paged_map(None, FAKE, 1, 1, page, FAKE, ld, FAKE, 8, FAKE, FAKE, 4, FAKE, FAKE, None, FAKE, None,
+                                  S0) == (want or fl.FATHOM_ERR_INVALID)
