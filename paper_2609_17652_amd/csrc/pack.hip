@@ -511,7 +511,7 @@ static void launch_pack_t(const Keys& keys, const int64_t* n, const int64_t* n_o
   using P = PackItem<typename Keys::Key>;
   // append: new tokens span at most ceil(max_new / 64) + 1 blocks per unit
   int64_t mb = nb_cap;
-  if (n_old) {
+  if (n_old && max_new / kBlockTokens < nb_cap) {  // (max_new may be as large as its type)
     mb = (max_new + kBlockTokens - 1) / kBlockTokens + 1;
     if (mb > nb_cap) mb = nb_cap;
   }

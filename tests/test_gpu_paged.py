@@ -1139,3 +1139,24 @@ def test_attn_large_scores(new):
     q = torch.full((new, 2, D), 1024.0, dtype=torch.float16, device=DEV)
     out = F.fathom_paged_attn(q, K, V, table, i64([0, new]), i64([n]), new, sm_scale=0.25).cpu()
     assert torch.equal(out, Vr[0][0, 100].expand(new, 2, D))
+
+
+@pytest.mark.parametrize("max_new", [64, 1 << 40, (1 << 63) - 1])
+def test_pack_append_under_any_bound(max_new):
+    """max_new is a bound on new tokens, however large: paged or not, the store grows by what there is."""
+    rng = np.random.default_rng(38)
+    lengths, H = [500, 129], 2
+    table, K, _, Kr, _ = pools(rng, lengths, H, 16, torch.float16)
+    flat = torch.zeros((4, 500, D))
+    for s, n in enumerate(lengths):
+        flat[2 * s:2 * s + 2, :n] = Kr[s].float()
+    flat, n, st = flat.to(DEV), i64(lengths), F.new_status()
+    nu = n.repeat_interleave(H)
+    want = F.fathom_pack(flat, nu)
+    for call in ("paged", "fp32", "fp16"):
+        p, s = F.fathom_pack(flat, nu - 50)
+        if call == "paged":
+            F.fathom_paged_pack(K, table, n, p, s, n - 50, max_new, dev_status=st)
+        else:
+            F.fathom_pack_append(flat if call == "fp32" else flat.half(), nu - 50, nu, max_new, p, s, dev_status=st)
+        assert torch.equal(p, want[0]) and torch.equal(s, want[1]) and status(st) == 0, call
