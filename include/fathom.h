@@ -494,9 +494,10 @@ fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fa
  *            sees, later ones among them.
  *   first    [T] int64 or NULL: the first position that a token sees (the start of
  *            its document).
- *   out      [T][H*G][D] of the pages' type, contiguous, 16-byte aligned.
+ *   out      [T][H*G][D] of the pages' type, contiguous, 16-byte aligned; it overlaps
+ *            no input.
  *   ws       device workspace of at least fathom_paged_attn_workspace_size(T, S,
- *            H, G, max_new) bytes, 256-byte aligned (any contents).
+ *            H, G, max_new) bytes, 256-byte aligned (any contents), for one call at a time.
  * Scores, softmax statistics and sums are fp32; the probabilities of chunks (more
  * than 32 query rows, new*G, of a request, or of a call's only request, more than 32 that
  * T and max_new allow) are rounded to the pages' type once, those of fewer rows enter as a
@@ -505,7 +506,7 @@ fathom_status fathom_paged_sparse_attn(const void* q, fathom_dtype qdt, const fa
  * S*ld_table*page <= 2^35.
  * Device status: BAD_N (n outside [0, ld_table*page], more new tokens than n or than
  * max_new, a start out of order or outside [0, T]: that request's rows are left as
- * they were), BAD_PAGE.
+ * they were), BAD_PAGE.  With S, T or max_new 0 nothing is launched and no status raised.
  */
 fathom_status fathom_paged_attn(const void* q, int64_t ldq_tok, int64_t ldq_head,
                                 const fathom_pages* pages, const int32_t* table, int64_t ld_table,
