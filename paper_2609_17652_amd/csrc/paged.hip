@@ -13,7 +13,7 @@
 // sums (16 bytes a request from L2); the first of them writes lengths and state, or, where
 // the caller's are in place and the others still read them, a second launch does.  Bound by
 // latency: launch, lengths, sums, then a search and two trips to memory a slot; 64 requests' one
-// token 4.8 us, 450000 slots of 512 requests 15.6 (two launches and slots one request after
+// token 4.4 us, 450000 slots of 512 requests 15.9 (two launches and slots one request after
 // another: 13 and 23; pages moved by the threads that have slots: 18).
 //
 // Write.  A copy of rows: 16 lanes take a row's 256 bytes of output, the row's
@@ -251,7 +251,7 @@ fathom_status launch_paged_map(const int64_t* n_old, const int64_t* n, int S, in
                                uint32_t* st, hipStream_t s) {
   const MapArgs a = {n_old, n,     S, H,     shift, table, ld_table, ring, P,
                      state, slots, T, start, n_now, n_unit, state_out, st};
-  // A step that moves few tokens is one small workgroup (64 requests' one token 4.8 us, 6.7 in a
+  // A step that moves few tokens is one small workgroup (launch after launch: 64 requests' one token 4.8 us, 6.7 in a
   // large one; 462 tokens 6.7 and 7.2; 538 8.7 and 7.9); else a slot a thread, over two
   // workgroups a CU at most, all writing what they find (1811 tokens 7.5 us, 13.6 in one
   // workgroup).  (Pages taken are bounded by the new tokens; pages that come back are not, but a

@@ -22,7 +22,7 @@
 // lengths are; each wave runs its share through two private LDS stages without
 // meeting the others, and pieces of a request join in attn_join_kernel.
 // attn_many_kernel takes the others, and a request that is the only one of a call whose bounds
-// allow more rows, 128 query rows a workgroup, bound by the matrix cores; keys are
+// allow more rows, 128 query rows a workgroup, bound by issue and power; keys are
 // split over workgroups where the tiles are few.
 //
 // Rows that a query must not see get a probability of 0, but 0 * Inf is not 0:
@@ -1066,8 +1066,15 @@ __device__ __forceinline__ int parts_of(const PagedAttnArgs& p, int units) {
 // sums, and Mx::kShift leaves room for it in the probabilities), so the sums are rarely
 // rescaled.
 //
-// Bound by the matrix cores' power: 2048 tokens over 65536 take 2.0 to 2.3 ms (as cards
-// differ), 1.0 to 1.1 PFLOP/s, where a large matrix product of this type reaches 1.2; with
+// Probabilities are rounded to the pages' type once (attn_few_kernel keeps them as a sum of two):
+// what is lost would take a second product with V, half as many matrix instructions again.
+// Against 64 bits the bf16 output is off by 2.0e-3 of its size there, and by 1.7e-3, its own
+// rounding, with probabilities of 32 bits.
+//
+// Bound by the power that the card allows and by issue: 2048 tokens over 65536 take 2.0 to 2.3
+// ms (as cards differ), 0.96 to 1.1 PFLOP/s, where a large matrix product of this type reaches
+// 1.2.  The clock falls to 1.7 GHz (2.2 and more where the matrix cores are mostly idle); in its
+// cycles the matrix cores are busy to 51 % and vector instructions issue in 47 %.  With
 // neither exponentials nor LDS reads the same instructions take 1.75 ms.  64 rows a wave and
 // one workgroup a CU need half of the LDS reads and are up to 5 % faster there, and slower where
 // tiles are short (6 requests of documents 303 us against 188).
