@@ -385,7 +385,8 @@ typedef struct {
  *   of the ring of free pages, in the order of s, into table[s][pages(n_old) ..];
  *   requests that shrink return table[s][pages(n) .. pages(n_old)) to its end,
  *   in the order of s (the entries are left as they were).  Pages returned by
- *   a call are taken by later calls only.
+ *   a call are taken by later calls only.  Who uses a page is not counted: one that several
+ *   tables list is returned by each request that lets it go, which a caller prevents.
  *   slots[start[s] + i] = table[s][p / page]*page + p % page, p = n_old[s] + i;
  *               every other slot below T is -1.
  *   n_now[s]  = n[s], and n_unit[s*H + h] = n_now[s] for the per-unit calls.
