@@ -251,8 +251,8 @@ fathom_status launch_paged_map(const int64_t* n_old, const int64_t* n, int S, in
                                uint32_t* st, hipStream_t s) {
   const MapArgs a = {n_old, n,     S, H,     shift, table, ld_table, ring, P,
                      state, slots, T, start, n_now, n_unit, state_out, st};
-  // A step that moves few tokens is one small workgroup (launch after launch: 64 requests' one token 4.8 us, 6.7 in a
-  // large one; 462 tokens 6.7 and 7.2; 538 8.7 and 7.9); else a slot a thread, over two
+  // A step that moves few tokens is one small workgroup (launch after launch: 64 requests' one
+  // token 4.8 us, 6.7 in a large one; 462 tokens 6.7 and 7.2; 538 8.7 and 7.9); else a slot a thread, over two
   // workgroups a CU at most, all writing what they find (1811 tokens 7.5 us, 13.6 in one
   // workgroup).  (Pages taken are bounded by the new tokens; pages that come back are not, but a
   // workgroup moves 1000 in about a microsecond.)

@@ -314,7 +314,8 @@ __device__ __forceinline__ float with_nonfinite(float o, short x, uint64_t& foun
 // there), against the maximum M; where `o`, that sum, is not finite the parts are added again,
 // and what is not finite in a part is kept where its weight is 0.
 template <class At>
-__device__ __forceinline__ f32x4 parts_sum(const PagedAttnArgs& p, f32x4 o, int first, int step, int count, float M, At at) {
+__device__ __forceinline__ f32x4 parts_sum(const PagedAttnArgs& p, f32x4 o, int first, int step, int count, float M,
+                                           At at) {
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f}, z = o * zero;
   if ((z[0] + z[1]) + (z[2] + z[3]) == 0.0f) return o;
   o = zero;
@@ -739,7 +740,8 @@ __global__ __launch_bounds__(kFewWaves * kWave, 1) void attn_few_kernel(PagedAtt
           for (int t = 0; t < CT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (k >= lo[t] && k < hi[t]) o[t][c][e] = with_nonfinite<BF>(o[t][c][e], x[e], found, 32 * t + 4 * c + e);
+              if (k >= lo[t] && k < hi[t])
+                o[t][c][e] = with_nonfinite<BF>(o[t][c][e], x[e], found, 32 * t + 4 * c + e);
         }
       });
     }
@@ -1297,7 +1299,8 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
     if (!__ballot(__builtin_fmaf(mx, c1, nr) > kSlack + Mx<BF>::kShift)) return false;
     const float top = fmaxf(mx, __shfl_xor(mx, 32, kWave));
     // scores far from 0 round it: downwards, or the probabilities taken against it overflow
-    const float at = __builtin_fmaf(-top, c1, Mx<BF>::kShift), to = fminf(nr, __builtin_fmaf(fabsf(at), -0x1p-23f, at));
+    const float at = __builtin_fmaf(-top, c1, Mx<BF>::kShift);
+    const float to = fminf(nr, __builtin_fmaf(fabsf(at), -0x1p-23f, at));
     f = __builtin_amdgcn_exp2f(to - nr);
     nr = to;
     l *= f;
@@ -1485,8 +1488,10 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(PagedAttnArgs p) {
         for (int y = 0; y < 16; ++y) {
           const s16x4 x = *reinterpret_cast<const s16x4*>(row + 8 * y + 4 * half);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (k >= lo && k < hi) o[y >> 2][4 * (y & 3) + e] = with_nonfinite<BF>(o[y >> 2][4 * (y & 3) + e], x[e], found, 4 * y + e);
+          for (int e = 0; e < 4; ++e) {
+            const int i = 4 * (y & 3) + e;
+            if (k >= lo && k < hi) o[y >> 2][i] = with_nonfinite<BF>(o[y >> 2][i], x[e], found, 4 * y + e);
+          }
         }
       });
     }
